@@ -271,8 +271,9 @@ QF_API qf_status qf_grouped_saved_size(const qf_grouped_desc* d, size_t* bytes);
 /*
  * qf_qlinear_grouped_fwd -- for every expert e, rows [off[e], off[e+1]) of X:
  *   Y_e = A_hat_e W_hat_e^T with W_hat_e = Q^-1(Q(W[e])), one tensor scale per expert.
- *   group_offsets: DEVICE int64 [E+1], non-decreasing, off[0] = 0, off[E] = T (the host never
- *   reads it).  X bf16 [T, K], W bf16 [E, N, K], Y bf16 [T, N].
+ *   group_offsets: DEVICE int64 [E+1], non-decreasing, off[0] = 0, off[E] <= T (the host never
+ *   reads it).  X bf16 [T, K], W bf16 [E, N, K], Y bf16 [T, N].  Rows from off[E] on (a dispatch's
+ *   dropped slots) belong to no expert: Y and dX are left alone there and dW has nothing from them.
  *   saved: NULL, or a 256-byte aligned device buffer of qf_grouped_saved_size bytes that
  *   receives the experts' packed W_hat (written by the same quantizer launch as W_hat).
  */
@@ -615,6 +616,140 @@ typedef struct {
 QF_API qf_status qf_payload_layout_of(int fmt, int64_t N, int64_t K, qf_payload_layout* out);
 QF_API qf_status qf_payload_write_header(int fmt, int64_t N, int64_t K, void* payload,
                                          qf_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Around the grouped layer: the router, the sort by expert and the weighted sum back (Sec. 3.3
+ * "Mixture-of-experts adaptation"; the router itself stays unquantized).  With T tokens, E experts
+ * and k choices a token, slot (t, j) is choice j of token t, flat index t k + j; "grouped" rows are
+ * the slots sorted by expert, the order of the grouped layer above.
+ * Limits: E <= 1024, 1 <= k <= min(E, 64), T k < 2^31.
+ * ------------------------------------------------------------------------------------ */
+typedef enum { QF_SCORE_SOFTMAX = 0, QF_SCORE_SIGMOID = 1 } qf_score;
+
+/*
+ * qf_moe_route -- the k largest logits of every token and their weights.
+ *   z      bf16 (z_f32 = 0) or FP32 (z_f32 = 1) logits [T, E], row stride ldz (a multiple of 8).
+ *   mask   uint8 [T] or NULL; 0: the token (padding) chooses nothing.  No alignment needed.
+ *   ids    int32 [T, k]: the experts by falling logit, equal logits by rising expert; -1 where a
+ *          token has no further expert (masked, or every logit left is -inf).
+ *   w      FP32 [T, k]: c times
+ *            softmax, norm = 0   exp(z_j) / sum over all E of exp(z)
+ *            sigmoid, norm = 0   1 / (1 + exp(-z_j))
+ *            norm = 1            that score over the sum of the chosen ones' scores
+ *          with c = `scale`; 0 where ids is -1.
+ * Sums are FP32.  With norm = 1 the sigmoid's ratios are formed from its logarithm, so they stay
+ * right where every score underflows.  A NaN logit ranks above +inf; the weights of a softmax row
+ * whose largest logit is NaN or +inf are NaN.
+ */
+QF_API qf_status qf_moe_route(const void* z, int z_f32, int64_t T, int64_t E, int64_t ldz, int64_t k,
+                              int score, int norm, float scale, const uint8_t* mask, int32_t* ids,
+                              float* w, qf_stream_t stream);
+
+/*
+ * qf_moe_route_bwd -- dz [T, E] (the type of z, row stride lddz; overwritten) from dw FP32 [T, k]:
+ * the gradient of qf_moe_route's w with the choice held fixed, zero for experts not chosen except
+ * with unnormalized softmax.  z, score, norm, scale as in the forward, ids as it wrote them (an id
+ * outside 0 .. E - 1 is no choice; its dw is not used).
+ */
+QF_API qf_status qf_moe_route_bwd(const void* z, int z_f32, int64_t T, int64_t E, int64_t ldz,
+                                  int64_t k, int score, int norm, float scale, const int32_t* ids,
+                                  const float* dw, void* dz, int64_t lddz, qf_stream_t stream);
+
+/*
+ * qf_moe_dispatch -- stable sort of the slots by expert and, with X, the tokens' rows copied into
+ * that order.
+ *   ids      int32 [T, k]; a value outside 0 .. E - 1 drops the slot.
+ *   offsets  int64 [E + 1]: expert e's rows are offsets[e] .. offsets[e + 1] - 1, as the grouped
+ *            calls take it; offsets[E] is the number of slots that were not dropped.
+ *   row_of   int32 [T, k]: the slot's row.  Dropped slots take the rows from offsets[E] on, in slot
+ *            order, and have their row's complement ~row (negative) here.
+ *   slot_of  int32 [T k]: a row's slot, -1 from row offsets[E] on.
+ *   X, Xg    bf16 [T, H] (row stride ldx) and [T k, H] (dense; H a multiple of 8), or both NULL:
+ *            Xg[row] = X[token of the row's slot], zeros from row offsets[E] on.
+ *   ws       qf_moe_dispatch_workspace_size bytes, 256-byte aligned.
+ * Deterministic.  Within an expert rows are in slot order.
+ */
+QF_API qf_status qf_moe_dispatch_workspace_size(int64_t T, int64_t E, int64_t k, size_t* bytes);
+QF_API qf_status qf_moe_dispatch(const int32_t* ids, int64_t T, int64_t E, int64_t k,
+                                 int64_t* offsets, int32_t* row_of, int32_t* slot_of,
+                                 const uint16_t* X, int64_t H, int64_t ldx, uint16_t* Xg, void* ws,
+                                 size_t ws_bytes, qf_stream_t stream);
+
+/*
+ * qf_moe_dispatch_bwd -- dX[t] = sum over j of dXg[row_of[t, j]], dropped slots left out: dX bf16
+ * [T, H] (row stride lddx; overwritten), dXg bf16 [T k, H].  FP32 sums in rising j, rounded once.
+ */
+QF_API qf_status qf_moe_dispatch_bwd(const int32_t* row_of, int64_t T, int64_t k, int64_t H,
+                                     const uint16_t* dXg, uint16_t* dX, int64_t lddx,
+                                     qf_stream_t stream);
+
+/*
+ * qf_moe_combine -- Y[t] = sum over j of w[t, j] Yg[row_of[t, j]], dropped slots left out (their
+ * rows and weights are not used): Yg bf16 [T k, H] (dense), w FP32 [T, k] or NULL (ones), Y bf16
+ * [T, H] (row stride ldy); a token with no slots left gets zeros.  FP32 sums in rising j, rounded
+ * once.  row_of as qf_moe_dispatch writes it: values r with r or ~r in 0 .. T k - 1, each row
+ * once (others are taken as dropped).
+ */
+QF_API qf_status qf_moe_combine(const int32_t* row_of, const float* w, int64_t T, int64_t k,
+                                int64_t H, const uint16_t* Yg, uint16_t* Y, int64_t ldy,
+                                qf_stream_t stream);
+
+/*
+ * qf_moe_combine_bwd -- dYg[row_of[t, j]] = w[t, j] dY[t] (bf16 [T k, H], or NULL; the rows of
+ * dropped slots get zeros) and dw[t, j] = sum over H of dY[t] Yg[row_of[t, j]] (FP32 [T, k], or
+ * NULL; 0 for dropped slots).  Yg is needed for dw only.  FP32 sums in a fixed order.
+ */
+QF_API qf_status qf_moe_combine_bwd(const int32_t* row_of, const float* w, int64_t T, int64_t k,
+                                    int64_t H, const uint16_t* dY, int64_t lddy,
+                                    const uint16_t* Yg, uint16_t* dYg, float* dw,
+                                    qf_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Products of few rows with packed weights (Sec. 3.4, 3.5: what the exported codes stand for in an
+ * engine; one token or a small batch)
+ * ------------------------------------------------------------------------------------ */
+/*
+ * A packed weight [E N, K] in the layout of the quantizers, the saved operands, the export and the
+ * payload's sections: E weights [N, K] back to back.
+ *   fmt     QF_FMT_NVFP4 (codes [E N, K/2], E4M3 scales [E N, K/16], S FP32 [E] the tensor decode
+ *           scales g / 2688), QF_FMT_MXFP4 (codes, E8M0 scales [E N, K/32]; S ignored) or
+ *           QF_FMT_Q4K (blocks [E N, K/256, 144] in codes; scales and S ignored).
+ *   K       a multiple of the format's block (16 / 32 / 256).  codes and scales 16-byte aligned.
+ */
+typedef struct {
+    int64_t E, N, K;
+    int32_t fmt;
+    const uint8_t* codes;
+    const uint8_t* scales;
+    const float* S;
+} qf_packed;
+
+/*
+ * qf_packed_matvec -- Y[M, N] = X W^T for 1 <= M <= 64 rows (M = 0: nothing; more rows: QF_ENOTSUP,
+ * use qf_gemm_packed_b) and one packed weight (w->E = 1), W exactly as its codes decode: S s_E4M3 V,
+ * 2^p V, (d s6) C - dmin m6 (Eqs. nvfp4-dequant, mxfp4-dequant, q4k-dequant).  Unlike W_hat of the
+ * layer calls no weight is rounded to bf16 first, so the result differs from theirs by up to 2^-8
+ * relative a weight (not at all for MXFP4).  FP32 accumulation in a fixed order.
+ *   X bf16 [M, K] (row stride ldx); Y bf16 (y_f32 = 0) or FP32 (y_f32 = 1) [M, N] (row stride ldy).
+ * A scale code that is NaN (E4M3 0x7F, E8M0 0xFF) makes its block's outputs NaN.
+ */
+QF_API qf_status qf_packed_matvec(const qf_packed* w, int64_t M, const uint16_t* X, int64_t ldx,
+                                  void* Y, int64_t ldy, int y_f32, qf_stream_t stream);
+
+/*
+ * qf_packed_matvec_grouped -- the same per expert: row r of Y in group_offsets[e] .. [e + 1] - 1 is
+ * X[x(r)] W_e^T, x(r) = r, or rows[r] / rows_div with `rows` (the slot_of and k of a dispatch: the
+ * token's row without a copy in expert order).  Any number of rows; meant for up to some dozens an
+ * expert.
+ *   group_offsets  DEVICE int64 [E + 1], non-decreasing, within 0 .. R; rows of Y outside
+ *                  group_offsets[0] .. [E] are left alone.  E <= 1024.
+ *   X bf16 [M, K] (row stride ldx); an x(r) outside 0 .. M - 1 counts as a row of zeros.
+ *   Y bf16 or FP32 [R, N] (row stride ldy); rows int32 [R] or NULL; rows_div >= 1.
+ */
+QF_API qf_status qf_packed_matvec_grouped(const qf_packed* w, const int64_t* group_offsets,
+                                          int64_t R, const int32_t* rows, int64_t rows_div,
+                                          int64_t M, const uint16_t* X, int64_t ldx, void* Y,
+                                          int64_t ldy, int y_f32, qf_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -21,6 +21,7 @@ FMT = {"none": 0, "nvfp4": 1, "mxfp4": 2, "q4k": 3}
 AMAX_COMPUTE, AMAX_GIVEN = 0, 1
 FLAG_REUSE_WS = 1
 FLAG_DECODE_IN_GEMM = 2
+SCORE = {"softmax": 0, "sigmoid": 1}
 STATUS = {0: "QF_OK", 1: "QF_EINVAL", 2: "QF_ESHAPE", 3: "QF_EALIGN", 4: "QF_ENOTSUP",
           5: "QF_EDEVICE"}
 
@@ -58,6 +59,12 @@ class GroupedDesc(ctypes.Structure):
     _fields_ = [("E", ctypes.c_int64), ("T", ctypes.c_int64), ("N", ctypes.c_int64),
                 ("K", ctypes.c_int64), ("wfmt", ctypes.c_int32), ("afmt", ctypes.c_int32),
                 ("w_amax", ctypes.c_void_p), ("flags", ctypes.c_uint32)]
+
+
+class Packed(ctypes.Structure):
+    _fields_ = [("E", ctypes.c_int64), ("N", ctypes.c_int64), ("K", ctypes.c_int64),
+                ("fmt", ctypes.c_int32), ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("S", ctypes.c_void_p)]
 
 
 _lib = None
@@ -150,6 +157,21 @@ def lib() -> ctypes.CDLL:
             "qf_qlinear_grouped_lora_bwd_ste": ([ctypes.POINTER(GroupedDesc), ctypes.POINTER(LoRA),
                                                  _P, _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t,
                                                  _P], ctypes.c_int),
+            "qf_moe_route": ([_P, ctypes.c_int, _I, _I, _I, _I, ctypes.c_int, ctypes.c_int,
+                              ctypes.c_float, _P, _P, _P, _P], ctypes.c_int),
+            "qf_moe_route_bwd": ([_P, ctypes.c_int, _I, _I, _I, _I, ctypes.c_int, ctypes.c_int,
+                                  ctypes.c_float, _P, _P, _P, _I, _P], ctypes.c_int),
+            "qf_moe_dispatch_workspace_size": ([_I, _I, _I, ctypes.POINTER(ctypes.c_size_t)],
+                                               ctypes.c_int),
+            "qf_moe_dispatch": ([_P, _I, _I, _I, _P, _P, _P, _P, _I, _I, _P, _P, ctypes.c_size_t,
+                                 _P], ctypes.c_int),
+            "qf_moe_dispatch_bwd": ([_P, _I, _I, _I, _P, _P, _I, _P], ctypes.c_int),
+            "qf_moe_combine": ([_P, _P, _I, _I, _I, _P, _P, _I, _P], ctypes.c_int),
+            "qf_moe_combine_bwd": ([_P, _P, _I, _I, _I, _P, _I, _P, _P, _P, _P], ctypes.c_int),
+            "qf_packed_matvec": ([ctypes.POINTER(Packed), _I, _P, _I, _P, _I, ctypes.c_int, _P],
+                                 ctypes.c_int),
+            "qf_packed_matvec_grouped": ([ctypes.POINTER(Packed), _P, _I, _P, _I, _I, _P, _I, _P, _I,
+                                          ctypes.c_int, _P], ctypes.c_int),
         }
         for name, (args, res) in sig.items():
             f = getattr(L, name)
@@ -464,6 +486,178 @@ def qlinear_grouped_lora_bwd_ste(desc, lo: LoRA, offsets, dY, X, W, dX, dA, dB, 
                                                  _ptr(offsets), _ptr(_bf16(dY)), _ptr(_bf16(X)),
                                                  _ptr(_bf16(W)), _ptr(_bf16(dX)), _ptr(dA),
                                                  _ptr(dB), _ptr(ws), ws.numel(), _stream()))
+
+
+# ---------------------------------------------------- around the grouped layer (MoE)
+def _mat(x):
+    """_rows for operands that may be empty or a single row, whose strides mean nothing."""
+    if x.dim() == 2 and (x.numel() == 0 or (x.shape[0] == 1 and (x.stride(1) == 1 or x.shape[1] == 1))):
+        return x.shape[0], x.shape[1], (x.shape[1] + 7) // 8 * 8
+    return _rows(x)
+
+
+def _typed(t, dtype, name, shape=None):
+    """t must be a contiguous tensor of the given type (and shape); None passes."""
+    if t is not None:
+        if t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        if shape is not None and tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name} must be {tuple(shape)}, not {tuple(t.shape)}")
+    return _ptr(t)
+
+
+def _logits(z):
+    T, E, ld = _mat(z)
+    if z.dtype == torch.float32:
+        return T, E, ld, 1
+    _bf16(z)
+    return T, E, ld, 0
+
+
+def moe_route(z, ids, w, score="softmax", norm=True, scale=1.0, mask=None):
+    """The ids.shape[1] largest logits of every row of z [T, E] (ids int32, w float32 [T, k])."""
+    T, E, ld, f32 = _logits(z)
+    k = ids.shape[1]
+    _check(lib().qf_moe_route(_ptr(z), f32, T, E, ld, k, SCORE[score], int(norm), float(scale),
+                              _typed(mask, torch.uint8, "mask", (T,)),
+                              _typed(ids, torch.int32, "ids", (T, k)),
+                              _typed(w, torch.float32, "w", (T, k)), _stream()))
+    return ids, w
+
+
+def moe_route_bwd(z, ids, dw, dz, score="softmax", norm=True, scale=1.0):
+    """dz [T, E], of z's type, from dw float32 [T, k] and the forward's z and ids."""
+    T, E, ld, f32 = _logits(z)
+    T2, E2, lddz, f2 = _logits(dz)
+    if (T2, E2, f2) != (T, E, f32):
+        raise ValueError("dz must have the shape and type of z")
+    k = ids.shape[1]
+    _check(lib().qf_moe_route_bwd(_ptr(z), f32, T, E, ld, k, SCORE[score], int(norm), float(scale),
+                                  _typed(ids, torch.int32, "ids", (T, k)),
+                                  _typed(dw, torch.float32, "dw", (T, k)), _ptr(dz), lddz,
+                                  _stream()))
+    return dz
+
+
+def moe_dispatch_workspace(T, E, k, device="cuda"):
+    n = ctypes.c_size_t()
+    _check(lib().qf_moe_dispatch_workspace_size(T, E, k, ctypes.byref(n)))
+    return torch.empty(max(n.value, 256), dtype=torch.uint8, device=device)
+
+
+def moe_dispatch(ids, offsets, row_of, slot_of, ws, X=None, Xg=None):
+    """Stable sort of the slots of ids [T, k] by expert (offsets int64 [E+1], row_of int32 [T, k],
+    slot_of int32 [T k]) and, with X [T, H], its rows in that order (Xg [T k, H])."""
+    T, k = ids.shape
+    H = ldx = 0
+    if X is not None and Xg is not None:
+        R, H, ldx = _mat(_bf16(X))
+        if R != T:
+            raise ValueError("X must have a row for every token")
+        _typed(_bf16(Xg), Xg.dtype, "Xg", (T * k, H))
+    _check(lib().qf_moe_dispatch(_typed(ids, torch.int32, "ids"), T, offsets.numel() - 1, k,
+                                 _typed(offsets, torch.int64, "offsets"),
+                                 _typed(row_of, torch.int32, "row_of", (T, k)),
+                                 _typed(slot_of, torch.int32, "slot_of", (T * k,)), _ptr(X), H, ldx,
+                                 _ptr(Xg), _ptr(ws), ws.numel(), _stream()))
+    return offsets, row_of, slot_of
+
+
+def _grouped_rows(g, name, T, k, H):
+    return _typed(_bf16(g), g.dtype if g is not None else None, name, (T * k, H))
+
+
+def moe_dispatch_bwd(row_of, dXg, dX):
+    """dX[t] = sum over j of dXg[row_of[t, j]]."""
+    T, k = row_of.shape
+    R, H, ld = _mat(_bf16(dX))
+    if R != T:
+        raise ValueError("dX must have a row for every token")
+    _check(lib().qf_moe_dispatch_bwd(_typed(row_of, torch.int32, "row_of"), T, k, H,
+                                     _grouped_rows(dXg, "dXg", T, k, H), _ptr(dX), ld, _stream()))
+    return dX
+
+
+def moe_combine(row_of, Yg, Y, w=None):
+    """Y[t] = sum over j of w[t, j] Yg[row_of[t, j]] (w None: ones)."""
+    T, k = row_of.shape
+    R, H, ld = _mat(_bf16(Y))
+    if R != T:
+        raise ValueError("Y must have a row for every token")
+    _check(lib().qf_moe_combine(_typed(row_of, torch.int32, "row_of"),
+                                _typed(w, torch.float32, "w", (T, k)), T, k, H,
+                                _grouped_rows(Yg, "Yg", T, k, H), _ptr(Y), ld, _stream()))
+    return Y
+
+
+def moe_combine_bwd(row_of, dY, dYg, Yg=None, w=None, dw=None):
+    """dYg[row_of[t, j]] = w[t, j] dY[t] and dw[t, j] = <dY[t], Yg[row_of[t, j]]>."""
+    T, k = row_of.shape
+    R, H, ld = _mat(_bf16(dY))
+    if R != T:
+        raise ValueError("dY must have a row for every token")
+    _check(lib().qf_moe_combine_bwd(_typed(row_of, torch.int32, "row_of"),
+                                    _typed(w, torch.float32, "w", (T, k)), T, k, H, _ptr(dY), ld,
+                                    _grouped_rows(Yg, "Yg", T, k, H),
+                                    _grouped_rows(dYg, "dYg", T, k, H),
+                                    _typed(dw, torch.float32, "dw", (T, k)), _stream()))
+
+
+# ---------------------------------------------------- few rows times packed weights
+def packed_weight(fmt, N, K, codes, scales=None, S=None, E=None) -> Packed:
+    """Descriptor of one packed weight [N, K] (E None) or of E of them back to back: codes, block
+    scales and (NVFP4) float32 tensor scales as the quantizers write them.  It holds references to
+    the tensors, so their device memory stays allocated while the descriptor is alive."""
+    n, block = (1 if E is None else E) * N, {"nvfp4": 16, "mxfp4": 32, "q4k": 256}[fmt]
+    if K % block == 0:
+        for t, name, size in ((codes, "codes", n * K // 256 * 144 if fmt == "q4k" else n * K // 2),
+                              (scales, "scales", 0 if fmt == "q4k" else n * K // block)):
+            if t is not None and size and t.numel() * t.element_size() < size:
+                raise ValueError(f"{name} holds fewer than {size} bytes")
+        if fmt == "nvfp4" and S is not None and S.numel() < (1 if E is None else E):
+            raise ValueError("S needs a tensor scale for every weight")
+    for t, name in ((codes, "codes"), (scales, "scales")):
+        if t is not None and not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+    p = Packed(1 if E is None else E, N, K, FMT[fmt], _ptr(codes), _ptr(scales),
+               _typed(S, torch.float32, "S"))
+    p._tensors = (codes, scales, S)
+    return p
+
+
+def _products(Y):
+    R, N, ld = _mat(Y)
+    if Y.dtype == torch.float32:
+        return R, N, ld, 1
+    _bf16(Y)
+    return R, N, ld, 0
+
+
+def packed_matvec(weight: Packed, X, Y):
+    """Y [M, N] (bf16 or float32) = X W^T for up to 64 rows of X."""
+    M, K, ldx = _mat(_bf16(X))
+    R, N, ldy, f32 = _products(Y)
+    if (R, N, K) != (M, weight.N, weight.K):
+        raise ValueError("X must be [M, K] and Y [M, N]")
+    _check(lib().qf_packed_matvec(ctypes.byref(weight), M, _ptr(X), ldx, _ptr(Y), ldy, f32,
+                                  _stream()))
+    return Y
+
+
+def packed_matvec_grouped(weight: Packed, offsets, X, Y, rows=None, rows_div=1):
+    """Y[r] = X[x(r)] W_e^T for r in offsets[e] .. offsets[e + 1] - 1; x(r) = r, or
+    rows[r] // rows_div (a dispatch's slot_of and k)."""
+    M, K, ldx = _mat(_bf16(X))
+    R, N, ldy, f32 = _products(Y)
+    if (N, K) != (weight.N, weight.K):
+        raise ValueError("X must be [M, K] and Y [R, N]")
+    _check(lib().qf_packed_matvec_grouped(ctypes.byref(weight),
+                                          _typed(offsets, torch.int64, "offsets", (weight.E + 1,)),
+                                          R, _typed(rows, torch.int32, "rows", (R,)), rows_div, M,
+                                          _ptr(X), ldx, _ptr(Y), ldy, f32, _stream()))
+    return Y
 
 
 # ------------------------------------------------------------------ QAD distillation loss

@@ -355,7 +355,7 @@ qf_status check_saved(const char* fn, const void* saved) {
 
 extern "C" {
 
-int qf_version(void) { return 200; }
+int qf_version(void) { return 300; }
 
 const char* qf_last_error(void) { return g_err; }
 
@@ -1661,6 +1661,203 @@ qf_status qf_dequantize_transposed(int fmt, const uint8_t* codes, const uint8_t*
   QF_TRY(check_out("qf_dequantize_transposed: codes", codes));
   QF_TRY(check_mat("qf_dequantize_transposed: out", out, K, R, ldo, true));
   QF_TRY(dev(qf::launch_dequant_t(fmt, codes, scales, Sp, R, K, out, ldo, S(stream)), fn));
+  return ok();
+}
+
+// -------------------------------------------------------- around the grouped layer (MoE)
+namespace {
+
+qf_status check_moe(const char* fn, int64_t T, int64_t E, int64_t k) {
+  if (T < 0 || E < 0) return fail(QF_ESHAPE, "%s: negative shape", fn);
+  if (E > 1024) return fail(QF_ENOTSUP, "%s: more than 1024 experts", fn);
+  if (k < 1 || k > E) return fail(QF_ESHAPE, "%s: %lld choices among %lld experts", fn, (long long)k, (long long)E);
+  if (k > 64) return fail(QF_ENOTSUP, "%s: more than 64 choices a token", fn);
+  if (T > INT32_MAX / k) return fail(QF_ENOTSUP, "%s: 2^31 slots or more", fn);
+  return QF_OK;
+}
+
+// The sum back and its gradients: rows [T k, H] in expert order against [T, H].
+qf_status check_rows(const char* fn, int64_t T, int64_t k, int64_t H, const int32_t* row_of) {
+  if (H < 0) return fail(QF_ESHAPE, "%s: negative shape", fn);
+  QF_TRY(check_moe(fn, T, 1024, k));
+  if (T > 0 && !row_of) return fail(QF_EINVAL, "%s: null row_of", fn);
+  return check_out("row_of", row_of);
+}
+
+// Logits or their gradient: [T, E] bf16 or FP32.
+qf_status check_logits(const char* name, const void* p, int64_t T, int64_t E, int64_t ld) {
+  return check_mat(name, p, T, E, ld, true);
+}
+
+qf_status check_score(const char* fn, int z_f32, int score, int norm) {
+  if ((z_f32 | norm) & ~1) return fail(QF_EINVAL, "%s: flags must be 0/1", fn);
+  if (score != QF_SCORE_SOFTMAX && score != QF_SCORE_SIGMOID) return fail(QF_EINVAL, "%s: bad score %d", fn, score);
+  return QF_OK;
+}
+
+}  // namespace
+
+qf_status qf_moe_route(const void* z, int z_f32, int64_t T, int64_t E, int64_t ldz, int64_t k,
+                       int score, int norm, float scale, const uint8_t* mask, int32_t* ids, float* w,
+                       qf_stream_t stream) {
+  const char* fn = "qf_moe_route";
+  QF_TRY(check_moe(fn, T, E, k));
+  QF_TRY(check_score(fn, z_f32, score, norm));
+  QF_TRY(check_logits("qf_moe_route: z", z, T, E, ldz));
+  if (T == 0) return ok();
+  if (!ids || !w) return fail(QF_EINVAL, "%s: null output", fn);
+  QF_TRY(check_out("qf_moe_route: ids", ids));
+  QF_TRY(check_out("qf_moe_route: w", w));
+  QF_TRY(dev(qf::launch_moe_route(z, z_f32, T, (int)E, ldz, (int)k, score, norm, scale, mask, ids, w, S(stream)), fn));
+  return ok();
+}
+
+qf_status qf_moe_route_bwd(const void* z, int z_f32, int64_t T, int64_t E, int64_t ldz, int64_t k,
+                           int score, int norm, float scale, const int32_t* ids, const float* dw,
+                           void* dz, int64_t lddz, qf_stream_t stream) {
+  const char* fn = "qf_moe_route_bwd";
+  QF_TRY(check_moe(fn, T, E, k));
+  QF_TRY(check_score(fn, z_f32, score, norm));
+  QF_TRY(check_logits("qf_moe_route_bwd: z", z, T, E, ldz));
+  QF_TRY(check_logits("qf_moe_route_bwd: dz", dz, T, E, lddz));
+  if (T == 0) return ok();
+  if (!ids || !dw) return fail(QF_EINVAL, "%s: null ids or dw", fn);
+  QF_TRY(check_out("qf_moe_route_bwd: ids", ids));
+  QF_TRY(check_out("qf_moe_route_bwd: dw", dw));
+  QF_TRY(dev(qf::launch_moe_route_bwd(z, z_f32, T, (int)E, ldz, (int)k, score, norm, scale, ids, dw, dz, lddz, S(stream)), fn));
+  return ok();
+}
+
+qf_status qf_moe_dispatch_workspace_size(int64_t T, int64_t E, int64_t k, size_t* bytes) {
+  const char* fn = "qf_moe_dispatch_workspace_size";
+  QF_TRY(check_moe(fn, T, E, k));
+  if (!bytes) return fail(QF_EINVAL, "%s: null output", fn);
+  *bytes = up(qf::moe_sort_ws_bytes(T * k, E));
+  return ok();
+}
+
+qf_status qf_moe_dispatch(const int32_t* ids, int64_t T, int64_t E, int64_t k, int64_t* offsets,
+                          int32_t* row_of, int32_t* slot_of, const uint16_t* X, int64_t H,
+                          int64_t ldx, uint16_t* Xg, void* ws, size_t ws_bytes, qf_stream_t stream) {
+  const char* fn = "qf_moe_dispatch";
+  QF_TRY(check_moe(fn, T, E, k));
+  if (!offsets) return fail(QF_EINVAL, "%s: null offsets", fn);
+  QF_TRY(check_out("qf_moe_dispatch: offsets", offsets));
+  if (T > 0 && (!ids || !row_of || !slot_of)) return fail(QF_EINVAL, "%s: null ids, row_of or slot_of", fn);
+  QF_TRY(check_out("qf_moe_dispatch: ids", ids));
+  QF_TRY(check_out("qf_moe_dispatch: row_of", row_of));
+  QF_TRY(check_out("qf_moe_dispatch: slot_of", slot_of));
+  if ((X == nullptr) != (Xg == nullptr) && T > 0) return fail(QF_EINVAL, "%s: X and Xg go together", fn);
+  if (X) {
+    QF_TRY(check_mat("qf_moe_dispatch: X", X, T, H, ldx, true));
+    QF_TRY(check_mat("qf_moe_dispatch: Xg", Xg, T * k, H, H, true));
+  }
+  if (T > 0) QF_TRY(check_ws(fn, qf::moe_sort_ws_bytes(T * k, E), ws, ws_bytes));
+  QF_TRY(dev(qf::launch_moe_sort(ids, T, (int)E, (int)k, offsets, row_of, slot_of, X, H, ldx, Xg,
+                                 static_cast<int32_t*>(ws), S(stream)), fn));
+  return ok();
+}
+
+qf_status qf_moe_dispatch_bwd(const int32_t* row_of, int64_t T, int64_t k, int64_t H,
+                              const uint16_t* dXg, uint16_t* dX, int64_t lddx, qf_stream_t stream) {
+  const char* fn = "qf_moe_dispatch_bwd";
+  QF_TRY(check_rows(fn, T, k, H, row_of));
+  QF_TRY(check_mat("qf_moe_dispatch_bwd: dXg", dXg, T * k, H, H, true));
+  QF_TRY(check_mat("qf_moe_dispatch_bwd: dX", dX, T, H, lddx, true));
+  if (T == 0 || H == 0) return ok();
+  QF_TRY(dev(qf::launch_moe_combine(row_of, nullptr, T, (int)k, H, dXg, dX, lddx, S(stream)), fn));
+  return ok();
+}
+
+qf_status qf_moe_combine(const int32_t* row_of, const float* w, int64_t T, int64_t k, int64_t H,
+                         const uint16_t* Yg, uint16_t* Y, int64_t ldy, qf_stream_t stream) {
+  const char* fn = "qf_moe_combine";
+  QF_TRY(check_rows(fn, T, k, H, row_of));
+  QF_TRY(check_out("qf_moe_combine: w", w));
+  QF_TRY(check_mat("qf_moe_combine: Yg", Yg, T * k, H, H, true));
+  QF_TRY(check_mat("qf_moe_combine: Y", Y, T, H, ldy, true));
+  if (T == 0 || H == 0) return ok();
+  QF_TRY(dev(qf::launch_moe_combine(row_of, w, T, (int)k, H, Yg, Y, ldy, S(stream)), fn));
+  return ok();
+}
+
+qf_status qf_moe_combine_bwd(const int32_t* row_of, const float* w, int64_t T, int64_t k, int64_t H,
+                             const uint16_t* dY, int64_t lddy, const uint16_t* Yg, uint16_t* dYg,
+                             float* dw, qf_stream_t stream) {
+  const char* fn = "qf_moe_combine_bwd";
+  QF_TRY(check_rows(fn, T, k, H, row_of));
+  QF_TRY(check_out("qf_moe_combine_bwd: w", w));
+  QF_TRY(check_out("qf_moe_combine_bwd: dw", dw));
+  QF_TRY(check_mat("qf_moe_combine_bwd: dY", dY, T, H, lddy, true));
+  QF_TRY(check_mat("qf_moe_combine_bwd: Yg", Yg, T * k, H, H, dw != nullptr));
+  QF_TRY(check_mat("qf_moe_combine_bwd: dYg", dYg, T * k, H, H, false));
+  if (T == 0 || (!dYg && !dw)) return ok();
+  QF_TRY(dev(qf::launch_moe_combine_bwd(row_of, w, T, (int)k, H, dY, lddy, Yg, dYg, dw, S(stream)), fn));
+  return ok();
+}
+
+// ---------------------------------------------------------- few rows times packed weights
+namespace {
+
+qf_status check_packed(const char* fn, const qf_packed* w) {
+  if (!w) return fail(QF_EINVAL, "%s: null weight", fn);
+  if (w->E < 0 || w->N < 0 || w->K < 0) return fail(QF_ESHAPE, "%s: negative shape", fn);
+  if (w->fmt != QF_FMT_NVFP4 && w->fmt != QF_FMT_MXFP4 && w->fmt != QF_FMT_Q4K)
+    return fail(QF_EINVAL, "%s: bad format %d", fn, w->fmt);
+  if (w->K % block_of(w->fmt)) return fail(QF_ESHAPE, "%s: K=%lld is not a multiple of the block size %lld",
+                                           fn, (long long)w->K, (long long)block_of(w->fmt));
+  if (w->K > INT32_MAX / 2 || w->N > INT32_MAX / 2) return fail(QF_ENOTSUP, "%s: N or K of 2^30 or more", fn);
+  return QF_OK;
+}
+
+// The operand's pointers, and X [M, K] and Y [R, N] (which the caller has found not empty).
+qf_status check_packed_call(const char* fn, const qf_packed* w, int64_t R, int64_t M, const uint16_t* X,
+                            int64_t ldx, const void* Y, int64_t ldy, int y_f32) {
+  if (y_f32 != 0 && y_f32 != 1) return fail(QF_EINVAL, "%s: y_f32 must be 0/1", fn);
+  QF_TRY(check_mat(fn, X, M, w->K, ldx, true));
+  QF_TRY(check_mat(fn, Y, R, w->N, ldy, true));
+  if (w->K > 0 && (!w->codes || (w->fmt != QF_FMT_Q4K && !w->scales)))
+    return fail(QF_EINVAL, "%s: null packed operand", fn);
+  if (w->fmt == QF_FMT_NVFP4 && !w->S) return fail(QF_EINVAL, "%s: NVFP4 needs its tensor scales S", fn);
+  QF_TRY(check_out(fn, w->codes));
+  QF_TRY(check_out(fn, w->scales));
+  return QF_OK;
+}
+
+qf::PackedOperand packed_op(const qf_packed* w) {
+  return {w->codes, w->scales, w->S, w->E, w->N, w->K, w->fmt};
+}
+
+}  // namespace
+
+qf_status qf_packed_matvec(const qf_packed* w, int64_t M, const uint16_t* X, int64_t ldx, void* Y,
+                           int64_t ldy, int y_f32, qf_stream_t stream) {
+  const char* fn = "qf_packed_matvec";
+  QF_TRY(check_packed(fn, w));
+  if (w->E != 1) return fail(QF_ESHAPE, "%s: %lld weights, not one", fn, (long long)w->E);
+  if (M < 0) return fail(QF_ESHAPE, "%s: negative shape", fn);
+  if (M > 64) return fail(QF_ENOTSUP, "%s: more than 64 rows (qf_gemm_packed_b takes them)", fn);
+  if (M == 0 || w->N == 0) return ok();
+  QF_TRY(check_packed_call(fn, w, M, M, X, ldx, Y, ldy, y_f32));
+  QF_TRY(dev(qf::launch_packed_matvec(packed_op(w), nullptr, M, nullptr, 1, M, X, ldx, Y, ldy, y_f32, S(stream)), fn));
+  return ok();
+}
+
+qf_status qf_packed_matvec_grouped(const qf_packed* w, const int64_t* group_offsets, int64_t R,
+                                   const int32_t* rows, int64_t rows_div, int64_t M,
+                                   const uint16_t* X, int64_t ldx, void* Y, int64_t ldy, int y_f32,
+                                   qf_stream_t stream) {
+  const char* fn = "qf_packed_matvec_grouped";
+  QF_TRY(check_packed(fn, w));
+  if (R < 0 || M < 0) return fail(QF_ESHAPE, "%s: negative shape", fn);
+  if (w->E > 1024) return fail(QF_ENOTSUP, "%s: more than 1024 experts", fn);
+  if (R > INT32_MAX / 2 || M > INT32_MAX / 2) return fail(QF_ENOTSUP, "%s: 2^30 rows or more", fn);
+  if (rows_div < 1 || rows_div > INT32_MAX) return fail(QF_EINVAL, "%s: rows_div must be 1 or more", fn);
+  if (w->E == 0 || R == 0 || w->N == 0) return ok();
+  if (!group_offsets) return fail(QF_EINVAL, "%s: null group_offsets", fn);
+  QF_TRY(check_packed_call(fn, w, R, M, X, ldx, Y, ldy, y_f32));
+  QF_TRY(dev(qf::launch_packed_matvec(packed_op(w), group_offsets, R, rows, rows_div, M, X, ldx, Y,
+                                      ldy, y_f32, S(stream)), fn));
   return ok();
 }
 

@@ -209,6 +209,41 @@ hipError_t launch_lora_colsum(const uint16_t* Big, int64_t M, int64_t C, int64_t
 hipError_t launch_transpose_f32(const float* F, int64_t N, int64_t r, int64_t batch, float* Ft,
                                 hipStream_t s);
 
+// ---- around the grouped layer (qf_moe.hip) ----------------------------------------------------
+// Router: the k largest of E logits a token (z bf16 or FP32 [T, E], row stride ldz) and their
+// weights; its gradient (T and k > 0, k <= min(E, 64), E <= 1024).
+hipError_t launch_moe_route(const void* z, int z_f32, int64_t T, int E, int64_t ldz, int k, int score,
+                            int norm, float scale, const uint8_t* mask, int32_t* ids, float* w,
+                            hipStream_t s);
+hipError_t launch_moe_route_bwd(const void* z, int z_f32, int64_t T, int E, int64_t ldz, int k,
+                                int score, int norm, float scale, const int32_t* ids,
+                                const float* dw, void* dz, int64_t lddz, hipStream_t s);
+// Stable sort of T k slots by expert (ws: moe_sort_ws_bytes) and, with X, the rows in that order.
+size_t moe_sort_ws_bytes(int64_t n, int64_t E);
+hipError_t launch_moe_sort(const int32_t* ids, int64_t T, int E, int k, int64_t* offsets,
+                           int32_t* row_of, int32_t* slot_of, const uint16_t* X, int64_t H,
+                           int64_t ldx, uint16_t* Xg, int32_t* ws, hipStream_t s);
+// Y[t] = sum over j of w[t, j] (or 1) Yg[row_of[t, j]], and its gradients (H a multiple of 8).
+hipError_t launch_moe_combine(const int32_t* row_of, const float* w, int64_t T, int k, int64_t H,
+                              const uint16_t* Yg, uint16_t* Y, int64_t ldy, hipStream_t s);
+hipError_t launch_moe_combine_bwd(const int32_t* row_of, const float* w, int64_t T, int k, int64_t H,
+                                  const uint16_t* dY, int64_t lddy, const uint16_t* Yg,
+                                  uint16_t* dYg, float* dw, hipStream_t s);
+
+// ---- few rows times packed weights (qf_matvec.hip) ---------------------------------------------
+// off null: dense, R = M rows (at most 64) against weight 0.  Else rows [off[e], off[e+1]) of Y (R
+// rows) against weight e; row r reads X row r, or rows[r] / rows_div.
+struct PackedOperand {
+  const uint8_t* codes;
+  const uint8_t* scales;
+  const float* S;
+  int64_t E, N, K;
+  int fmt;
+};
+hipError_t launch_packed_matvec(const PackedOperand& w, const int64_t* off, int64_t R,
+                                const int32_t* rows, int64_t rows_div, int64_t M, const uint16_t* X,
+                                int64_t ldx, void* Y, int64_t ldy, int y_f32, hipStream_t s);
+
 // ---- QAD distillation loss (qf_kl.hip) ---------------------------------------------------------
 // Per row of bf16 logits [L, V] (V % 8 == 0): row_kl[t], optional loss (mean), grad
 // (gscale (p_S - p_T), bf16) and agree (top-1 equality).

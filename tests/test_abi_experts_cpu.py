@@ -1,0 +1,116 @@
+"""Host-only checks of the router, sort, sum and packed-product entry points: each call here fails
+validation (or has nothing to do), so nothing is launched."""
+import ctypes
+import os
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+LIB = os.path.join(ROOT, "paper_2609_39223_amd", "libqf.so")
+QF_OK, QF_EINVAL, QF_ESHAPE, QF_EALIGN, QF_ENOTSUP = 0, 1, 2, 3, 4
+I, P, F = ctypes.c_int64, ctypes.c_void_p, ctypes.c_float
+A, B, C, D = P(256), P(512), P(768), P(1024)
+
+
+class Packed(ctypes.Structure):
+    _fields_ = [("E", ctypes.c_int64), ("N", ctypes.c_int64), ("K", ctypes.c_int64),
+                ("fmt", ctypes.c_int32), ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("S", ctypes.c_void_p)]
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not os.path.exists(LIB):
+        pytest.skip("libqf.so not built (run __graft_entry__.build())")
+    import torch  # noqa: F401  (same HIP runtime as the GPU path)
+    lib = ctypes.CDLL(LIB)
+    lib.qf_last_error.restype = ctypes.c_char_p
+    return lib
+
+
+def test_route(L):
+    def fwd(z=A, f32=0, T=4, E=16, ld=16, k=2, score=0, norm=1, ids=B, w=C):
+        return L.qf_moe_route(z, f32, I(T), I(E), I(ld), I(k), score, norm, F(1), None, ids, w, None)
+    assert fwd(T=0) == QF_OK
+    assert fwd(T=-1) == QF_ESHAPE and fwd(E=-1) == QF_ESHAPE
+    assert fwd(k=0) == QF_ESHAPE and fwd(k=17) == QF_ESHAPE
+    assert b"17 choices among 16" in L.qf_last_error()
+    assert fwd(E=1025, ld=1032) == QF_ENOTSUP and fwd(E=128, ld=128, k=65) == QF_ENOTSUP
+    assert fwd(T=1 << 30) == QF_ENOTSUP                           # 2^31 slots
+    assert fwd(score=2) == QF_EINVAL and fwd(f32=3) == QF_EINVAL and fwd(norm=-1) == QF_EINVAL
+    assert fwd(z=None) == QF_EINVAL and fwd(ids=None) == QF_EINVAL and fwd(w=None) == QF_EINVAL
+    assert fwd(ld=8) == QF_ESHAPE and fwd(ld=20) == QF_EALIGN
+    assert fwd(z=P(264)) == QF_EALIGN and fwd(ids=P(260)) == QF_EALIGN and fwd(w=P(260)) == QF_EALIGN
+
+    def bwd(T=4, k=2, ids=B, dw=C, dz=D, lddz=16, score=1):
+        return L.qf_moe_route_bwd(A, 0, I(T), I(16), I(16), I(k), score, 0, F(1), ids, dw, dz, I(lddz), None)
+    assert bwd(T=0) == QF_OK
+    assert bwd(ids=None) == QF_EINVAL and bwd(dw=None) == QF_EINVAL and bwd(dz=None) == QF_EINVAL
+    assert bwd(lddz=8) == QF_ESHAPE and bwd(lddz=18) == QF_EALIGN and bwd(dz=P(8)) == QF_EALIGN
+    assert bwd(score=-1) == QF_EINVAL and bwd(k=40) == QF_ESHAPE
+
+
+def test_dispatch(L):
+    n = ctypes.c_size_t()
+    assert L.qf_moe_dispatch_workspace_size(I(100), I(16), I(4), ctypes.byref(n)) == QF_OK and n.value > 0
+    assert L.qf_moe_dispatch_workspace_size(I(100), I(16), I(4), None) == QF_EINVAL
+    assert L.qf_moe_dispatch_workspace_size(I(100), I(16), I(20), ctypes.byref(n)) == QF_ESHAPE
+
+    def call(ids=A, off=B, row=C, slot=D, X=A, H=64, ldx=64, Xg=B, ws=P(4096), nws=1 << 20, k=4):
+        return L.qf_moe_dispatch(ids, I(100), I(16), I(k), off, row, slot, X, I(H), I(ldx), Xg, ws,
+                                 ctypes.c_size_t(nws), None)
+    assert call(ids=None) == QF_EINVAL and call(off=None) == QF_EINVAL
+    assert call(row=None) == QF_EINVAL and call(slot=None) == QF_EINVAL
+    assert call(X=None) == QF_EINVAL and call(Xg=None) == QF_EINVAL
+    assert b"go together" in L.qf_last_error()
+    assert call(nws=8) == QF_EINVAL and b"workspace" in L.qf_last_error()
+    assert call(ws=None) == QF_EINVAL and call(ws=P(4100)) == QF_EALIGN
+    assert call(H=60, ldx=64) == QF_EALIGN                        # dense rows of 60 elements
+    assert call(ldx=56) == QF_ESHAPE and call(H=-8) == QF_ESHAPE
+    assert call(off=P(264)) == QF_EALIGN and call(row=P(4)) == QF_EALIGN and call(slot=P(4)) == QF_EALIGN
+    assert call(k=0) == QF_ESHAPE
+
+
+def test_sum(L):
+    def fwd(row=A, w=B, T=4, k=2, H=64, Yg=C, Y=D, ldy=64):
+        return L.qf_moe_combine(row, w, I(T), I(k), I(H), Yg, Y, I(ldy), None)
+    assert fwd(T=0) == QF_OK and fwd(H=0) == QF_OK
+    assert fwd(row=None) == QF_EINVAL and fwd(Yg=None) == QF_EINVAL and fwd(Y=None) == QF_EINVAL
+    assert fwd(k=0) == QF_ESHAPE and fwd(k=65) == QF_ENOTSUP and fwd(T=-2) == QF_ESHAPE
+    assert fwd(H=12) == QF_EALIGN and fwd(ldy=56) == QF_ESHAPE and fwd(w=P(8)) == QF_EALIGN
+    d = L.qf_moe_dispatch_bwd
+    assert d(A, I(4), I(2), I(64), None, B, I(64), None) == QF_EINVAL
+    assert d(A, I(4), I(2), I(64), B, C, I(60), None) == QF_ESHAPE
+
+    def bwd(dY=A, Yg=B, dYg=C, dw=D, lddy=64, H=64):
+        return L.qf_moe_combine_bwd(A, None, I(4), I(2), I(H), dY, I(lddy), Yg, dYg, dw, None)
+    assert bwd(dYg=None, dw=None) == QF_OK                        # nothing asked for
+    assert bwd(Yg=None) == QF_EINVAL                              # dw needs it
+    assert bwd(dY=None) == QF_EINVAL and bwd(lddy=68) == QF_EALIGN and bwd(dw=P(8)) == QF_EALIGN
+    assert bwd(dYg=P(8)) == QF_EALIGN and bwd(H=4) == QF_EALIGN
+
+
+def test_packed_products(L):
+    def dense(fmt=1, E=1, N=32, K=64, M=2, X=A, ldx=64, Y=B, ldy=32, f32=0, codes=C, scales=D, S=A):
+        w = Packed(E, N, K, fmt, codes, scales, S)
+        return L.qf_packed_matvec(ctypes.byref(w), I(M), X, I(ldx), Y, I(ldy), f32, None)
+    assert L.qf_packed_matvec(None, I(1), A, I(64), B, I(32), 0, None) == QF_EINVAL
+    assert dense(M=0) == QF_OK and dense(N=0) == QF_OK
+    assert dense(M=65) == QF_ENOTSUP and b"qf_gemm_packed_b" in L.qf_last_error()
+    assert dense(M=-1) == QF_ESHAPE and dense(E=2) == QF_ESHAPE and dense(N=-1) == QF_ESHAPE
+    assert dense(fmt=0) == QF_EINVAL and dense(fmt=4) == QF_EINVAL and dense(f32=2) == QF_EINVAL
+    assert dense(K=40) == QF_ESHAPE and dense(fmt=2, K=48) == QF_ESHAPE and dense(fmt=3, K=128) == QF_ESHAPE
+    assert dense(codes=None) == QF_EINVAL and dense(scales=None) == QF_EINVAL and dense(S=None) == QF_EINVAL
+    assert dense(X=None) == QF_EINVAL and dense(Y=None) == QF_EINVAL
+    assert dense(ldx=56) == QF_ESHAPE and dense(ldy=24) == QF_ESHAPE and dense(ldy=36) == QF_EALIGN
+    assert dense(codes=P(8)) == QF_EALIGN and dense(scales=P(8)) == QF_EALIGN and dense(X=P(8)) == QF_EALIGN
+    assert dense(K=1 << 31, ldx=1 << 31) == QF_ENOTSUP
+
+    def grouped(off=A, R=6, rows=None, div=1, M=6, E=3, fmt=2, K=64, X=B, Y=C):
+        w = Packed(E, 32, K, fmt, A, B, None)
+        return L.qf_packed_matvec_grouped(ctypes.byref(w), off, I(R), rows, I(div), I(M), X, I(64), Y, I(32), 0, None)
+    assert grouped(R=0) == QF_OK and grouped(E=0) == QF_OK
+    assert grouped(off=None) == QF_EINVAL and grouped(div=0) == QF_EINVAL and grouped(X=None) == QF_EINVAL
+    assert grouped(E=1025) == QF_ENOTSUP and grouped(R=-1) == QF_ESHAPE and grouped(M=-1) == QF_ESHAPE
+    assert grouped(fmt=1) == QF_EINVAL                            # no tensor scales
+    assert grouped(R=1 << 30) == QF_ENOTSUP

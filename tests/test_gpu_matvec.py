@@ -1,0 +1,301 @@
+"""GPU parity of the products of few rows with packed weights, dense and per expert, against the
+FP64 decode of the same codes.
+
+Bound: a sum of K exact products of bf16 values in binary32, in chains of at most 32 terms (one
+MFMA) + K / 128 steps of one wave x 4 + 8 waves, each addition rounding a partial sum no larger than
+sum |x| |w|: D u sum |x| |w| with D = 32 + K / 32 + 8 and u = 2^-23 (the matrix cores' additions
+need not round to nearest); two more roundings for the block and tensor scales.  Q4_K sums
+(16 + q) x and x: |w| there counts as |d s6| (16 + q) + |dmin m6 + 16 d s6|.  A bf16 result adds
+2^-8 relative, FP32 2^-24."""
+import numpy as np
+import pytest
+
+import workloads
+from oracle import experts as ox
+from tests.helpers import bf16_to_f64, from_dev, to_dev
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+BLOCK = {"nvfp4": 16, "mxfp4": 32, "q4k": 256}
+
+
+@pytest.fixture(scope="module")
+def qf():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2609_39223_amd as qf
+    qf.lib()
+    return qf
+
+
+def _codes(rng, fmt, R, K, E=1):
+    """Arbitrary codes under arbitrary scales of a realistic range."""
+    if fmt == "q4k":
+        c = rng.integers(0, 256, (R, K // 256, 144)).astype(np.uint8)
+        half = (rng.random((R, K // 256, 2)) * 0.01).astype(np.float16)
+        c[..., :4] = half.view(np.uint8).reshape(R, K // 256, 4)
+        return c, None, None
+    codes = rng.integers(0, 256, (R, K // 2)).astype(np.uint8)
+    if fmt == "nvfp4":
+        return codes, rng.integers(0, 0x7F, (R, K // 16)).astype(np.uint8), (rng.random(E) * 1e-3 + 1e-5).astype(np.float32)
+    return codes, rng.integers(100, 130, (R, K // 32)).astype(np.uint8), None
+
+
+def _magnitude(fmt, codes, W):
+    if fmt != "q4k":
+        return np.abs(W)
+    zero_q = codes.copy()
+    zero_q[..., 16:] = 0
+    off = np.abs(ox.decode(fmt, zero_q))                          # dmin m6
+    one_q = zero_q.copy()
+    one_q[..., 16:] = 0x11
+    step = np.abs(ox.decode(fmt, one_q) + off)                    # d s6
+    return np.abs(W) + off + 16 * step + off + 16 * step
+
+
+def _bound(x, W, mag, K, f32):
+    ref = x @ W.T
+    return ref, ((32 + K / 32 + 8) * 2.0 ** -23 + 2.0 ** -22) * (np.abs(x) @ mag.T) + (2.0 ** -24 if f32 else 2.0 ** -8) * np.abs(ref)
+
+
+def _weight(qf, fmt, N, K, codes, scales, S, E=None):
+    return qf.packed_weight(fmt, N, K, to_dev(codes), None if scales is None else to_dev(scales),
+                            None if S is None else to_dev(S), E=E)
+
+
+def _out(R, N, f32, pad=8):
+    cols = (N + 7) // 8 * 8 + pad
+    return torch.full((R, cols), 7.0, dtype=torch.float32 if f32 else torch.bfloat16, device="cuda")
+
+
+SHAPES = [(1, 1, 256), (1, 16, 512), (1, 4096, 256), (2, 37, 768), (5, 1000, 1024), (16, 129, 2304), (17, 64, 768),
+          (33, 40, 1024), (64, 257, 4096), (3, 24, 256 * 9), (1, 9000, 256), (40, 17000, 256)]
+FP4_SHAPES = [(1, 8, 32), (3, 20, 96), (7, 33, 160), (16, 50, 1056), (50, 9, 4000)]
+ODD_SHAPES = [(1, 8, 16), (2, 17, 48), (9, 33, 272), (33, 20, 1040 + 16), (64, 40, 4080)]
+
+
+@pytest.mark.parametrize("fmt,M,N,K", [(f, *s) for f in ("nvfp4", "mxfp4", "q4k") for s in SHAPES]
+                         + [(f, *s) for f in ("nvfp4", "mxfp4") for s in FP4_SHAPES]
+                         + [("nvfp4", *s) for s in ODD_SHAPES])
+@pytest.mark.parametrize("f32", [False, True])
+def test_dense(qf, fmt, M, N, K, f32):
+    rng = np.random.default_rng(M * N + K)
+    codes, scales, S = _codes(rng, fmt, N, K)
+    xh = workloads.normal_bf16(rng, (M, K))
+    wide = np.full((M, (K + 7) // 8 * 8 + 16), 0x7FC0, np.uint16)
+    wide[:, :K] = xh
+    full = _out(M, N, f32)
+    weight = _weight(qf, fmt, N, K, codes, scales, S)
+    qf.packed_matvec(weight, to_dev(wide)[:, :K], full[:, :N])
+    W = ox.decode(fmt, codes, scales, None if S is None else S[0])
+    ref, bound = _bound(bf16_to_f64(xh), W, _magnitude(fmt, codes, W), K, f32)
+    got = full[:, :N].double().cpu().numpy()
+    assert np.all(np.abs(got - ref) <= bound), float((np.abs(got - ref) / bound).max())
+    assert bool((full[:, N:] == 7).all())
+    again = _out(M, N, f32)
+    qf.packed_matvec(weight, to_dev(wide)[:, :K], again[:, :N])
+    assert torch.equal(full, again)
+
+
+@pytest.mark.parametrize("fmt", ["nvfp4", "mxfp4", "q4k"])
+def test_codes_of_the_quantizers(qf, fmt):
+    """A weight quantized by the library, one token: near the layer's product on W_hat."""
+    rng = np.random.default_rng(4)
+    N, K = 96, 512
+    W, x = to_dev(workloads.normal_bf16(rng, (N, K), 0.02)), workloads.normal_bf16(rng, (1, K))
+    hat = torch.empty(N, K, dtype=torch.int16, device="cuda")
+    if fmt == "q4k":
+        codes, scales, S = torch.empty(N, K // 256, 144, dtype=torch.uint8, device="cuda"), None, None
+        qf.fakequant_q4k(W, codes, hat)
+    else:
+        codes = torch.empty(N, K // 2, dtype=torch.uint8, device="cuda")
+        scales, S = torch.empty(N, K // BLOCK[fmt], dtype=torch.uint8, device="cuda"), None
+        if fmt == "nvfp4":
+            S = torch.empty(1, device="cuda")
+            qf.fakequant_nvfp4(W, torch.empty(1, device="cuda"), qf.AMAX_COMPUTE, S, codes, scales, hat)
+        else:
+            qf.fakequant_mxfp4(W, codes, scales, hat)
+    Y = torch.empty(1, N, device="cuda")
+    qf.packed_matvec(qf.packed_weight(fmt, N, K, codes, scales, S), to_dev(x), Y)
+    Wh, xf = bf16_to_f64(from_dev(hat)), bf16_to_f64(x)
+    assert np.all(np.abs(from_dev(Y) - xf @ Wh.T) <= (2.0 ** -8 * 1.01 + 1e-4) * (np.abs(xf) @ np.abs(Wh).T))
+
+
+def test_non_finite(qf):
+    rng = np.random.default_rng(6)
+    N, K = 40, 512
+    for fmt, bad in (("nvfp4", 0x7F), ("mxfp4", 0xFF)):
+        codes, scales, S = _codes(rng, fmt, N, K)
+        scales[5, 3] = bad
+        x = workloads.normal_bf16(rng, (2, K))
+        Y = torch.empty(2, N, device="cuda")
+        qf.packed_matvec(_weight(qf, fmt, N, K, codes, scales, S), to_dev(x), Y)
+        nan = torch.isnan(Y)
+        assert bool(nan[:, 5].all()) and int(nan.sum()) == 2
+        x[0, 100] = 0x7F80                                         # an infinite activation: its row alone
+        codes, scales, S = _codes(rng, fmt, N, K)
+        codes[:, 50] |= 0x11                                       # (under weights that are not zero)
+        scales[:, 100 // BLOCK[fmt]] = np.maximum(scales[:, 100 // BLOCK[fmt]], 1)
+        qf.packed_matvec(_weight(qf, fmt, N, K, codes, scales, S), to_dev(x), Y)
+        assert not bool(torch.isfinite(Y[0]).any()) and bool(torch.isfinite(Y[1]).all())
+
+
+def test_no_rows_no_columns_no_depth(qf):
+    rng = np.random.default_rng(7)
+    codes, scales, S = _codes(rng, "nvfp4", 16, 64)
+    qf.packed_matvec(_weight(qf, "nvfp4", 16, 64, codes, scales, S), torch.empty(0, 64, dtype=torch.bfloat16, device="cuda"),
+                     torch.empty(0, 16, device="cuda"))
+    z = torch.empty(0, dtype=torch.uint8, device="cuda")
+    Y = torch.full((3, 16), 7.0, device="cuda")
+    qf.packed_matvec(qf.packed_weight("mxfp4", 16, 0, z, z), torch.empty(3, 0, dtype=torch.bfloat16, device="cuda"), Y)
+    assert bool((Y == 0).all())
+
+
+def _grouped(rng, counts):
+    off = np.zeros(len(counts) + 1, np.int64)
+    off[1:] = np.cumsum(counts)
+    return off
+
+
+@pytest.mark.parametrize("fmt,N,K,counts", [
+    ("nvfp4", 64, 256, [1]), ("nvfp4", 40, 272, [0, 3, 0, 17, 1, 0]), ("mxfp4", 33, 96, [5, 0, 70, 1]),
+    ("q4k", 24, 512, [2, 0, 33, 16]), ("nvfp4", 16, 128, [0] * 129 + [4]), ("mxfp4", 16, 64, [1] * 300),
+    ("nvfp4", 272, 512, [20] * 5), ("q4k", 48, 256, [40, 9, 0, 64, 65]), ("mxfp4", 17, 32, [0, 0, 0])])
+@pytest.mark.parametrize("f32", [False, True])
+def test_grouped(qf, fmt, N, K, counts, f32):
+    rng = np.random.default_rng(N + K + len(counts))
+    E, off = len(counts), _grouped(rng, counts)
+    R, live = int(off[-1]) + 3, int(off[-1])                       # three rows of no expert
+    codes, scales, S = _codes(rng, fmt, E * N, K, E)
+    div, M = 3, 29
+    rows = rng.integers(0, M * div, R).astype(np.int32)
+    rows[live:] = -1
+    if live > 2:
+        rows[1], rows[2] = -1, M * div + 5                         # X rows that do not exist
+    xh = workloads.normal_bf16(rng, (M, K))
+    full = _out(R, N, f32)
+    weight = _weight(qf, fmt, N, K, codes, scales, S, E=E)
+    qf.packed_matvec_grouped(weight, to_dev(off), to_dev(xh), full[:, :N], rows=to_dev(rows), rows_div=div)
+    x = np.zeros((R, K))
+    ok = (rows >= 0) & (rows < M * div)
+    x[ok] = bf16_to_f64(xh)[rows[ok] // div]
+    got = full[:, :N].double().cpu().numpy()
+    for e in range(E):
+        a, b = off[e], off[e + 1]
+        if a == b:
+            continue
+        part = slice(e * N, (e + 1) * N)
+        W = ox.decode(fmt, codes[part], None if scales is None else scales[part], None if S is None else S[e])
+        ref, bound = _bound(x[a:b], W, _magnitude(fmt, codes[part], W), K, f32)
+        assert np.all(np.abs(got[a:b] - ref) <= bound), e
+    assert bool((full[live:] == 7).all()) and bool((full[:, N:] == 7).all())
+    # rows in expert order already
+    if live:
+        xg = np.zeros((R, K), np.uint16)
+        xg[ok] = xh[rows[ok] // div]
+        same = _out(R, N, f32)
+        qf.packed_matvec_grouped(weight, to_dev(off), to_dev(xg), same[:, :N])
+        assert torch.equal(full, same)
+
+
+def test_grouped_offsets_out_of_range_and_no_x(qf):
+    """Offsets that leave 0 .. R are cut to it; no X rows at all: zeros."""
+    rng = np.random.default_rng(3)
+    codes, scales, S = _codes(rng, "mxfp4", 32, 64)
+    weight = _weight(qf, "mxfp4", 16, 64, codes, scales, S, E=2)
+    x = workloads.normal_bf16(rng, (6, 64))
+    Y = _out(6, 16, True)
+    qf.packed_matvec_grouped(weight, torch.tensor([-4, 3, 900], device="cuda"), to_dev(x), Y[:, :16])
+    W = ox.decode("mxfp4", codes, scales)
+    ref = np.concatenate([bf16_to_f64(x)[:3] @ W[:16].T, bf16_to_f64(x)[3:] @ W[16:].T])
+    assert np.allclose(from_dev(Y[:, :16]), ref, rtol=1e-4, atol=1e-4 * np.abs(ref).max())
+    qf.packed_matvec_grouped(weight, torch.tensor([0, 3, 6], device="cuda"), torch.empty(0, 64, dtype=torch.bfloat16, device="cuda"),
+                             Y[:, :16])
+    assert bool((Y[:, :16] == 0).all())
+
+
+def test_weights_past_32_bits_of_bytes(qf):
+    """Experts whose codes start past 2^32 bytes (5 GB of NVFP4 codes)."""
+    E, N, K = 320, 4096, 8192
+    g = torch.Generator(device="cuda").manual_seed(1)
+    codes = torch.randint(0, 256, (N, K // 2), generator=g, device="cuda", dtype=torch.uint8).repeat(E, 1)
+    scales = torch.randint(40, 80, (E * N, K // 16), generator=g, device="cuda", dtype=torch.uint8)
+    S = torch.rand(E, generator=g, device="cuda") + 0.5
+    off = torch.zeros(E + 1, dtype=torch.int64, device="cuda")
+    off[E - 1:] = 1
+    off[E] = 3
+    x = torch.randn(3, K, generator=g, device="cuda").to(torch.bfloat16)
+    Y = torch.empty(3, N, device="cuda")
+    qf.packed_matvec_grouped(qf.packed_weight("nvfp4", N, K, codes, scales, S, E=E), off, x, Y)
+    pick = [0, 1, 77, N - 1]
+    for r, e in ((0, E - 2), (1, E - 1), (2, E - 1)):
+        W = ox.decode("nvfp4", from_dev(codes[[e * N + p for p in pick]]), from_dev(scales[[e * N + p for p in pick]]), float(S[e]))
+        ref, bound = _bound(x[r:r + 1].double().cpu().numpy(), W, np.abs(W), K, True)
+        assert np.all(np.abs(from_dev(Y[r:r + 1, pick]) - ref) <= bound)
+
+
+def test_in_a_graph_and_on_a_side_stream(qf):
+    rng = np.random.default_rng(12)
+    E, N, K, R = 6, 80, 512, 24
+    codes, scales, S = _codes(rng, "nvfp4", E * N, K, E)
+    weight = _weight(qf, "nvfp4", N, K, codes, scales, S, E=E)
+    off = torch.empty(E + 1, dtype=torch.int64, device="cuda")
+    X = torch.empty(R, K, dtype=torch.bfloat16, device="cuda")
+    Y = torch.empty(R, N, dtype=torch.bfloat16, device="cuda")
+
+    def load(seed):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        X.copy_(torch.randn(R, K, generator=g, device="cuda"))
+        off.copy_(torch.cat([torch.zeros(1), torch.randint(0, R + 1, (E - 1,), generator=g, device="cuda").cpu().sort().values,
+                             torch.full((1,), R)]).long())
+
+    load(0)
+    qf.packed_matvec_grouped(weight, off, X, Y)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        qf.packed_matvec_grouped(weight, off, X, Y)
+    for seed in (1, 2, 3, 1):
+        load(seed)
+        qf.packed_matvec_grouped(weight, off, X, Y)
+        torch.cuda.synchronize()
+        want = Y.clone()
+        Y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(Y, want), seed
+        Y.zero_()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            qf.packed_matvec_grouped(weight, off, X, Y)
+        torch.cuda.current_stream().wait_stream(side)
+        torch.cuda.synchronize()
+        assert torch.equal(Y, want), seed
+
+
+def test_refusals(qf):
+    rng = np.random.default_rng(2)
+    codes, scales, S = _codes(rng, "nvfp4", 16, 64)
+    weight = _weight(qf, "nvfp4", 16, 64, codes, scales, S)
+    X, Y = torch.zeros(65, 64, dtype=torch.bfloat16, device="cuda"), torch.full((65, 16), 7.0, device="cuda")
+    with pytest.raises(qf.QFError, match="QF_ENOTSUP"):
+        qf.packed_matvec(weight, X, Y)
+    with pytest.raises(qf.QFError, match="tensor scales"):
+        qf.packed_matvec(qf.packed_weight("nvfp4", 16, 64, to_dev(codes), to_dev(scales)), X[:1], Y[:1])
+    with pytest.raises(qf.QFError, match="QF_EALIGN"):
+        qf.packed_matvec(qf.packed_weight("mxfp4", 4, 32, to_dev(codes).view(-1)[8:], to_dev(scales)), X[:1, :32], Y[:1, :4])
+    with pytest.raises(qf.QFError, match="QF_ESHAPE"):
+        qf.packed_matvec(qf.packed_weight("q4k", 16, 64, to_dev(codes)), X[:1], Y[:1])
+    with pytest.raises(ValueError):
+        qf.packed_weight("nvfp4", 17, 64, to_dev(codes), to_dev(scales), to_dev(S))
+    with pytest.raises(ValueError):
+        qf.packed_matvec(weight, X[:1, :32], Y[:1])
+    with pytest.raises(ValueError):
+        qf.packed_matvec_grouped(weight, torch.zeros(3, dtype=torch.int64, device="cuda"), X, Y)
+    with pytest.raises(qf.QFError, match="QF_EINVAL"):
+        qf.packed_matvec_grouped(weight, torch.zeros(2, dtype=torch.int64, device="cuda"), X, Y, rows_div=0)
+    torch.cuda.synchronize()
+    assert bool((Y == 7).all())

@@ -1,0 +1,367 @@
+"""GPU parity of the router, the sort by expert, the weighted sum back and their gradients (Sec. 3.3
+"Mixture-of-experts adaptation") against the FP64 reference.
+
+Bounds, with u = 2^-24 (a binary32 rounding) and 2^-8 (bf16 has 8 significant bits):
+  router weights  exp(a - m) errs by the rounding of a (|a| u: the logarithm of the sigmoid) and of
+                  a - m (|a - m| u) in its argument and a few u of its own, the sum of up to 1024
+                  such terms by as much again and its at most 30 additions (16 a lane, then a
+                  tree): a relative error of at most 2 (max |a| + max |a - m|) u + 64 u.
+  router gradient the same of every product in q_e (g_e - sum q g), so that bound times
+                  q_e (|g_e| + 2 sum |q g|); then the result's rounding.
+  weighted sum    k fused multiply-adds: k u sum |w y|; then bf16.
+  dw              a chain of at most H / 256 + 16 additions: (H / 256 + 16) u sum |dY Yg|.
+Ids, orders, offsets, copies and dYg (one product rounded once, through binary32) are whole or exact
+to one rounding."""
+import math
+
+import numpy as np
+import pytest
+
+import workloads
+from oracle import experts as ox
+from tests.helpers import bf16_to_f64, empty_bf16, from_dev, to_dev
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def qf():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2609_39223_amd as qf
+    qf.lib()
+    return qf
+
+
+def _logits(rng, T, E, dtype):
+    """Rows with ties, -inf, all -inf, the types' lowest values and wide ranges."""
+    z = rng.normal(size=(T, E)) * 2
+    z[0::5] = np.round(z[0::5])                                    # ties
+    z[1::5, E // 2:] = -np.inf                                     # a masked half
+    if T > 2:
+        z[2] = -np.inf                                             # no expert at all
+    z[3::7] *= 40
+    z[4::9, 0] = -3.3895313892515355e38                            # bf16's lowest
+    z[6::11] = np.where(rng.random(E) < 0.5, 0.0, -0.0)
+    h = workloads.to_bf16(z.astype(np.float32))
+    return (h, bf16_to_f64(h)) if dtype == "bf16" else (z.astype(np.float32), z.astype(np.float32).astype(np.float64))
+
+
+def _padded(a, pad, fill):
+    """a on the GPU as columns of a wider tensor (row stride a multiple of 8) filled with `fill`."""
+    cols = (a.shape[1] + 7) // 8 * 8 + pad
+    wide = np.full((a.shape[0], cols), fill, a.dtype)
+    wide[:, :a.shape[1]] = a
+    return to_dev(wide)[:, :a.shape[1]]
+
+
+def _route_err(z, ids, score):
+    """The relative bound of a row's weights (see the module's text)."""
+    out = np.zeros(z.shape[0])
+    for t in range(z.shape[0]):
+        row = z[t][z[t] > -np.inf]
+        if row.size:
+            a = [row.max(), row.min()] if score == "softmax" else [ox._log_sigmoid(v) for v in (row.max(), row.min())]
+            # experts further down than 200 below the best weigh nothing in binary32
+            low = max(a[1], a[0] - 200.0)
+            out[t] = (2 * (max(abs(a[0]), abs(low)) + a[0] - low) + 64) * U
+    return out[:, None]
+
+
+CASES = [(1, 8, 2), (37, 128, 8), (64, 129, 8), (33, 60, 4), (19, 1, 1), (23, 5, 5), (9, 1024, 8), (17, 512, 33),
+         (9, 1000, 64), (40, 128, 16), (40, 128, 17), (260, 16, 1)]
+
+
+@pytest.mark.parametrize("T,E,k", CASES)
+@pytest.mark.parametrize("score,norm", [("softmax", True), ("softmax", False), ("sigmoid", True), ("sigmoid", False)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_route_and_gradient(qf, T, E, k, score, norm, dtype):
+    rng = np.random.default_rng(T * E + k)
+    raw, z = _logits(rng, T, E, dtype)
+    mask = (rng.random(T) < 0.8).astype(np.uint8) if T > 3 else None
+    dw = rng.normal(size=(T, k)).astype(np.float32)
+    nan = 0x7FC0 if dtype == "bf16" else np.nan
+    zd = _padded(raw, 8 * (T % 3), nan)
+    ids = torch.full((T, k), 77, dtype=torch.int32, device="cuda")
+    w = torch.full((T, k), 77.0, device="cuda")
+    md = None if mask is None else to_dev(mask)
+    qf.moe_route(zd, ids, w, score=score, norm=norm, scale=1.5, mask=md)
+    rid, rw = ox.route(z, k, score, norm, 1.5, mask)
+    assert np.array_equal(from_dev(ids), rid)
+    err = _route_err(z, rid, score)
+    assert np.all(np.abs(from_dev(w) - rw) <= err * rw + 1e-37)
+
+    dz = _padded(np.full((T, E), nan, raw.dtype), 8 * (T % 3), nan)
+    qf.moe_route_bwd(zd, ids, to_dev(dw), dz, score=score, norm=norm, scale=1.5)
+    got = from_dev(dz)
+    got = bf16_to_f64(got) if dtype == "bf16" else got.astype(np.float64)
+    ref = ox.route_bwd(z, rid, dw, score, norm, 1.5)
+    bound = np.zeros((T, E))
+    for t in range(T):
+        c = [int(e) for e in rid[t] if e >= 0]
+        if not c:
+            continue
+        q = np.array(ox.scores([float(v) for v in z[t]], c, score, norm))
+        g = 1.5 * np.abs(dw[t, :len(c)].astype(np.float64))
+        if score == "softmax" and not norm:
+            full, gf = np.exp(z[t] - z[t].max()), np.zeros(E)
+            full /= full.sum()
+            gf[c] = g
+            bound[t] = full * (gf + 2 * (q * g).sum())
+        else:
+            bound[t, c] = q * (g + 2 * (q * g).sum())
+    out = 2.0 ** -8 if dtype == "bf16" else U
+    assert np.all(np.abs(got - ref) <= 2 * err * bound + out * np.abs(ref) + 1e-37)
+    # what lies past E in a row is left alone
+    if (E + 7) // 8 * 8 != E:
+        tail = dz.as_strided((T, 1), (dz.stride(0), 1), dz.storage_offset() + E)
+        assert torch.equal(tail.isnan() if dtype != "bf16" else tail == 0x7FC0, torch.ones_like(tail, dtype=torch.bool))
+
+
+def test_route_non_finite_logits(qf):
+    z = torch.zeros(4, 16, device="cuda")
+    z[0, 5], z[0, 2] = math.nan, math.inf
+    z[1, 3] = math.inf
+    z[2, 7] = -math.nan
+    z[3, 0:15] = -math.inf
+    for norm in (True, False):
+        ids = torch.empty(4, 3, dtype=torch.int32, device="cuda")
+        w = torch.empty(4, 3, device="cuda")
+        qf.moe_route(z, ids, w, norm=norm)
+        assert from_dev(ids).tolist() == [[5, 2, 0], [3, 0, 1], [7, 0, 1], [15, -1, -1]]
+        a = from_dev(w)
+        assert np.isnan(a[0]).all() and np.isnan(a[1, 0]) and np.isnan(a[2]).all()
+        assert a[3].tolist() == [1.0, 0.0, 0.0]
+        qf.moe_route(z, ids, w, score="sigmoid", norm=norm)
+        assert from_dev(ids)[0].tolist() == [5, 2, 0] and np.isnan(from_dev(w)[0, 0])
+
+
+def test_route_sigmoid_where_every_score_underflows(qf):
+    z = torch.full((2, 8), -300.0, device="cuda")
+    z[1] = -3.0e38
+    ids, w = torch.empty(2, 4, dtype=torch.int32, device="cuda"), torch.empty(2, 4, device="cuda")
+    qf.moe_route(z, ids, w, score="sigmoid")
+    assert np.allclose(from_dev(w), 0.25, rtol=1e-6)
+    dz = torch.empty_like(z)
+    qf.moe_route_bwd(z, ids, torch.ones(2, 4, device="cuda"), dz, score="sigmoid")
+    assert torch.isfinite(dz).all() and float(dz.abs().max()) <= 1e-6
+
+
+def test_route_many_tokens_match_torch(qf):
+    T, E, k = 5000, 128, 8
+    g = torch.Generator(device="cuda").manual_seed(3)
+    z = torch.randn(T, E, generator=g, device="cuda").to(torch.bfloat16)
+    ids, w = torch.empty(T, k, dtype=torch.int32, device="cuda"), torch.empty(T, k, device="cuda")
+    qf.moe_route(z, ids, w)
+    v, i = z.double().sort(dim=1, descending=True, stable=True)
+    assert torch.equal(ids.long(), i[:, :k])
+    assert float((w.double() - torch.softmax(v[:, :k], 1)).abs().max()) < 1e-6
+
+
+def _ids(rng, T, E, k, drop):
+    ids = np.stack([rng.permutation(E)[:k] for _ in range(T)]).astype(np.int32) if T else np.zeros((0, k), np.int32)
+    ids[rng.random((T, k)) < drop] = -1
+    if T > 2 and drop:
+        ids[1] = -1
+        ids[2, 0] = E                                              # past the experts: dropped too
+    return ids
+
+
+def _sorted(qf, ids, E, X=None):
+    T, k = ids.shape
+    off = torch.full((E + 1,), -5, dtype=torch.int64, device="cuda")
+    row_of = torch.full((T, k), -99, dtype=torch.int32, device="cuda")
+    slot_of = torch.full((T * k,), -99, dtype=torch.int32, device="cuda")
+    ws = qf.moe_dispatch_workspace(T, E, k)
+    Xg = None if X is None else torch.full((T * k, X.shape[1]), 0x7FC0, dtype=torch.int16, device="cuda")
+    qf.moe_dispatch(to_dev(ids), off, row_of, slot_of, ws, X=X, Xg=Xg)
+    return off, row_of, slot_of, Xg
+
+
+@pytest.mark.parametrize("T,E,k,H,drop", [
+    (0, 8, 2, 64, 0.0), (1, 8, 2, 8, 0.0), (1, 1, 1, 520, 0.0), (5, 4, 4, 1000, 0.3), (16, 128, 8, 256, 0.0),
+    (300, 60, 4, 512, 0.2), (700, 1024, 8, 64, 0.1), (1777, 32, 4, 72, 0.1), (40, 16, 2, 64, 1.0),
+    (9000, 3, 1, 16, 0.0), (700, 200, 64, 8, 0.05)])
+def test_sort_and_copy(qf, T, E, k, H, drop):
+    rng = np.random.default_rng(T + E)
+    ids = _ids(rng, T, E, k, drop)
+    x = workloads.normal_bf16(rng, (T, H)) if T else np.zeros((0, H), np.uint16)
+    off, row_of, slot_of, Xg = _sorted(qf, ids, E, _padded(x, 16, 0x7FC0))
+    roff, rrow, rslot = ox.dispatch(ids, E)
+    assert np.array_equal(from_dev(off), roff)
+    assert np.array_equal(from_dev(row_of), rrow)
+    assert np.array_equal(from_dev(slot_of), rslot)
+    assert np.array_equal(from_dev(Xg), ox.gather(rslot, x, k))
+    off2, row2, slot2, _ = _sorted(qf, ids, E)                     # the plan alone
+    assert torch.equal(off, off2) and torch.equal(row_of, row2) and torch.equal(slot_of, slot2)
+
+
+def test_sort_of_many_slots(qf):
+    """More slots than 256 chunks of 2048, one expert taking most of them."""
+    T, E, k = 300000, 130, 2
+    g = torch.Generator(device="cuda").manual_seed(5)
+    ids = torch.randint(-1, E, (T, k), generator=g, device="cuda", dtype=torch.int32)
+    ids[T // 3:, 0] = 7
+    off, row_of, slot_of, _ = _sorted(qf, from_dev(ids), E)
+    key = torch.where(ids < 0, E, ids).reshape(-1).long()
+    order = key.argsort(stable=True)
+    count = torch.bincount(key, minlength=E + 1)
+    assert torch.equal(off[1:], count[:E].cumsum(0)) and int(off[0]) == 0
+    live = int(off[E])
+    assert torch.equal(slot_of[:live].long(), order[:live]) and bool((slot_of[live:] == -1).all())
+    row = torch.empty_like(order)
+    row[order] = torch.arange(T * k, device="cuda")
+    assert torch.equal(row_of.reshape(-1).long(), torch.where(key < E, row, -1 - row))
+
+
+@pytest.mark.parametrize("T,E,k,H,drop", [
+    (1, 8, 1, 8, 0.0), (1, 8, 8, 520, 0.0), (33, 16, 2, 1000, 0.2), (64, 60, 4, 4096, 0.1), (50, 64, 6, 504, 0.3),
+    (20, 128, 8, 1536, 0.0), (12, 128, 20, 2056, 0.2), (7, 64, 64, 64, 0.5)])
+@pytest.mark.parametrize("weighted", [True, False])
+def test_sum_and_gradients(qf, T, E, k, H, drop, weighted):
+    rng = np.random.default_rng(T + k + H)
+    ids = _ids(rng, T, E, k, drop)
+    _, rrow, rslot = ox.dispatch(ids, E)
+    yg, dy = workloads.normal_bf16(rng, (T * k, H)), workloads.normal_bf16(rng, (T, H))
+    yg[rslot < 0] = 0x7FC0                                         # what a dropped slot's row holds is not used
+    w = rng.normal(size=(T, k)).astype(np.float32)
+    w_nan = np.where(rrow < 0, np.float32(np.nan), w)              # nor its weight
+    wd = to_dev(w_nan) if weighted else None
+    row_of = to_dev(rrow)
+    Y = _padded(np.full((T, H), 0x7FC0, np.uint16), 8, 0x7FC0)
+    qf.moe_combine(row_of, to_dev(yg), Y, w=wd)
+    yf, df, wf = bf16_to_f64(np.where((rslot < 0)[:, None], 0, yg)), bf16_to_f64(dy), w if weighted else None
+    ref = ox.combine(rrow, yf, wf)
+    mag = ox.combine(rrow, np.abs(yf), None if wf is None else np.abs(wf))
+    assert np.all(np.abs(bf16_to_f64(from_dev(Y)) - ref) <= 2.0 ** -8 * np.abs(ref) + 2 * k * U * mag)
+    if not weighted:                                               # the copy's gradient is the same sum
+        dX = empty_bf16((T, H))
+        qf.moe_dispatch_bwd(row_of, to_dev(yg), dX)
+        assert torch.equal(dX, Y)
+
+    dYg = torch.full((T * k, H), 0x7FC0, dtype=torch.int16, device="cuda")
+    dw = torch.full((T, k), 77.0, device="cuda")
+    dyd, ygd = _padded(dy, 8, 0x7FC0), to_dev(yg)
+    qf.moe_combine_bwd(row_of, dyd, dYg, Yg=ygd, w=wd, dw=dw)
+    rdyg, rdw = ox.combine_bwd(rrow, df, yf, wf)
+    _, mdw = ox.combine_bwd(rrow, np.abs(df), np.abs(yf), wf)
+    got = bf16_to_f64(from_dev(dYg))
+    assert np.all(np.abs(got - rdyg) <= 2.0 ** -8 * 1.001 * np.abs(rdyg))
+    assert not got[rslot < 0].any()
+    assert np.all(np.abs(from_dev(dw) - rdw) <= (H / 256 + 16) * U * mdw)
+    # each gradient alone
+    one = torch.full_like(dYg, 0x7FC0)
+    qf.moe_combine_bwd(row_of, dyd, one, w=wd)
+    assert torch.equal(one, dYg)
+    two = torch.full_like(dw, 77.0)
+    qf.moe_combine_bwd(row_of, dyd, None, Yg=ygd, w=wd, dw=two)
+    assert torch.equal(two, dw)
+
+
+def test_rows_past_32_bits_of_bytes(qf):
+    """Expert rows whose byte offsets pass 2^32: T k = 70000 rows of 32768 columns (4.6 GB)."""
+    T, E, k, H = 35000, 4, 2, 32768
+    g = torch.Generator(device="cuda").manual_seed(2)
+    ids = torch.stack([torch.randperm(E, generator=g, device="cuda")[:k] for _ in range(64)]).to(torch.int32)
+    ids = ids.repeat(T // 64 + 1, 1)[:T].contiguous()
+    X = torch.randint(-30000, 30000, (T, H), generator=g, device="cuda", dtype=torch.int16)
+    off, row_of, slot_of, Xg = _sorted(qf, from_dev(ids), E, X)
+    probe = torch.tensor([0, 1, 65535, 65536, 65537, 69000, 69999], device="cuda")
+    assert int(off[E]) == T * k
+    assert torch.equal(Xg[probe], X[slot_of[probe].long() // k])
+    Xg &= 0x3FFF                                                   # finite positive bf16
+    dX = torch.empty(T, H, dtype=torch.int16, device="cuda")
+    qf.moe_dispatch_bwd(row_of, Xg, dX)
+    t = torch.tensor([0, 17, T // 2, T - 2, T - 1], device="cuda")
+    rows = Xg[row_of[t].long()].view(torch.bfloat16).double()
+    want = rows.sum(1)
+    got = dX[t].view(torch.bfloat16).double()
+    assert bool(((got - want).abs() <= want * 2.0 ** -8 * 1.001 + 1e-38).all())
+
+
+def test_router_to_sum_in_a_graph_and_on_a_side_stream(qf):
+    """The five calls of an expert layer's surroundings, captured once and replayed on new inputs,
+    every replay equal to eager calls, and eager calls on a side stream equal to those on the
+    current one."""
+    T, E, k, H = 96, 16, 4, 512
+    z = torch.empty(T, E, dtype=torch.bfloat16, device="cuda")
+    X, dY = (torch.empty(T, H, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    ids, row_of = (torch.empty(T, k, dtype=torch.int32, device="cuda") for _ in range(2))
+    w, dw = (torch.empty(T, k, device="cuda") for _ in range(2))
+    off = torch.empty(E + 1, dtype=torch.int64, device="cuda")
+    slot_of = torch.empty(T * k, dtype=torch.int32, device="cuda")
+    Xg, dYg = (torch.empty(T * k, H, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    Y, dX = (torch.empty(T, H, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    dz, ws = torch.empty_like(z), qf.moe_dispatch_workspace(T, E, k)
+    outs = (ids, w, off, row_of, slot_of, Xg, Y, dYg, dw, dz, dX)
+
+    def calls():
+        qf.moe_route(z, ids, w)
+        qf.moe_dispatch(ids, off, row_of, slot_of, ws, X=X, Xg=Xg)
+        qf.moe_combine(row_of, Xg, Y, w=w)
+        qf.moe_combine_bwd(row_of, dY, dYg, Yg=Xg, w=w, dw=dw)
+        qf.moe_route_bwd(z, ids, dw, dz)
+        qf.moe_dispatch_bwd(row_of, dYg, dX)
+
+    def load(seed):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        for t in (z, X, dY):
+            t.copy_(torch.randn(t.shape, generator=g, device="cuda"))
+
+    load(0)
+    calls()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for seed in (1, 2, 3, 1):
+        load(seed)
+        calls()
+        torch.cuda.synchronize()
+        want = [t.clone() for t in outs]
+        for replay in (True, False):
+            for t in outs:
+                t.zero_()
+            torch.cuda.synchronize()
+            if replay:
+                graph.replay()
+            else:
+                side = torch.cuda.Stream()
+                side.wait_stream(torch.cuda.current_stream())
+                with torch.cuda.stream(side):
+                    calls()
+                torch.cuda.current_stream().wait_stream(side)
+            torch.cuda.synchronize()
+            for a, b in zip(outs, want):
+                assert torch.equal(a, b), (seed, replay)
+
+
+def test_refusals_leave_outputs_alone(qf):
+    z = torch.zeros(4, 16, device="cuda")
+    ids, w = torch.full((4, 2), 5, dtype=torch.int32, device="cuda"), torch.zeros(4, 2, device="cuda")
+    with pytest.raises(qf.QFError, match="QF_ESHAPE"):
+        qf.moe_route(z, torch.full((4, 17), 5, dtype=torch.int32, device="cuda"), torch.zeros(4, 17, device="cuda"))
+    with pytest.raises(qf.QFError, match="QF_EALIGN"):
+        qf.moe_route(torch.zeros(4, 20, device="cuda")[:, :16], ids, w)
+    with pytest.raises(TypeError):
+        qf.moe_route(z, ids.long(), w)
+    with pytest.raises(TypeError):
+        qf.moe_route(z, ids, w, mask=torch.ones(4, device="cuda"))
+    with pytest.raises(ValueError):
+        qf.moe_route(z, ids, w[:2])
+    off, slot = torch.empty(17, dtype=torch.int64, device="cuda"), torch.empty(8, dtype=torch.int32, device="cuda")
+    ws = qf.moe_dispatch_workspace(4, 16, 2)
+    with pytest.raises(qf.QFError, match="go together"):
+        qf.moe_dispatch(ids, off, ids.clone(), slot, ws, X=empty_bf16((4, 8)))
+    with pytest.raises(qf.QFError, match="QF_EALIGN"):
+        qf.moe_dispatch(ids, off, ids.clone(), slot, ws, X=empty_bf16((4, 16))[:, :12], Xg=empty_bf16((8, 12)))
+    with pytest.raises(ValueError):
+        qf.moe_combine(ids, empty_bf16((7, 8)), empty_bf16((4, 8)))
+    with pytest.raises(TypeError):
+        qf.moe_combine(ids, empty_bf16((8, 8)), empty_bf16((4, 8)), w=w.double())
+    torch.cuda.synchronize()
+    assert bool((ids == 5).all())
