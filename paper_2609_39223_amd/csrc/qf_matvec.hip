@@ -1,18 +1,28 @@
 // Products of few rows with packed weights (QATFactory Sec. 3.4, 3.5: the weights an engine serves),
 // dense or per expert: Y = X W^T with W decoded in registers on its way to the matrix cores.
 //
-// A workgroup takes 16 NT weight rows against up to 16 MT rows of X; its waves split K by steps and
-// add their FP32 partial sums in LDS in wave order.  On v_mfma_f32_16x16x32_bf16 X is the A operand
-// (lane: row lane % 16, k 8 (lane / 16) + 0..7) and W the B operand (lane: weight row lane % 16, the
-// same k); any bijection of k is fine as long as both sides use it, so a lane takes 32 consecutive
-// codes of its weight row (16 bytes) per step of 128 and feeds them to four MFMAs.
+// A workgroup takes 16 NT weight rows against up to 16 rows of X, its waves take slices of 512 k in
+// turn, and their FP32 partial sums meet in LDS in wave order.  A slice's codes and X rows go straight
+// from memory to LDS, each wave into a region of its own, so nothing but the final sum waits for
+// another wave, and no registers are held while the copies are under way: up to 32 waves a compute
+// unit wait for 4 to 5 KB of codes each.  Copies are contiguous (256 bytes of four rows per
+// instruction) where loads in the shape of the matrix operand, 16 bytes of 16 rows, kept the L1's
+// address port busy four times as long (24576 x 4096 NVFP4 times one row: 18.2 us with such loads,
+// 14.3 with copies).  A 16-byte chunk c of row r lies at c ^ r of its row in LDS, so the operand
+// reads, the same chunk of 16 rows, fall on different banks.
+//
+// On v_mfma_f32_16x16x32_bf16 X is the A operand (lane: row lane % 16, k 8 (lane / 16) + 0..7) and W
+// the B operand (lane: weight row lane % 16, the same k); any bijection of k is fine as long as both
+// sides use it: lane group g = lane / 16 takes k 128 g .. 128 g + 127 of a slice, so the scales of a
+// lane's codes are consecutive bytes too (8 or 4, loaded into registers).
 //   NVFP4  V s is exact in bf16 (E2M1 has 2 significant bits, E4M3 4; 2^-10 <= |V s| <= 2688), so the
 //          block scale goes into the operand and the tensor scale S onto the finished sum.
 //   MXFP4  V 2^p is exact in bf16.
-//   Q4_K   a sub-block is one MFMA deep: P = sum (16 + q) x and X1 = sum x, 16 + q being exact in
-//          bf16 and formed from a code by a shift and a mask; the sub-block adds
-//          (d s6) P - (dmin m6 + 16 d s6) X1.
-// Bound by reading the weight once: 0.53 to 0.56 bytes an element.
+//   Q4_K   a sub-block of 32 is one MFMA deep.  16 + q is exact in bf16 and made from a code by a shift
+//          and a mask; with X1 = -16 sum x from one MFMA as the next one's addend, P = sum (16 + q) x
+//          + X1 = sum q x, and a super-block adds d sum s6 P + (dmin / 16) sum m6 X1.
+// Bound by reading the weight once: 0.53 to 0.56 bytes an element (NVFP4, 24576 x 4096, one row: 56.7
+// MB in 14.3 us = 4.0 TB/s).  Small weights are bound by the launch and one trip to memory (4096 x 4096: 5.0 us).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -21,6 +31,9 @@
 #include "qf.h"
 #include "qf_codecs.h"
 #include "qf_internal.h"
+
+#define QF_LDS(p) ((__attribute__((address_space(3))) void*)(p))
+#define QF_GLOBAL(p) ((__attribute__((address_space(1))) void*)(p))
 
 namespace qf {
 namespace {
@@ -33,6 +46,24 @@ __device__ __forceinline__ f32x4_t mfma16(uint4 a, uint4 b, f32x4_t c) {
                                                  __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
 }
 
+// Copies from memory to LDS: lane l's 16 (4) bytes at g go to l + 16 (4) lane.  The non-temporal form
+// leaves the caches to others.
+__device__ __forceinline__ void copy16(const void* g, void* l) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_global_load_lds(QF_GLOBAL(const_cast<void*>(g)), QF_LDS(l), 16, 0, 0);
+#endif
+}
+__device__ __forceinline__ void copy16_nt(const void* g, void* l) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_global_load_lds(QF_GLOBAL(const_cast<void*>(g)), QF_LDS(l), 16, 0, 2);
+#endif
+}
+__device__ __forceinline__ void copy4(const void* g, void* l) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_global_load_lds(QF_GLOBAL(const_cast<void*>(g)), QF_LDS(l), 4, 0, 0);
+#endif
+}
+
 struct MatvecArgs {
   PackedOperand w;
   const uint16_t* X;
@@ -43,22 +74,35 @@ struct MatvecArgs {
   const int64_t* off;     // null: dense
   const int32_t* rows;
   int rows_div;
+  int xmax;               // rows of X a workgroup takes at most (1 .. 16)
+  int waves;              // waves that share a tile's slices
+  int items;              // row groups the grid holds
 };
 
-// Work item `item` of a grouped call: expert e and rows [r0, r1) of at most `chunk`, items counted
-// over the experts in order.  Every wave finds it by itself: lane l sums the chunks of its E / 64
-// experts, a prefix sum over the lanes finds whose they are.  False past the last item.
+// The X row of row r of Y, -1 if there is none.
+__device__ __forceinline__ int64_t x_row(const MatvecArgs& p, int64_t r) {
+  int64_t x = r;
+  if (p.rows) x = p.rows[r] < 0 ? -1 : p.rows[r] / p.rows_div;
+  return x < p.M ? x : -1;
+}
+
+// Work item `item` of a grouped call: expert e and its rows [r0, r1), at most `chunk`; items count
+// the experts' chunks in order.  Every wave finds it by itself: lane l sums the chunks of its experts
+// (offsets cut to 0 .. R < 2^30), a prefix sum over the lanes finds whose the item is.  False past
+// the last one.
 __device__ __forceinline__ bool find_item(const int64_t* off, int E, int64_t R, int item, int chunk,
                                           int& e, int64_t& r0, int64_t& r1) {
   const int lane = threadIdx.x & 63, per = (E + 63) / 64, e0 = lane * per;
-  int sum = 0;
-  int64_t a = e0 <= E ? min(max(off[e0 <= E ? e0 : E], (int64_t)0), R) : 0;
-  const int64_t first = a;
-  for (int i = 0; i < per; ++i) {
-    if (e0 + i >= E) break;
-    const int64_t b = min(max(off[e0 + i + 1], (int64_t)0), R);
-    if (b > a) sum += (int)((b - a + chunk - 1) / chunk);
-    a = b;
+  auto at = [&](int i) { return (int)min(max(off[i < E ? i : E], (int64_t)0), R); };
+  auto chunks = [&](int a, int b) { return b > a ? (b - a + chunk - 1) / chunk : 0; };
+  int sum = 0, o0 = 0, o1 = 0, o2 = 0;
+  if (per <= 2) {                                 // the usual case: three loads at once
+    o0 = at(e0);
+    o1 = at(e0 + 1);
+    o2 = at(e0 + per);
+    sum = chunks(o0, o1) + chunks(o1, o2);
+  } else {
+    for (int i = 0; i < per; ++i) sum += chunks(at(e0 + i), at(e0 + i + 1));
   }
   int inc = sum;
 #pragma unroll
@@ -66,80 +110,80 @@ __device__ __forceinline__ bool find_item(const int64_t* off, int E, int64_t R, 
     const int o = __shfl_up(inc, d, 64);
     if (lane >= d) inc += o;
   }
-  if (item >= __shfl(inc, 63, 64)) return false;
-  const uint64_t past = __ballot(inc > item);
-  const int owner = __ffsll((unsigned long long)past) - 1;
-  int left = item - (inc - sum), found = 0;         // meaningful in the owner
-  int64_t lo = 0, hi = 0;
-  a = first;
-  for (int i = 0; i < per; ++i) {
-    if (e0 + i >= E) break;
-    const int64_t b = min(max(off[e0 + i + 1], (int64_t)0), R);
-    const int n = b > a ? (int)((b - a + chunk - 1) / chunk) : 0;
-    if (left >= 0 && left < n) {
-      found = e0 + i;
-      lo = a + (int64_t)left * chunk;
-      hi = min(lo + chunk, b);
+  if (item >= __builtin_amdgcn_readlane(inc, 63)) return false;
+  const int owner = __ffsll((unsigned long long)__ballot(inc > item)) - 1;
+  int left = item - (inc - sum), i = 0;           // meaningful in the owner
+  if (per <= 2) {
+    if (left >= chunks(o0, o1)) {
+      left -= chunks(o0, o1);
+      i = 1;
+      o0 = o1;
+      o1 = o2;
     }
-    left -= n;
-    a = b;
+  } else {
+    for (; i < per; ++i) {
+      o0 = at(e0 + i);
+      o1 = at(e0 + i + 1);
+      if (left < chunks(o0, o1)) break;
+      left -= chunks(o0, o1);
+    }
   }
-  e = __builtin_amdgcn_readfirstlane(__shfl(found, owner, 64));
-  const int l = __shfl((int)lo, owner, 64), h = __shfl((int)hi, owner, 64);   // R < 2^30
-  r0 = __builtin_amdgcn_readfirstlane(l);
-  r1 = __builtin_amdgcn_readfirstlane(h);
+  const int lo = o0 + left * chunk;
+  e = __builtin_amdgcn_readlane(e0 + i, owner);
+  r0 = __builtin_amdgcn_readlane(lo, owner);
+  r1 = __builtin_amdgcn_readlane(min(lo + chunk, o1), owner);
   return true;
 }
 
-// ---- FP4 formats: a step is 128 deep ----------------------------------------------------------
-// A lane's 32 codes and their scale bytes (NVFP4: two, MXFP4: one) for each of its NT weight rows,
-// and the four A operands for each of the MT row blocks.
-template <int MT, int NT>
-struct Stage {
-  uint4 c[NT];
-  uint32_t s[NT];
-  uint4 x[MT][4];
-};
+// ------------------------------------------------------------------------------- the formats
+template <int FMT>
+constexpr int kCodeBytes = FMT == QF_FMT_Q4K ? 5120 : 4096;   // LDS of 16 rows x 512 codes
 
-// ODD: K = 16 modulo 32 (NVFP4): code rows 8-byte aligned, scale rows with an odd pitch.
-template <int FMT, int MT, int NT, bool ODD>
-__device__ __forceinline__ void load_stage(Stage<MT, NT>& st, const uint8_t* const cp[NT],
-                                           const uint8_t* const sp[NT], const uint16_t* const xp[MT],
-                                           int k, int kend) {
-  const bool in = k < kend, half = !ODD || k + 16 < kend;   // (kend: past every k in the full steps)
+// Copies of 16 code rows (row i at base + min(i, last) pitch) of slice sl into l, in whole 64-lane
+// instructions; lanes with nothing to fetch fetch something that exists.  FP4: 16 rows of 256 bytes,
+// chunks exchanged as above; rows 8-byte aligned (K = 16 modulo 32) go in words.  Q4_K: two
+// super-blocks a row as they lie (16 rows of 288 bytes: rows 8 banks apart); `half`: only one is left.
+enum Copy { kCopy = 0, kCopyNt = 1, kCopyWords = 2 };
+template <int FMT, int COPY>
+__device__ __forceinline__ void copy_codes(const uint8_t* base, int64_t pitch, int last, int sl,
+                                           bool half, char* l) {
+  const int lane = threadIdx.x & 63;
+  if (FMT == QF_FMT_Q4K) {
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    st.c[t] = make_uint4(0, 0, 0, 0);
-    st.s[t] = 0;
-    if (!in) continue;
-    const uint8_t* const c = cp[t] + k / 2;
-    if (ODD) {
-      const uint2 a = *reinterpret_cast<const uint2*>(c);
-      st.c[t].x = a.x;
-      st.c[t].y = a.y;
-      st.s[t] = sp[t][k / 16];
-      if (half) {
-        const uint2 b = *reinterpret_cast<const uint2*>(c + 8);
-        st.c[t].z = b.x;
-        st.c[t].w = b.y;
-        st.s[t] |= (uint32_t)sp[t][k / 16 + 1] << 8;
-      }
-    } else {
-      st.c[t] = *reinterpret_cast<const uint4*>(c);
-      if (FMT == QF_FMT_NVFP4) st.s[t] = *reinterpret_cast<const uint16_t*>(sp[t] + k / 16);
-      else st.s[t] = sp[t][k / 32];
+    for (int j = 0; j < 5; ++j) {
+      const int i = j * 64 + lane, row = i / 18 < 15 ? i / 18 : 15, c = half ? i % 18 % 9 : i % 18;
+      const uint8_t* const g = base + (row < last ? row : last) * pitch + (int64_t)sl * 288 + 16 * c;
+      if (COPY == kCopyNt) copy16_nt(g, l + j * 1024);
+      else copy16(g, l + j * 1024);
+    }
+  } else if (COPY == kCopyWords) {
+#pragma unroll 4
+    for (int row = 0; row < 16; ++row)
+      copy4(base + (row < last ? row : last) * pitch + (int64_t)sl * 256 + 16 * ((lane >> 2) ^ row) + 4 * (lane & 3),
+            l + row * 256);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int row = 4 * j + (lane >> 4);
+      const uint8_t* const g = base + (row < last ? row : last) * pitch + (int64_t)sl * 256 + 16 * ((lane & 15) ^ row);
+      if (COPY == kCopyNt) copy16_nt(g, l + j * 1024);
+      else copy16(g, l + j * 1024);
     }
   }
-#pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      st.x[m][i] = make_uint4(0, 0, 0, 0);
-      if (in && (i < 2 || half)) st.x[m][i] = *reinterpret_cast<const uint4*>(xp[m] + k + 8 * i);
-    }
 }
 
-// The B operand of 8 codes: V s (NVFP4, s FP32) or V 2^p (MXFP4, s the E8M0 code).
+// The scale bytes of this lane's 128 codes in slice sl (NVFP4 8, MXFP4 4), at any address.
+struct Bytes8 { uint8_t b[8]; };
+struct Bytes4 { uint8_t b[4]; };
+template <int FMT>
+__device__ __forceinline__ uint2 load_scales(const uint8_t* sp, int sl) {
+  if (FMT == QF_FMT_NVFP4) return __builtin_bit_cast(uint2, *reinterpret_cast<const Bytes8*>(sp + (int64_t)sl * 32));
+  if (FMT == QF_FMT_MXFP4)
+    return make_uint2(__builtin_bit_cast(uint32_t, *reinterpret_cast<const Bytes4*>(sp + (int64_t)sl * 16)), 0u);
+  return make_uint2(0u, 0u);
+}
+
+// The B operand of 8 codes: V s (NVFP4, s FP32) or V 2^p (MXFP4, e the E8M0 code).
 __device__ __forceinline__ uint4 decode_nvfp4(uint32_t cw, float s) {
   uint32_t w[4];
   codec::nvfp4_decode8_finite(cw, s, w);     // exact: nothing is rounded (a NaN scale stays NaN)
@@ -151,203 +195,214 @@ __device__ __forceinline__ uint4 decode_mxfp4(uint32_t cw, uint32_t e) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-template <int FMT, int MT, int NT>
-__device__ __forceinline__ void multiply_stage(const Stage<MT, NT>& st, f32x4_t acc[MT][NT]) {
+// 32 codes under their scale bytes s (NVFP4: two, MXFP4: one; low bytes).
+template <int FMT>
+__device__ __forceinline__ void multiply32(const uint4& c, uint32_t s, const uint4 x[4], f32x4_t& acc) {
+  const uint32_t cw[4] = {c.x, c.y, c.z, c.w};
+  const auto sf = __builtin_amdgcn_cvt_pk_f32_fp8((int)s, false);
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const uint32_t cw[4] = {st.c[t].x, st.c[t].y, st.c[t].z, st.c[t].w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint4 b;
-      if (FMT == QF_FMT_NVFP4) {
-        const auto s = __builtin_amdgcn_cvt_pk_f32_fp8((int)st.s[t], false);
-        b = decode_nvfp4(cw[i], i < 2 ? s[0] : s[1]);
-      } else {
-        b = decode_mxfp4(cw[i], st.s[t]);
-      }
-#pragma unroll
-      for (int m = 0; m < MT; ++m) acc[m][t] = mfma16(st.x[m][i], b, acc[m][t]);
-    }
+  for (int i = 0; i < 4; ++i) {
+    const uint4 b = FMT == QF_FMT_NVFP4 ? decode_nvfp4(cw[i], i < 2 ? sf[0] : sf[1]) : decode_mxfp4(cw[i], s & 0xFFu);
+    acc = mfma16(x[i], b, acc);
   }
 }
 
-// ---- Q4_K: a step is one super-block of 256 ------------------------------------------------------
-// Two bf16 values 16 + q of the codes at bits 4 (..) of bytes P and P + 2 of w.
+// Two bf16 values 16 + q of the codes in the low (HIGH: high) nibbles of bytes P and P + 2 of w.
 template <int P, bool HIGH>
 __device__ __forceinline__ uint32_t q4k_pair(uint32_t w) {
   constexpr int at = 8 * P + (HIGH ? 4 : 0);
-  const uint32_t v = at < 3 ? w << (3 - at) : w >> (at - 3);
+  uint32_t v;
+  if constexpr (at < 3) v = w << (3 - at);
+  else v = w >> (at - 3);
   return (v & 0x00780078u) | 0x41804180u;
 }
 
-template <int MT, int NT>
-__device__ __forceinline__ void q4k_step(const uint8_t* const cp[NT], const uint16_t* const xp[MT],
-                                         int sb, int g, f32x4_t acc[MT][NT]) {
-  uint4 head[NT];
-  uint2 c[NT][4];
-  uint4 x[MT][8];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const uint8_t* const p = cp[t] + (int64_t)sb * 144;
-    head[t] = *reinterpret_cast<const uint4*>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c[t][i] = *reinterpret_cast<const uint2*>(p + 16 + 32 * i + 8 * g);
-  }
-#pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      x[m][j] = *reinterpret_cast<const uint4*>(xp[m] + sb * 256 + 32 * j + 8 * g);
-  const uint4 ones = make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
+// One super-block of this lane's weight row (144 bytes at `row`) against the X row at xl (chunks of 8
+// exchanged by xw, the super-block's first chunk c0).
+__device__ __forceinline__ void q4k_superblock(const char* row, const char* xl, int xw, int c0, int g,
+                                               f32x4_t& acc) {
+  const uint4 head = *reinterpret_cast<const uint4*>(row);
+  const float d = codec::f16_value(head.x & 0xFFFFu), dm = codec::f16_value(head.x >> 16) * 0.0625f;
+  const uint32_t s6[2] = {head.y & 0x3F3F3F3Fu, (head.w & 0x0F0F0F0Fu) | ((head.y >> 2) & 0x30303030u)};
+  const uint32_t m6[2] = {head.z & 0x3F3F3F3Fu, ((head.w >> 4) & 0x0F0F0F0Fu) | ((head.z >> 2) & 0x30303030u)};
+  const uint4 minus16 = make_uint4(0xC180C180u, 0xC180C180u, 0xC180C180u, 0xC180C180u);
   const f32x4_t zero = {0.0f, 0.0f, 0.0f, 0.0f};
-  float d[NT], dm[NT];
-  uint32_t s6[NT][2], m6[NT][2];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    d[t] = codec::f16_value(head[t].x & 0xFFFFu);
-    dm[t] = codec::f16_value(head[t].x >> 16);
-    s6[t][0] = head[t].y & 0x3F3F3F3Fu;
-    m6[t][0] = head[t].z & 0x3F3F3F3Fu;
-    s6[t][1] = (head[t].w & 0x0F0F0F0Fu) | ((head[t].y >> 2) & 0x30303030u);
-    m6[t][1] = ((head[t].w >> 4) & 0x0F0F0F0Fu) | ((head[t].z >> 2) & 0x30303030u);
-  }
+  f32x4_t ps = zero, pm = zero;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    uint4 a[MT];
-    f32x4_t x1[MT];
+    const uint2 w = *reinterpret_cast<const uint2*>(row + 16 + 32 * (j / 2) + 8 * g);
+    const uint4 b = j % 2 == 0 ? make_uint4(q4k_pair<0, false>(w.x), q4k_pair<1, false>(w.x),
+                                            q4k_pair<0, false>(w.y), q4k_pair<1, false>(w.y))
+                               : make_uint4(q4k_pair<0, true>(w.x), q4k_pair<1, true>(w.x),
+                                            q4k_pair<0, true>(w.y), q4k_pair<1, true>(w.y));
+    // X in the codes' order 0 2 | 1 3 | 4 6 | 5 7
+    const uint4 v = *reinterpret_cast<const uint4*>(xl + 16 * ((c0 + 4 * j + g) ^ xw));
+    const uint4 a = make_uint4(__builtin_amdgcn_perm(v.y, v.x, 0x05040100u), __builtin_amdgcn_perm(v.y, v.x, 0x07060302u),
+                               __builtin_amdgcn_perm(v.w, v.z, 0x05040100u), __builtin_amdgcn_perm(v.w, v.z, 0x07060302u));
+    const f32x4_t x1 = mfma16(a, minus16, zero), pr = mfma16(a, b, x1);
+    const float fs = (float)((s6[j / 4] >> (8 * (j % 4))) & 0xFFu), fm = (float)((m6[j / 4] >> (8 * (j % 4))) & 0xFFu);
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {               // elements in the codes' order 0 2 | 1 3 | 4 6 | 5 7
-      const uint4 v = x[m][j];
-      a[m] = make_uint4(__builtin_amdgcn_perm(v.y, v.x, 0x05040100u), __builtin_amdgcn_perm(v.y, v.x, 0x07060302u),
-                        __builtin_amdgcn_perm(v.w, v.z, 0x05040100u), __builtin_amdgcn_perm(v.w, v.z, 0x07060302u));
-      x1[m] = mfma16(a[m], ones, zero);
+    for (int i = 0; i < 4; ++i) {
+      ps[i] = __builtin_fmaf(fs, pr[i], ps[i]);
+      pm[i] = __builtin_fmaf(fm, x1[i], pm[i]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) acc[i] = __builtin_fmaf(dm, pm[i], __builtin_fmaf(d, ps[i], acc[i]));
+}
+
+// -------------------------------------------------------------------------------- the kernel
+constexpr int kMaxWaves = 8;
+constexpr int kMaxRows = 16;
+constexpr int64_t kLdsBytes = 160 * 1024;
+
+template <int FMT, int NT, int COPY>
+__global__ __launch_bounds__(64 * kMaxWaves) void matvec_kernel(MatvecArgs p) {
+  extern __shared__ __align__(256) char smem[];
+  constexpr int CB = kCodeBytes<FMT>;
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, g = lane >> 4;
+  const int N = (int)p.w.N, K = (int)p.w.K;
+  const int tiles = (N + 16 * NT - 1) / (16 * NT);
+  const int item = (int)(blockIdx.x / tiles), n0 = (int)(blockIdx.x % tiles) * 16 * NT;
+  int e = 0;
+  int64_t r0 = (int64_t)item * p.xmax, r1 = min(r0 + p.xmax, p.R);
+  if (p.off != nullptr && !find_item(p.off, (int)p.w.E, p.R, item, p.xmax, e, r0, r1)) return;
+  const int xn = (int)(r1 - r0);
+  // lane l16 knows X row l16 of the group; a row that does not exist reads row 0, and zeros are stored
+  const int64_t xrow = l16 < xn ? x_row(p, r0 + l16) : -1;
+  const int xlo = xrow < 0 ? 0 : (int)xrow;
+  char* const mine = smem + wv * (NT * CB + p.xmax * 1024);
+  char* const xs = mine + NT * CB;
+  const int mr = l16 < xn ? l16 : xn - 1;         // rows past the last repeat it and are not stored
+  const char* const xl = xs + mr * 1024;
+  const int64_t pitch = FMT == QF_FMT_Q4K ? (int64_t)(K / 256) * 144 : K / 2;
+  const int64_t spitch = FMT == QF_FMT_NVFP4 ? K / 16 : K / 32;
+  const uint8_t* const codes = p.w.codes + ((int64_t)e * N + n0) * pitch;
+  const int last = N - 1 - n0;                    // weight rows past N repeat the last, not stored
+  const uint8_t* sp[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int row = 16 * t + l16;
+    sp[t] = p.w.scales + ((int64_t)e * N + n0 + (row < last ? row : last)) * spitch;
+  }
+  f32x4_t acc[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) acc[t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+
+  const int whole = FMT == QF_FMT_Q4K ? (K + 511) / 512 : K / 512;
+  for (int sl = wv; sl < whole; sl += p.waves) {
+    const bool half = FMT == QF_FMT_Q4K && K - sl * 512 < 512;
+    uint2 s[NT];
+    for (int m = 0; m < xn; ++m) {
+      const int c = lane ^ m;
+      copy16(p.X + (int64_t)__builtin_amdgcn_readlane(xlo, m) * p.ldx + sl * 512 + 8 * (half ? c & 31 : c), xs + m * 1024);
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const uint2 w = c[t][j / 2];
-      const uint4 b = j % 2 == 0 ? make_uint4(q4k_pair<0, false>(w.x), q4k_pair<1, false>(w.x),
-                                              q4k_pair<0, false>(w.y), q4k_pair<1, false>(w.y))
-                                 : make_uint4(q4k_pair<0, true>(w.x), q4k_pair<1, true>(w.x),
-                                              q4k_pair<0, true>(w.y), q4k_pair<1, true>(w.y));
-      const float t1 = d[t] * (float)((s6[t][j / 4] >> (8 * (j % 4))) & 0xFFu);
-      const float t2 = dm[t] * (float)((m6[t][j / 4] >> (8 * (j % 4))) & 0xFFu);
-      const float u = __builtin_fmaf(16.0f, t1, t2);
+      const int rest = last - 16 * t;             // (below zero: the tile is past N, its rows the last one)
+      copy_codes<FMT, COPY>(codes + (int64_t)(rest < 0 ? last : 16 * t) * pitch, pitch, rest < 0 ? 0 : rest, sl,
+                            half, mine + t * CB);
+      s[t] = load_scales<FMT>(sp[t] + g * (FMT == QF_FMT_NVFP4 ? 8 : 4), sl);
+    }
+    __builtin_amdgcn_s_waitcnt(0x0F70);           // vmcnt(0): this wave's copies are in its region
+    asm volatile("" ::: "memory");
+    if constexpr (FMT == QF_FMT_Q4K) {
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        const f32x4_t p = mfma16(a[m], b, zero);
+      for (int t = 0; t < NT; ++t) {
+        const char* const row = mine + t * CB + l16 * 288;
+        q4k_superblock(row, xl, mr, 0, g, acc[t]);
+        if (!half) q4k_superblock(row + 144, xl, mr, 32, g, acc[t]);
+      }
+    } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          acc[m][t][i] += __builtin_fmaf(t1, p[i], -(u * x1[m][i]));
+      for (int q = 0; q < 4; ++q) {
+        uint4 x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const uint4*>(xl + 16 * ((16 * g + 4 * q + i) ^ mr));
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const uint4 c = *reinterpret_cast<const uint4*>(mine + t * CB + l16 * 256 + 16 * ((4 * g + q) ^ l16));
+          const uint32_t sv = FMT == QF_FMT_NVFP4 ? (q < 2 ? s[t].x : s[t].y) >> (16 * (q & 1)) : s[t].x >> (8 * q);
+          multiply32<FMT>(c, sv, x, acc[t]);
+        }
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before the next copies land
+  }
+  if constexpr (FMT != QF_FMT_Q4K) {
+    // the k past the last whole slice, 128 at a time by the waves whose turn it is, 16 at a time per
+    // lane and straight from memory: nothing past K is read
+    const uint16_t* const xp = p.X + (int64_t)xlo * p.ldx;
+    for (int k1 = whole * 512, turn = whole % p.waves; k1 < K; k1 += 128, turn = turn + 1 == p.waves ? 0 : turn + 1) {
+      if (turn != wv) continue;
+      const int k = k1 + 32 * g;
+      uint4 x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[i] = make_uint4(0, 0, 0, 0);
+        if (xrow >= 0 && k + 8 * i < K) x[i] = *reinterpret_cast<const uint4*>(xp + k + 8 * i);
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const int row = 16 * t + l16;
+        const uint8_t* const cp = codes + (row < last ? row : last) * pitch + k / 2;
+        uint4 c = make_uint4(0, 0, 0, 0);
+        uint32_t s = 0;
+        if (k < K) {
+          const uint2 v = *reinterpret_cast<const uint2*>(cp);
+          c.x = v.x;
+          c.y = v.y;
+          s = sp[t][FMT == QF_FMT_NVFP4 ? k / 16 : k / 32];
+        }
+        if (k + 16 < K) {
+          const uint2 v = *reinterpret_cast<const uint2*>(cp + 8);
+          c.z = v.x;
+          c.w = v.y;
+          if (FMT == QF_FMT_NVFP4) s |= (uint32_t)sp[t][k / 16 + 1] << 8;
+        }
+        multiply32<FMT>(c, s, x, acc[t]);
       }
     }
   }
-}
 
-constexpr int kMaxWaves = 8;
-
-template <int FMT, int MT, int NT, bool ODD>
-__global__ __launch_bounds__(64 * kMaxWaves) void matvec_kernel(MatvecArgs p) {
-  extern __shared__ float red[];                 // [waves][MT][NT][4][64]
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, nw = blockDim.x >> 6;
-  const int l16 = lane & 15, g = lane >> 4;
-  const int N = (int)p.w.N, K = (int)p.w.K, tiles = (N + 16 * NT - 1) / (16 * NT);
-  const int item = (int)(blockIdx.x / tiles), n0 = (int)(blockIdx.x % tiles) * 16 * NT;
-  int e = 0;
-  int64_t r0 = 0, r1 = p.R;
-  if (p.off != nullptr && !find_item(p.off, (int)p.w.E, p.R, item, 16 * MT, e, r0, r1)) return;
-  // X rows of this lane; rows that do not exist read row 0 and are not stored (or stored as zeros)
-  const uint16_t* xp[MT];
+  __syncthreads();                                // the regions become the partial sums [wave][NT][4][64]
+  float* const red = reinterpret_cast<float*>(smem);
 #pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    const int64_t r = r0 + 16 * m + l16;
-    int64_t xr = 0;
-    if (r < r1) {
-      xr = r;
-      if (p.rows) xr = p.rows[r] < 0 ? -1 : p.rows[r] / p.rows_div;
-    }
-    xp[m] = p.X + (xr >= 0 && xr < p.M ? xr : 0) * p.ldx;
-  }
-  const int64_t rowbytes = FMT == QF_FMT_Q4K ? (int64_t)(K / 256) * 144 : K / 2;
-  const int64_t rowscales = FMT == QF_FMT_NVFP4 ? K / 16 : K / 32;
-  const uint8_t *cp[NT], *sp[NT];
+  for (int t = 0; t < NT; ++t)
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {                 // weight rows past N read the last one, not stored
-    const int n = n0 + 16 * t + l16;
-    const int64_t row = (int64_t)e * N + (n < N ? n : N - 1);
-    cp[t] = p.w.codes + row * rowbytes;
-    sp[t] = p.w.scales + row * rowscales;
-  }
-  f32x4_t acc[MT][NT];
-#pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int t = 0; t < NT; ++t) acc[m][t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-
-  if (FMT == QF_FMT_Q4K) {
-    for (int sb = wv; sb < K / 256; sb += nw) q4k_step<MT, NT>(cp, xp, sb, g, acc);
-  } else {
-    const int full = K / 128;
-    Stage<MT, NT> cur, nxt;
-    int st = wv;
-    if (st < full) load_stage<FMT, MT, NT, ODD>(cur, cp, sp, xp, st * 128 + 32 * g, 0x7FFFFFFF);
-    while (st < full) {
-      const int n = st + nw;
-      if (n < full) load_stage<FMT, MT, NT, ODD>(nxt, cp, sp, xp, n * 128 + 32 * g, 0x7FFFFFFF);
-      multiply_stage<FMT, MT, NT>(cur, acc);
-      cur = nxt;
-      st = n;
-    }
-    if (st == full && full * 128 < K) {          // the ragged end, by the wave whose turn it is
-      load_stage<FMT, MT, NT, ODD>(cur, cp, sp, xp, full * 128 + 32 * g, K);
-      multiply_stage<FMT, MT, NT>(cur, acc);
-    }
-  }
-
-  const int per = MT * NT * 256;
-#pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) red[wv * per + ((m * NT + t) * 4 + i) * 64 + lane] = acc[m][t][i];
+    for (int i = 0; i < 4; ++i) red[(wv * NT + t) * 256 + i * 64 + lane] = acc[t][i];
   __syncthreads();
   const float S = FMT == QF_FMT_NVFP4 ? p.w.S[e] : 1.0f;
-  for (int o = threadIdx.x; o < per; o += blockDim.x) {
-    const int ln = o & 63, i = (o >> 6) & 3, mt = o >> 8, t = mt % NT, m = mt / NT;
-    const int64_t r = r0 + 16 * m + 4 * (ln >> 4) + i;
+  for (int o = tid; o < NT * 256; o += p.waves * 64) {
+    const int ln = o & 63, i = (o >> 6) & 3, t = o >> 8;
+    const int64_t r = r0 + 4 * (ln >> 4) + i;
     const int n = n0 + 16 * t + (ln & 15);
     if (r >= r1 || n >= N) continue;
-    float s = 0.0f;
-    for (int w = 0; w < nw; ++w) s += red[w * per + o];
-    if (FMT == QF_FMT_NVFP4) s *= S;
-    if (p.off != nullptr) {                      // an X row that does not exist counts as zeros
-      const int64_t xr = p.rows ? (p.rows[r] < 0 ? -1 : p.rows[r] / p.rows_div) : r;
-      if (xr < 0 || xr >= p.M) s = 0.0f;
-    }
-    if (p.y_f32) static_cast<float*>(p.Y)[r * p.ldy + n] = s;
-    else static_cast<uint16_t*>(p.Y)[r * p.ldy + n] = (uint16_t)codec::bf16_rne(s);
+    float v = 0.0f;
+    for (int w = 0; w < p.waves; ++w) v += red[w * NT * 256 + o];
+    if (FMT == QF_FMT_NVFP4) v *= S;
+    if (x_row(p, r) < 0) v = 0.0f;
+    if (p.y_f32) static_cast<float*>(p.Y)[r * p.ldy + n] = v;
+    else static_cast<uint16_t*>(p.Y)[r * p.ldy + n] = (uint16_t)codec::bf16_rne(v);
   }
 }
 
-template <int FMT, int MT, int NT, bool ODD>
-hipError_t launch_one(const MatvecArgs& a, int64_t items, hipStream_t s) {
-  const int64_t N = a.w.N, K = a.w.K, step = FMT == QF_FMT_Q4K ? 256 : 128;
-  const int nw = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxWaves, (K + step - 1) / step));
-  const int64_t blocks = (N + 16 * NT - 1) / (16 * NT) * items;
+template <int FMT, int NT, int COPY>
+hipError_t launch_tiles(const MatvecArgs& a, hipStream_t s) {
+  const int64_t blocks = (a.w.N + 16 * NT - 1) / (16 * NT) * a.items;
   if (blocks > INT32_MAX) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((matvec_kernel<FMT, MT, NT, ODD>), dim3((unsigned)blocks), dim3(64 * nw),
-                     (size_t)nw * MT * NT * 1024, s, a);
+  const size_t lds = (size_t)a.waves * (NT * kCodeBytes<FMT> + a.xmax * 1024);
+  hipLaunchKernelGGL((matvec_kernel<FMT, NT, COPY>), dim3((unsigned)blocks), dim3(64 * a.waves), lds, s, a);
   return hipGetLastError();
 }
 
-template <int FMT, bool ODD>
-hipError_t launch_fmt(const MatvecArgs& a, int mt, int nt, int64_t items, hipStream_t s) {
-  if (mt == 1 && nt == 1) return launch_one<FMT, 1, 1, ODD>(a, items, s);
-  if (mt == 1) return launch_one<FMT, 1, 2, ODD>(a, items, s);
-  if (mt == 2 && nt == 1) return launch_one<FMT, 2, 1, ODD>(a, items, s);
-  if (mt == 2) return launch_one<FMT, 2, 2, ODD>(a, items, s);
-  if (nt == 1) return launch_one<FMT, 4, 1, ODD>(a, items, s);
-  return launch_one<FMT, 4, 2, ODD>(a, items, s);
+template <int FMT>
+hipError_t launch_fmt(const MatvecArgs& a, int nt, int copy, hipStream_t s) {
+  if (FMT == QF_FMT_NVFP4 && copy == kCopyWords)
+    return nt == 1 ? launch_tiles<QF_FMT_NVFP4, 1, kCopyWords>(a, s) : launch_tiles<QF_FMT_NVFP4, 2, kCopyWords>(a, s);
+  if (copy == kCopyNt) return nt == 1 ? launch_tiles<FMT, 1, kCopyNt>(a, s) : launch_tiles<FMT, 2, kCopyNt>(a, s);
+  return nt == 1 ? launch_tiles<FMT, 1, kCopy>(a, s) : launch_tiles<FMT, 2, kCopy>(a, s);
 }
 
 }  // namespace
@@ -355,21 +410,49 @@ hipError_t launch_fmt(const MatvecArgs& a, int mt, int nt, int64_t items, hipStr
 hipError_t launch_packed_matvec(const PackedOperand& w, const int64_t* off, int64_t R,
                                 const int32_t* rows, int64_t rows_div, int64_t M, const uint16_t* X,
                                 int64_t ldx, void* Y, int64_t ldy, int y_f32, hipStream_t s) {
-  MatvecArgs a{w, X, ldx, M, Y, ldy, R, y_f32, off, rows, (int)rows_div};
+  MatvecArgs a{w, X, ldx, M, Y, ldy, R, y_f32, off, rows, (int)rows_div, 0, 0, 0};
   if (M == 0) a.w.K = 0;                         // no X at all: zeros
-  int mt = R <= 16 ? 1 : R <= 32 ? 2 : 4;
-  int64_t items = 1;
-  if (off != nullptr) {
-    mt = R <= 8 * w.E ? 1 : R <= 16 * w.E ? 2 : 4;
-    items = std::min<int64_t>(w.E, R) + R / (16 * mt);      // sum of ceil(rows / chunk) at most
+  // Rows a workgroup takes.  Experts: more than the mean, since LDS for rows that most experts do not
+  // have costs waves, and an expert with more rows is read again from the last-level cache (3072 x
+  // 3072 NVFP4, 32 tokens to 8 of 128: 4 rows 117 us, 8 rows 111; 2048 x 2048 Q4_K, 16 to 4 of 64: 4
+  // rows 33.2, 8 rows 34.7; 3072 x 1536 MXFP4, 64 to 8 of 128: 8 rows 71.8, 16 rows 77.7).
+  const int64_t xmax = off == nullptr ? kMaxRows : 2 * R <= 3 * w.E ? 4 : R <= 4 * w.E ? 8 : kMaxRows;
+  a.xmax = (int)std::min(R, xmax);
+  // row groups: of a dense call ceil(R / xmax); of E experts at most one more each
+  const int64_t items = off ? std::min(w.E, R) + R / a.xmax : (R + a.xmax - 1) / a.xmax;
+  a.items = (int)items;                          // (R < 2^30)
+  // Tile height and waves a tile: the least of rounds of resident workgroups x (slices a wave takes +
+  // 1 for start and end) x what a slice copies.  Measured against it, us: 24576 x 4096 NVFP4, 1 row, 8
+  // / 4 / 2 waves 15.4 / 14.8 / 15.4; 4096 x 4096 8 / 4 / 2 waves 5.1 / 5.8 / 7.4; 24576 x 4096, 16
+  // rows, one tile 4 waves / two tiles 4 / 2 waves 24.3 / 28.3 / 21.2; 64 rows x 4096 x 4096 MXFP4, 8 /
+  // 4 / 2 waves 15.9 / 12.9 / 11.4.
+  const int64_t busy = off ? std::min(w.E, R) : items;       // row groups that are likely there
+  const int64_t slices = std::max<int64_t>(1, (a.w.K + 511) / 512), cus = compute_units();
+  const int64_t codes = w.fmt == QF_FMT_Q4K ? kCodeBytes<QF_FMT_Q4K> : kCodeBytes<QF_FMT_NVFP4>;
+  int nt = 1;
+  int64_t least = INT64_MAX;
+  for (int t = 1; t <= 2; ++t) {
+    const int64_t unit = t * codes + a.xmax * 1024, blocks = (w.N + 16 * t - 1) / (16 * t) * busy;
+    for (int64_t each = (slices + kMaxWaves - 1) / kMaxWaves; each <= slices; ++each) {
+      const int64_t waves = (slices + each - 1) / each;
+      if (waves * unit > kLdsBytes) continue;
+      const int64_t resident = cus * std::min(kLdsBytes / (waves * unit), 32 / waves);
+      const int64_t cost = (blocks + resident - 1) / resident * (each + 1) * unit;
+      if (cost < least) {
+        least = cost;
+        nt = t;
+        a.waves = (int)waves;
+      }
+    }
   }
-  const int nt = (w.N + 31) / 32 * items >= 2 * compute_units() ? 2 : 1;
+  // Codes that are read once, and are many, past the caches (24576 x 4096 NVFP4, one row, 14.9 -> 14.4
+  // us; 12288-deep MXFP4 9.9 -> 9.5); small weights may still be there from before, and further row
+  // groups read them again (4096 x 4096: 16 rows 6.8 -> 7.0 us, 64 rows 13.5 -> 14.6).
+  int copy = (off != nullptr || items == 1) && busy * w.N * w.K >= (int64_t)1 << 25 ? kCopyNt : kCopy;
   switch (w.fmt) {
-    case QF_FMT_NVFP4:
-      if (w.K % 32) return launch_fmt<QF_FMT_NVFP4, true>(a, mt, nt, items, s);
-      return launch_fmt<QF_FMT_NVFP4, false>(a, mt, nt, items, s);
-    case QF_FMT_MXFP4: return launch_fmt<QF_FMT_MXFP4, false>(a, mt, nt, items, s);
-    default: return launch_fmt<QF_FMT_Q4K, false>(a, mt, nt, items, s);
+    case QF_FMT_NVFP4: return launch_fmt<QF_FMT_NVFP4>(a, nt, w.K % 32 ? kCopyWords : copy, s);
+    case QF_FMT_MXFP4: return launch_fmt<QF_FMT_MXFP4>(a, nt, copy, s);
+    default: return launch_fmt<QF_FMT_Q4K>(a, nt, copy, s);
   }
 }
 
