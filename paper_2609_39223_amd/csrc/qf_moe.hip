@@ -42,17 +42,22 @@ struct AddF {
     return as_u32(as_f32(a) + as_f32(b));
   }
 };
-// Reduction over the L lanes of a token (16 or 64), the same bits in all of them: lane ^ 1, ^ 2,
-// then the mirror images inside 8 and 16 lanes (whose sources are alike within 4 and 8), ^ 16, ^ 32.
+// Reduction over the L lanes of a token (16, 32 or 64), the same bits in all of them: lane ^ 1, ^ 2,
+// then the mirror images inside 8 and 16 lanes (whose sources are alike within 4 and 8), ^ 16 and ^ 32
+// by the swaps of 16- and 32-lane rows (which hand a register's even and odd rows to every lane).
 template <int L, class Op>
 __device__ __forceinline__ uint32_t group_reduce(uint32_t v, Op op) {
   v = op(v, dpp_u32<0xB1>(v));
   v = op(v, dpp_u32<0x4E>(v));
   v = op(v, dpp_u32<0x141>(v));
   v = op(v, dpp_u32<0x140>(v));
+  if (L >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = op(r[0], r[1]);
+  }
   if (L == 64) {
-    v = op(v, (uint32_t)__shfl_xor((int)v, 16, 64));
-    v = op(v, (uint32_t)__shfl_xor((int)v, 32, 64));
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    v = op(r[0], r[1]);
   }
   return v;
 }
@@ -117,8 +122,10 @@ __device__ __forceinline__ float log_sigmoid(float x) {
   return fminf(x, 0.0f) - log1pf(expf(-fabsf(x)));
 }
 
-// One round per choice over the keys of this lane; lane j < k of the group ends up with choice j
-// (expert id, -1: none left; its logit v).
+// Lane j < k of the group ends up with choice j (expert id, -1: none left; its logit v).
+//
+// FP32 logits: a round finds the largest key of the row, the first lane that has it and that lane's
+// first expert with it, which is struck out.
 template <int L, int C>
 __device__ __forceinline__ void choose(uint32_t key[8 * C], int lane, int k, int& id, float& v) {
   id = -1;
@@ -145,6 +152,38 @@ __device__ __forceinline__ void choose(uint32_t key[8 * C], int lane, int k, int
   }
 }
 
+// bf16 logits leave 16 bits of a key for the expert's complement, so one maximum decides a round;
+// a lane sorts its eight keys once and a round takes the best lane's first one away (32768 x 128, 8
+// choices: 9.8 us without either, 7.0 so).
+__device__ __forceinline__ void sort8_falling(uint32_t a[8]) {
+  constexpr int net[19][2] = {{0, 1}, {2, 3}, {4, 5}, {6, 7}, {0, 2}, {1, 3}, {4, 6}, {5, 7}, {1, 2}, {5, 6},
+                              {0, 4}, {1, 5}, {2, 6}, {3, 7}, {2, 4}, {3, 5}, {1, 2}, {3, 4}, {5, 6}};
+#pragma unroll
+  for (int i = 0; i < 19; ++i) {
+    const uint32_t x = a[net[i][0]], y = a[net[i][1]];
+    a[net[i][0]] = x > y ? x : y;
+    a[net[i][1]] = x > y ? y : x;
+  }
+}
+template <int L>
+__device__ __forceinline__ void choose_sorted(uint32_t key[8], int lane, int k, int& id, float& v) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    key[i] = key[i] ? (key[i] & 0xFFFF0000u) | (0xFFFFu - (uint32_t)(8 * lane + i)) : 0u;
+  sort8_falling(key);
+  uint32_t mine = 0;
+  for (int j = 0; j < k; ++j) {
+    const uint32_t top = group_reduce<L>(key[0], MaxU());
+    const bool taken = key[0] == top;             // one lane's, or top = 0 and nothing is left
+#pragma unroll
+    for (int i = 0; i < 7; ++i) key[i] = taken ? key[i + 1] : key[i];
+    key[7] = taken ? 0u : key[7];
+    if (lane == j) mine = top;
+  }
+  id = mine ? (int)(0xFFFFu - (mine & 0xFFFFu)) : -1;
+  v = mine ? key_value((mine >> 31) ? mine & 0xFFFF0000u : mine | 0xFFFFu) : 0.0f;
+}
+
 template <class Z, int L, int C>
 __global__ __launch_bounds__(kRouteThreads) void route_kernel(
     const Z* __restrict__ z, int64_t T, int E, int64_t ldz, int k, int score, int norm, float scale,
@@ -167,7 +206,8 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(
   for (int i = 0; i < 8 * C; ++i) key[i] = key_of(x[i]);
   int id;
   float v;
-  choose<L, C>(key, lane, k, id, v);
+  if constexpr (sizeof(Z) == 2 && C == 1) choose_sorted<L>(key, lane, k, id, v);
+  else choose<L, C>(key, lane, k, id, v);
   const bool has = id >= 0;
   float out;
   if (norm) {
@@ -257,7 +297,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_bwd_kernel(
   __syncthreads();
   if (t >= T) return;
   // a token without choices has no gradient, whatever its logits are
-  const bool none = whole && (__ballot(has) >> ((threadIdx.x & 63) / L * L) & (L == 64 ? ~0ull : 0xFFFFull)) == 0;
+  const bool none = whole && (__ballot(has) >> ((threadIdx.x & 63) / L * L) & (L == 64 ? ~0ull : (1ull << L % 64) - 1)) == 0;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const int e0 = 8 * (c * L + lane);
@@ -285,12 +325,16 @@ __device__ __forceinline__ int bucket_of(int id, int E) { return id >= 0 && id <
 constexpr int kSortThreads = 256;
 constexpr int kSortWaves = kSortThreads / 64;
 constexpr int kMaxChunks = 256;
+constexpr int64_t kMinChunk = 1024;
+// A launch that compares all pairs, or three: 256 tokens x 8 10.3 / 10.9 us, 1024 x 2 7.1 / 14.4, 512 x 8
+// 18.5 / 11.4 (128 and 256 experts, rows of 512 and 2048 columns copied).
+constexpr int64_t kSmallSort = 2048;
 constexpr int kMaxBuckets = 1025;
 
 // Slots of a chunk: a multiple of 256, such that at most kMaxChunks chunks cover n slots.
 int64_t sort_chunk(int64_t n) {
   const int64_t c = (n + kMaxChunks - 1) / kMaxChunks;
-  return std::max<int64_t>(2048, (c + 255) / 256 * 256);
+  return std::max<int64_t>(kMinChunk, (c + 255) / 256 * 256);
 }
 
 // counts [chunk][E + 1].
@@ -343,21 +387,27 @@ __global__ __launch_bounds__(kSortThreads) void sort_rank_kernel(
     const int32_t* __restrict__ ids, int64_t n, int E, int64_t chunk, const int32_t* __restrict__ counts,
     int64_t* __restrict__ offsets, int32_t* __restrict__ row_of, int32_t* __restrict__ slot_of) {
   __shared__ int first[kMaxBuckets];                 // total, then first row, of each bucket
-  __shared__ int next[kSortWaves][kMaxBuckets];      // next row of the bucket in each wave
   __shared__ int before[kMaxBuckets];                // slots of the bucket in earlier chunks
+  __shared__ int next[kSortWaves][kMaxBuckets];      // next row of the bucket in each wave
   __shared__ int part[kSortWaves];
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, nb = E + 1;
   const int nchunks = gridDim.x, me = blockIdx.x;
   for (int e = threadIdx.x; e < nb; e += kSortThreads) {
+    first[e] = before[e] = 0;
+    for (int i = 0; i < kSortWaves; ++i) next[i][e] = 0;
+  }
+  __syncthreads();
+  // wave w sums the chunks w, w + 4, ..., a lane per bucket (a long chain of loads if one wave did)
+  for (int e = lane; e < nb; e += 64) {
     int pre = 0, all = 0;
-    for (int c = 0; c < nchunks; ++c) {
+#pragma unroll 8
+    for (int c = wv; c < nchunks; c += kSortWaves) {
       const int v = counts[(int64_t)c * nb + e];
       all += v;
       pre += c < me ? v : 0;
     }
-    first[e] = all;
-    before[e] = pre;
-    for (int i = 0; i < kSortWaves; ++i) next[i][e] = 0;
+    atomicAdd(&first[e], all);
+    atomicAdd(&before[e], pre);
   }
   __syncthreads();
   block_exclusive(first, nb, part);
@@ -401,7 +451,77 @@ __global__ __launch_bounds__(kSortThreads) void sort_rank_kernel(
   }
 }
 
+// Few slots, all in one launch: workgroup t counts, for each of token t's slots, the slots that come
+// before it (a lower bucket, or the same one and a lower slot) by ballots over all n, and copies its
+// row; the last workgroup counts the buckets.  T n comparisons instead of two more launches.
+__global__ __launch_bounds__(kSortThreads) void sort_small_kernel(
+    const int32_t* __restrict__ ids, int64_t T, int E, int k, int64_t* __restrict__ offsets,
+    int32_t* __restrict__ row_of, int32_t* __restrict__ slot_of, const uint16_t* __restrict__ X,
+    int64_t H, int64_t ldx, uint16_t* __restrict__ Xg) {
+  __shared__ int h[kMaxBuckets];
+  __shared__ int part[kSortWaves];
+  __shared__ int count[kSortWaves][64];
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, n = (int)T * k, t = blockIdx.x;
+  if (t == (int)T) {
+    for (int e = tid; e <= E; e += kSortThreads) h[e] = 0;
+    __syncthreads();
+    for (int i = tid; i < n; i += kSortThreads) atomicAdd(&h[bucket_of(ids[i], E)], 1);
+    __syncthreads();
+    block_exclusive(h, E + 1, part);
+    for (int e = tid; e <= E; e += kSortThreads) offsets[e] = h[e];
+    return;
+  }
+  // lane j < k of every wave: the bucket and the slots found before slot (t, j)
+  const int own = lane < k ? bucket_of(ids[t * k + lane], E) : 0;
+  int before = 0;
+  for (int i0 = wv * 64; i0 < n; i0 += kSortThreads) {
+    const int i = i0 + lane, e = i < n ? bucket_of(ids[i], E) : 0x7FFFFFFF;
+    for (int j = 0; j < k; ++j) {
+      const int b = __builtin_amdgcn_readlane(own, j);
+      const int c = __popcll(__ballot(e < b || (e == b && i < t * k + j)));
+      if (lane == j) before += c;
+    }
+  }
+  count[wv][lane] = before;
+  __syncthreads();
+  int row = 0;
+  if (lane < k) {
+    for (int i = 0; i < kSortWaves; ++i) row += count[i][lane];
+    if (wv == 0) {
+      row_of[t * k + lane] = own < E ? row : ~row;
+      slot_of[row] = own < E ? t * k + lane : -1;
+    }
+  }
+  if (X == nullptr) return;
+  for (int64_t c = tid * 8; c < H; c += kSortThreads * 8) {
+    const uint4 v = *reinterpret_cast<const uint4*>(X + t * ldx + c);
+    for (int j = 0; j < k; ++j)
+      *reinterpret_cast<uint4*>(Xg + (int64_t)__builtin_amdgcn_readlane(row, j) * H + c) =
+          __builtin_amdgcn_readlane(own, j) < E ? v : make_uint4(0, 0, 0, 0);
+  }
+}
+
+// Expert rows are read non-temporally: a launch reads each once, and seldom again soon.  They are
+// written so only past half the last-level cache of 256 MB: below, the product that follows finds them
+// there (8 rows of 3072 a token, us without / with: sum of 2048 tokens 24.3 / 20.9, of 32768 351 / 328;
+// sort, copy and gradient of 32768 738 / 708; gradients of 4096 91.6 / 84.2 alone, but with the sum that
+// reads them next 106 / 124).
+typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint4 load_nt(const uint16_t* p) {
+  const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p));
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+template <bool NT>
+__device__ __forceinline__ void store_row(uint16_t* p, uint4 q) {
+  const u32x4_t u = {q.x, q.y, q.z, q.w};
+  if (NT) __builtin_nontemporal_store(u, reinterpret_cast<u32x4_t*>(p));
+  else *reinterpret_cast<uint4*>(p) = q;
+}
+bool rows_past_cache(int64_t n, int64_t H) { return n * H * 2 > (int64_t)128 << 20; }
+
 // Xg[row] = X[t] for the rows of token t's slots, zeros for dropped ones: a wave copies 512 columns.
+// Bound by writing the rows: 32768 tokens x 8 x 3072 377 us = 4.8 TB/s.
+template <bool NT>
 __global__ __launch_bounds__(256) void gather_kernel(const int32_t* __restrict__ row_of, int64_t T,
                                                      int k, int64_t H, int64_t ldx, int segs,
                                                      const uint16_t* __restrict__ X,
@@ -414,14 +534,36 @@ __global__ __launch_bounds__(256) void gather_kernel(const int32_t* __restrict__
   const int32_t* const r = row_of + t * k;
   for (int j = 0; j < k; ++j) {
     const int row = r[j];
-    *reinterpret_cast<uint4*>(Xg + (int64_t)(row >= 0 ? row : ~row) * H + c) =
-        row >= 0 ? v : make_uint4(0, 0, 0, 0);
+    store_row<NT>(Xg + (int64_t)(row >= 0 ? row : ~row) * H + c, row >= 0 ? v : make_uint4(0, 0, 0, 0));
   }
 }
 
 // ============================================================================= weighted sum
-// Y[t] = sum over j of w_j Yg[row_j]: a wave takes 512 columns of a token and keeps KB rows' loads
-// in flight.
+// A wave's view of KB slots of token t from j0 on: lane j < KB holds slot j0 + j's entry of row_of
+// (kNoRow past k) and its weight; bit j of `live`: the slot has a row.
+constexpr int kNoRow = 0x7FFFFFFF;
+template <int KB>
+struct Slots {
+  int row;
+  float wt;
+  uint32_t live;
+  __device__ __forceinline__ Slots(const int32_t* row_of, const float* w, int64_t t, int k, int j0, int64_t n) {
+    const int j = j0 + (threadIdx.x & 63);
+    const bool in = (int)(threadIdx.x & 63) < KB && j < k;
+    row = in ? row_of[t * k + j] : kNoRow;
+    wt = in && w ? w[t * k + j] : 1.0f;
+    live = (uint32_t)__ballot(row >= 0 && row < n);        // (n < 2^31, so never a kNoRow)
+  }
+  __device__ __forceinline__ int row_at(int j) const { return __builtin_amdgcn_readlane(row, j); }
+  __device__ __forceinline__ float weight_at(int j) const {
+    return as_f32((uint32_t)__builtin_amdgcn_readlane((int)as_u32(wt), j));
+  }
+  __device__ __forceinline__ bool has(int j) const { return (live >> j) & 1u; }
+};
+
+// Y[t] = sum over j of w_j Yg[row_j]: a wave takes 512 columns of a token and has KB rows' loads in
+// flight (a slot without a row loads row 0 and leaves it: no branch between the loads).  Bound by
+// reading the rows: 32768 tokens x 8 x 3072 328 us = 5.5 TB/s.
 template <int KB>
 __global__ __launch_bounds__(256) void combine_kernel(const int32_t* __restrict__ row_of,
                                                       const float* __restrict__ w, int64_t T, int k,
@@ -429,77 +571,73 @@ __global__ __launch_bounds__(256) void combine_kernel(const int32_t* __restrict_
                                                       uint16_t* __restrict__ Y, int64_t ldy) {
   const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int64_t t = __builtin_amdgcn_readfirstlane((int)(item / segs)), n = T * k;
-  const int64_t c = (item % segs) * 512 + (threadIdx.x & 63) * 8;
-  if (t >= T || c >= H) return;
+  const int64_t c0 = (item % segs) * 512 + (threadIdx.x & 63) * 8, c = c0 < H ? c0 : 0;
+  if (t >= T) return;
   float acc[8] = {};
   for (int j0 = 0; j0 < k; j0 += KB) {
+    const Slots<KB> s(row_of, w, t, k, j0, n);
+    if (s.live == 0) continue;
     uint4 v[KB];
-    float wt[KB];
+#pragma unroll
+    for (int j = 0; j < KB; ++j) v[j] = load_nt(Yg + (s.has(j) ? (int64_t)s.row_at(j) * H : 0) + c);
 #pragma unroll
     for (int j = 0; j < KB; ++j) {
-      const int row = j0 + j < k ? row_of[t * k + j0 + j] : -1;
-      v[j] = make_uint4(0, 0, 0, 0);
-      wt[j] = 0.0f;
-      if (row >= 0 && row < n) {
-        v[j] = *reinterpret_cast<const uint4*>(Yg + (int64_t)row * H + c);
-        wt[j] = w ? w[t * k + j0 + j] : 1.0f;
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < KB; ++j) {
+      if (!s.has(j)) continue;
       uint32_t h[8];
       codec::unpack8(v[j], h);
+      const float wt = s.weight_at(j);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) acc[i] = __builtin_fmaf(wt[j], as_f32(h[i] << 16), acc[i]);
+      for (int i = 0; i < 8; ++i) acc[i] = __builtin_fmaf(wt, as_f32(h[i] << 16), acc[i]);
     }
   }
-  store8(Y + t * ldy + c, acc);
+  if (c0 < H) store8(Y + t * ldy + c, acc);
 }
 
 // dYg[row_j] = w_j dY[t] and dw_j = <dY[t], Yg[row_j]>: a workgroup of W waves takes a token, wave w
 // the 512-column pieces w, w + W, ..., KB rows at a time; dw's partial sums meet in LDS in wave
-// order.
-template <int KB, int W>
+// order.  Bound by the rows read and written: 32768 tokens x 8 x 3072 650 us = 5.3 TB/s.
+template <int KB, int W, bool NT>
 __global__ __launch_bounds__(64 * W) void combine_bwd_kernel(
     const int32_t* __restrict__ row_of, const float* __restrict__ w, int64_t T, int k, int64_t H,
     const uint16_t* __restrict__ dY, int64_t lddy, const uint16_t* __restrict__ Yg,
     uint16_t* __restrict__ dYg, float* __restrict__ dw) {
   __shared__ float part[W][KB];
   const int64_t t = blockIdx.x, n = T * k;
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   for (int j0 = 0; j0 < k; j0 += KB) {
-    int row[KB];
-    float wt[KB], dot[KB];
+    const Slots<KB> s(row_of, w, t, k, j0, n);
+    float dot[KB];
 #pragma unroll
-    for (int j = 0; j < KB; ++j) {
-      row[j] = j0 + j < k ? row_of[t * k + j0 + j] : 0x7FFFFFFF;   // no row at all
-      wt[j] = j0 + j < k && w ? w[t * k + j0 + j] : 1.0f;
-      dot[j] = 0.0f;
-    }
-    for (int64_t c = wv * 512 + lane * 8; c < H; c += 512 * W) {
+    for (int j = 0; j < KB; ++j) dot[j] = 0.0f;
+    for (int64_t c0 = wv * 512; c0 < H; c0 += 512 * W) {
+      const int64_t c1 = c0 + lane * 8, c = c1 < H ? c1 : 0;
+      const bool in = c1 < H;
       float d[8];
-      load_logits8(dY + t * lddy + c, d);
       uint4 y[KB];
+      load_logits8(dY + t * lddy + c, d);
+      if (dw) {
 #pragma unroll
-      for (int j = 0; j < KB; ++j) {
-        y[j] = make_uint4(0, 0, 0, 0);
-        if (dw && row[j] >= 0 && row[j] < n) y[j] = *reinterpret_cast<const uint4*>(Yg + (int64_t)row[j] * H + c);
+        for (int j = 0; j < KB; ++j) y[j] = load_nt(Yg + (s.has(j) ? (int64_t)s.row_at(j) * H : 0) + c);
       }
+      if (dYg) {
 #pragma unroll
-      for (int j = 0; j < KB; ++j) {
-        const bool has = row[j] >= 0 && row[j] < n;
-        if (dw && has) {
+        for (int j = 0; j < KB; ++j) {
+          const int row = s.row_at(j);
+          const int64_t to = row >= 0 ? row : ~row;
+          const float wt = s.weight_at(j);
+          uint32_t o[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) o[i] = s.has(j) ? codec::bf16_rne(wt * d[i]) : 0u;
+          if (to < n && in) store_row<NT>(dYg + to * H + c, codec::pack8(o));
+        }
+      }
+      if (dw) {
+#pragma unroll
+        for (int j = 0; j < KB; ++j) {
           uint32_t h[8];
           codec::unpack8(y[j], h);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) dot[j] = __builtin_fmaf(d[i], as_f32(h[i] << 16), dot[j]);
-        }
-        const int64_t to = row[j] >= 0 ? row[j] : ~row[j];
-        if (dYg && to < n) {
-          float o[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) o[i] = has ? wt[j] * d[i] : 0.0f;
-          store8(dYg + to * H + c, o);
+          for (int i = 0; i < 8; ++i) dot[j] = __builtin_fmaf(in ? d[i] : 0.0f, in ? as_f32(h[i] << 16) : 0.0f, dot[j]);
         }
       }
     }
@@ -512,25 +650,52 @@ __global__ __launch_bounds__(64 * W) void combine_bwd_kernel(
     }
     __syncthreads();
     if (threadIdx.x < KB && j0 + (int)threadIdx.x < k) {
-      float s = 0.0f;
-      for (int i = 0; i < W; ++i) s += part[i][threadIdx.x];
-      dw[t * k + j0 + threadIdx.x] = s;
+      float v = 0.0f;
+      for (int i = 0; i < W; ++i) v += part[i][threadIdx.x];
+      dw[t * k + j0 + threadIdx.x] = s.has((int)threadIdx.x) ? v : 0.0f;   // (a slot without a row saw row 0)
     }
     __syncthreads();
   }
+}
+
+// Waves a token: as many as its row has 512-column pieces, up to 4, which then take several each (8
+// rows of 3072, 32768 tokens, us, 1 / 2 / 4 / 8 waves 1041 / 1035 / 1034 / 1032; 9000 x 4 rows of 1000:
+// 58 / 55 / 58 / 76), 8 where tokens are fewer than compute units (16 tokens 20.1 / 13.7 / 11.6 / 10.7).
+template <int KB, int W>
+void launch_combine_bwd_waves(const int32_t* row_of, const float* w, int64_t T, int k, int64_t H,
+                              const uint16_t* dY, int64_t lddy, const uint16_t* Yg, uint16_t* dYg,
+                              float* dw, hipStream_t s) {
+  if (rows_past_cache(T * k, H))
+    hipLaunchKernelGGL((combine_bwd_kernel<KB, W, true>), dim3((unsigned)T), dim3(64 * W), 0, s, row_of, w, T, k, H,
+                       dY, lddy, Yg, dYg, dw);
+  else
+    hipLaunchKernelGGL((combine_bwd_kernel<KB, W, false>), dim3((unsigned)T), dim3(64 * W), 0, s, row_of, w, T, k, H,
+                       dY, lddy, Yg, dYg, dw);
+}
+template <int KB>
+void launch_combine_bwd(const int32_t* row_of, const float* w, int64_t T, int k, int64_t H,
+                        const uint16_t* dY, int64_t lddy, const uint16_t* Yg, uint16_t* dYg, float* dw,
+                        hipStream_t s) {
+  if (H <= 512) launch_combine_bwd_waves<KB, 1>(row_of, w, T, k, H, dY, lddy, Yg, dYg, dw, s);
+  else if (H <= 1024) launch_combine_bwd_waves<KB, 2>(row_of, w, T, k, H, dY, lddy, Yg, dYg, dw, s);
+  else if (H <= 2048 || T >= compute_units()) launch_combine_bwd_waves<KB, 4>(row_of, w, T, k, H, dY, lddy, Yg, dYg, dw, s);
+  else launch_combine_bwd_waves<KB, 8>(row_of, w, T, k, H, dY, lddy, Yg, dYg, dw, s);
 }
 
 int rows_at_once(int k) { return k <= 1 ? 1 : k <= 2 ? 2 : k <= 4 ? 4 : 8; }
 
 }  // namespace
 
-// E <= 128 and k <= 16 fit 16 lanes a token (four tokens a wave); else a wave takes one token.
+// 8 experts a lane: 16 lanes a token (four tokens a wave) for up to 128 experts and 16 choices, 32
+// for up to 256 and 32, else 64, with 16 experts a lane past 512 (32768 tokens, us: 128 experts 7.1, 256
+// in 32 lanes 11.6, in 64 22.3).
 #define QF_ROUTE(KERNEL, Z, L, C, ...)                                                           \
   hipLaunchKernelGGL((KERNEL<Z, L, C>), dim3((unsigned)((T + kRouteThreads / L - 1) / (kRouteThreads / L))), \
                      dim3(kRouteThreads), 0, s, __VA_ARGS__)
 #define QF_ROUTE_BY_SIZE(KERNEL, Z, ...)                            \
   do {                                                              \
     if (E <= 128 && k <= 16) QF_ROUTE(KERNEL, Z, 16, 1, __VA_ARGS__); \
+    else if (E <= 256 && k <= 32) QF_ROUTE(KERNEL, Z, 32, 1, __VA_ARGS__); \
     else if (E <= 512) QF_ROUTE(KERNEL, Z, 64, 1, __VA_ARGS__);     \
     else QF_ROUTE(KERNEL, Z, 64, 2, __VA_ARGS__);                   \
   } while (0)
@@ -560,13 +725,19 @@ hipError_t launch_moe_sort(const int32_t* ids, int64_t T, int E, int k, int64_t*
                            int32_t* row_of, int32_t* slot_of, const uint16_t* X, int64_t H,
                            int64_t ldx, uint16_t* Xg, int32_t* ws, hipStream_t s) {
   const int64_t n = T * k, chunk = sort_chunk(n);
-  const dim3 grid((unsigned)std::max<int64_t>(1, (n + chunk - 1) / chunk));
-  if (n > 0) hipLaunchKernelGGL(sort_count_kernel, grid, dim3(kSortThreads), 0, s, ids, n, E, chunk, ws);
-  if (n == 0) return launch_fill_f32(reinterpret_cast<float*>(offsets), 2 * (E + 1), 0.0f, s);
+  if (n <= kSmallSort) {
+    hipLaunchKernelGGL(sort_small_kernel, dim3((unsigned)T + 1), dim3(kSortThreads), 0, s, ids, T, E, k, offsets,
+                       row_of, slot_of, X, H, ldx, Xg);
+    return hipGetLastError();
+  }
+  const dim3 grid((unsigned)((n + chunk - 1) / chunk));
+  hipLaunchKernelGGL(sort_count_kernel, grid, dim3(kSortThreads), 0, s, ids, n, E, chunk, ws);
   hipLaunchKernelGGL(sort_rank_kernel, grid, dim3(kSortThreads), 0, s, ids, n, E, chunk, ws, offsets, row_of, slot_of);
   if (X && H > 0) {
     const int segs = (int)((H + 511) / 512);
-    hipLaunchKernelGGL(gather_kernel, dim3((unsigned)((T * segs + 3) / 4)), dim3(256), 0, s, row_of, T, k, H, ldx, segs, X, Xg);
+    const dim3 rows((unsigned)((T * segs + 3) / 4)), b(256);
+    if (rows_past_cache(n, H)) hipLaunchKernelGGL(gather_kernel<true>, rows, b, 0, s, row_of, T, k, H, ldx, segs, X, Xg);
+    else hipLaunchKernelGGL(gather_kernel<false>, rows, b, 0, s, row_of, T, k, H, ldx, segs, X, Xg);
   }
   return hipGetLastError();
 }
@@ -587,12 +758,11 @@ hipError_t launch_moe_combine(const int32_t* row_of, const float* w, int64_t T, 
 hipError_t launch_moe_combine_bwd(const int32_t* row_of, const float* w, int64_t T, int k, int64_t H,
                                   const uint16_t* dY, int64_t lddy, const uint16_t* Yg,
                                   uint16_t* dYg, float* dw, hipStream_t s) {
-  const dim3 grid((unsigned)T), b(256);
   switch (rows_at_once(k)) {
-    case 1: hipLaunchKernelGGL((combine_bwd_kernel<1, 4>), grid, b, 0, s, row_of, w, T, k, H, dY, lddy, Yg, dYg, dw); break;
-    case 2: hipLaunchKernelGGL((combine_bwd_kernel<2, 4>), grid, b, 0, s, row_of, w, T, k, H, dY, lddy, Yg, dYg, dw); break;
-    case 4: hipLaunchKernelGGL((combine_bwd_kernel<4, 4>), grid, b, 0, s, row_of, w, T, k, H, dY, lddy, Yg, dYg, dw); break;
-    default: hipLaunchKernelGGL((combine_bwd_kernel<8, 4>), grid, b, 0, s, row_of, w, T, k, H, dY, lddy, Yg, dYg, dw);
+    case 1: launch_combine_bwd<1>(row_of, w, T, k, H, dY, lddy, Yg, dYg, dw, s); break;
+    case 2: launch_combine_bwd<2>(row_of, w, T, k, H, dY, lddy, Yg, dYg, dw, s); break;
+    case 4: launch_combine_bwd<4>(row_of, w, T, k, H, dY, lddy, Yg, dYg, dw, s); break;
+    default: launch_combine_bwd<8>(row_of, w, T, k, H, dY, lddy, Yg, dYg, dw, s);
   }
   return hipGetLastError();
 }
