@@ -433,8 +433,8 @@ hipError_t launch_packed_matvec(const PackedOperand& w, const int64_t* off, int6
   int64_t least = INT64_MAX;
   for (int t = 1; t <= 2; ++t) {
     const int64_t unit = t * codes + a.xmax * 1024, blocks = (w.N + 16 * t - 1) / (16 * t) * busy;
-    for (int64_t each = (slices + kMaxWaves - 1) / kMaxWaves; each <= slices; ++each) {
-      const int64_t waves = (slices + each - 1) / each;
+    for (int64_t most = std::min<int64_t>(kMaxWaves, slices); most > 0; --most) {
+      const int64_t each = (slices + most - 1) / most, waves = (slices + each - 1) / each;
       if (waves * unit > kLdsBytes) continue;
       const int64_t resident = cus * std::min(kLdsBytes / (waves * unit), 32 / waves);
       const int64_t cost = (blocks + resident - 1) / resident * (each + 1) * unit;
@@ -448,7 +448,8 @@ hipError_t launch_packed_matvec(const PackedOperand& w, const int64_t* off, int6
   // Codes that are read once, and are many, past the caches (24576 x 4096 NVFP4, one row, 14.9 -> 14.4
   // us; 12288-deep MXFP4 9.9 -> 9.5); small weights may still be there from before, and further row
   // groups read them again (4096 x 4096: 16 rows 6.8 -> 7.0 us, 64 rows 13.5 -> 14.6).
-  int copy = (off != nullptr || items == 1) && busy * w.N * w.K >= (int64_t)1 << 25 ? kCopyNt : kCopy;
+  const bool many = (double)busy * (double)w.N * (double)w.K >= (double)(1 << 25);
+  const int copy = (off != nullptr || items == 1) && many ? kCopyNt : kCopy;
   switch (w.fmt) {
     case QF_FMT_NVFP4: return launch_fmt<QF_FMT_NVFP4>(a, nt, w.K % 32 ? kCopyWords : copy, s);
     case QF_FMT_MXFP4: return launch_fmt<QF_FMT_MXFP4>(a, nt, copy, s);
