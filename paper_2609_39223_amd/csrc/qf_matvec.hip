@@ -8,7 +8,7 @@
 // unit wait for 4 to 5 KB of codes each.  Copies are contiguous (256 bytes of four rows per
 // instruction) where loads in the shape of the matrix operand, 16 bytes of 16 rows, kept the L1's
 // address port busy four times as long (24576 x 4096 NVFP4 times one row: 18.2 us with such loads,
-// 14.3 with copies).  A 16-byte chunk c of row r lies at c ^ r of its row in LDS, so the operand
+// 14.3 with copies, the decode as it was).  A 16-byte chunk c of row r lies at c ^ r of its row in LDS, so the operand
 // reads, the same chunk of 16 rows, fall on different banks.
 //
 // On v_mfma_f32_16x16x32_bf16 X is the A operand (lane: row lane % 16, k 8 (lane / 16) + 0..7) and W
@@ -21,8 +21,10 @@
 //   Q4_K   a sub-block of 32 is one MFMA deep.  16 + q is exact in bf16 and made from a code by a shift
 //          and a mask; with X1 = -16 sum x from one MFMA as the next one's addend, P = sum (16 + q) x
 //          + X1 = sum q x, and a super-block adds d sum s6 P + (dmin / 16) sum m6 X1.
-// Bound by reading the weight once: 0.53 to 0.56 bytes an element (NVFP4, 24576 x 4096, one row: 56.7
-// MB in 14.3 us = 4.0 TB/s).  Small weights are bound by the launch and one trip to memory (4096 x 4096: 5.0 us).
+// Bound by reading the weight once, 0.53 to 0.56 bytes an element (NVFP4, 24576 x 4096, one row: 56.7
+// MB in 12.1 us = 4.7 TB/s; the copies alone take 11.2), Q4_K by its decode (14336 x 4096, five rows:
+// 13.2 us, 9.9 without the arithmetic).  Small weights are bound by the launch and one trip to memory
+// (4096 x 4096: 4.7 us).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -62,6 +64,14 @@ __device__ __forceinline__ void copy4(const void* g, void* l) {
 #if defined(__HIP_DEVICE_COMPILE__)
   __builtin_amdgcn_global_load_lds(QF_GLOBAL(const_cast<void*>(g)), QF_LDS(l), 4, 0, 0);
 #endif
+}
+
+// v_mfma_f32_4x4x4_16b_bf16: sixteen products of 4 x 4 x 4, block b = lane / 4.  A: row lane % 4, four k;
+// B: column lane % 4, four k; C: column lane % 4, the four rows.
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ f32x4_t mfma4(uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1, f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_4x4x4bf16_1k(__builtin_bit_cast(s16x4_t, make_uint2(a0, a1)),
+                                                __builtin_bit_cast(s16x4_t, make_uint2(b0, b1)), c, 0, 0, 0);
 }
 
 struct MatvecArgs {
@@ -207,6 +217,28 @@ __device__ __forceinline__ void multiply32(const uint4& c, uint32_t s, const uin
   }
 }
 
+// The same for NVFP4 and at most four rows of X, on 4 x 4 x 4 blocks: a lane's columns are its own, so
+// the sixteen products of a scale block come out by themselves and the scale goes onto their sum, one
+// multiplication a row instead of one a weight (2.06 vector operations a weight -> 0.6 to 0.8; 24576 x
+// 4096, one row: 14.2 -> 12.1 us).
+__device__ __forceinline__ void multiply32_small(const uint4& c, uint32_t s, const uint4 x[4], f32x4_t& acc) {
+  const uint32_t cw[4] = {c.x, c.y, c.z, c.w};
+  const auto sf = __builtin_amdgcn_cvt_pk_f32_fp8((int)s, false);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    f32x4_t p = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 2 * h; i < 2 * h + 2; ++i) {
+      uint32_t w[4];
+      codec::fp4_decode8(cw[i], 1.0f, w);
+      p = mfma4(x[i].x, x[i].y, w[0], w[1], p);
+      p = mfma4(x[i].z, x[i].w, w[2], w[3], p);
+    }
+#pragma unroll
+    for (int m = 0; m < 4; ++m) acc[m] = __builtin_fmaf(sf[h], p[m], acc[m]);
+  }
+}
+
 // Two bf16 values 16 + q of the codes in the low (HIGH: high) nibbles of bytes P and P + 2 of w.
 template <int P, bool HIGH>
 __device__ __forceinline__ uint32_t q4k_pair(uint32_t w) {
@@ -256,7 +288,9 @@ constexpr int kMaxWaves = 8;
 constexpr int kMaxRows = 16;
 constexpr int64_t kLdsBytes = 160 * 1024;
 
-template <int FMT, int NT, int COPY>
+// SMALL: xmax <= 4 and NVFP4 (multiply32_small); A operand rows are then lane % 4, and the four lane
+// groups hold partial sums of their own k.
+template <int FMT, int NT, int COPY, bool SMALL>
 __global__ __launch_bounds__(64 * kMaxWaves) void matvec_kernel(MatvecArgs p) {
   extern __shared__ __align__(256) char smem[];
   constexpr int CB = kCodeBytes<FMT>;
@@ -274,17 +308,19 @@ __global__ __launch_bounds__(64 * kMaxWaves) void matvec_kernel(MatvecArgs p) {
   const int xlo = xrow < 0 ? 0 : (int)xrow;
   char* const mine = smem + wv * (NT * CB + p.xmax * 1024);
   char* const xs = mine + NT * CB;
-  const int mr = l16 < xn ? l16 : xn - 1;         // rows past the last repeat it and are not stored
+  const int am = SMALL ? lane & 3 : l16;          // A operand row
+  const int mr = am < xn ? am : xn - 1;           // rows past the last repeat it and are not stored
   const char* const xl = xs + mr * 1024;
   const int64_t pitch = FMT == QF_FMT_Q4K ? (int64_t)(K / 256) * 144 : K / 2;
   const int64_t spitch = FMT == QF_FMT_NVFP4 ? K / 16 : K / 32;
   const uint8_t* const codes = p.w.codes + ((int64_t)e * N + n0) * pitch;
   const int last = N - 1 - n0;                    // weight rows past N repeat the last, not stored
+  const uint8_t* const scales = p.w.scales + ((int64_t)e * N + n0) * spitch;
   const uint8_t* sp[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int row = 16 * t + l16;
-    sp[t] = p.w.scales + ((int64_t)e * N + n0 + (row < last ? row : last)) * spitch;
+    sp[t] = scales + (row < last ? row : last) * spitch;
   }
   f32x4_t acc[NT];
 #pragma unroll
@@ -303,8 +339,10 @@ __global__ __launch_bounds__(64 * kMaxWaves) void matvec_kernel(MatvecArgs p) {
       const int rest = last - 16 * t;             // (below zero: the tile is past N, its rows the last one)
       copy_codes<FMT, COPY>(codes + (int64_t)(rest < 0 ? last : 16 * t) * pitch, pitch, rest < 0 ? 0 : rest, sl,
                             half, mine + t * CB);
-      s[t] = load_scales<FMT>(sp[t] + g * (FMT == QF_FMT_NVFP4 ? 8 : 4), sl);
     }
+    asm volatile("" ::: "memory");                // the codes first: they are what takes long
+#pragma unroll
+    for (int t = 0; t < NT; ++t) s[t] = load_scales<FMT>(sp[t] + g * (FMT == QF_FMT_NVFP4 ? 8 : 4), sl);
     __builtin_amdgcn_s_waitcnt(0x0F70);           // vmcnt(0): this wave's copies are in its region
     asm volatile("" ::: "memory");
     if constexpr (FMT == QF_FMT_Q4K) {
@@ -319,12 +357,15 @@ __global__ __launch_bounds__(64 * kMaxWaves) void matvec_kernel(MatvecArgs p) {
       for (int q = 0; q < 4; ++q) {
         uint4 x[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const uint4*>(xl + 16 * ((16 * g + 4 * q + i) ^ mr));
+        for (int i = 0; i < 4; ++i)               // (rows 0 .. 3 exchange chunks of four: one address for all q)
+          x[i] = *reinterpret_cast<const uint4*>(SMALL ? xl + 256 * g + 16 * (i ^ mr) + 64 * q
+                                                       : xl + 16 * ((16 * g + 4 * q + i) ^ mr));
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           const uint4 c = *reinterpret_cast<const uint4*>(mine + t * CB + l16 * 256 + 16 * ((4 * g + q) ^ l16));
           const uint32_t sv = FMT == QF_FMT_NVFP4 ? (q < 2 ? s[t].x : s[t].y) >> (16 * (q & 1)) : s[t].x >> (8 * q);
-          multiply32<FMT>(c, sv, x, acc[t]);
+          if constexpr (SMALL) multiply32_small(c, sv, x, acc[t]);
+          else multiply32<FMT>(c, sv, x, acc[t]);
         }
       }
     }
@@ -333,7 +374,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void matvec_kernel(MatvecArgs p) {
   if constexpr (FMT != QF_FMT_Q4K) {
     // the k past the last whole slice, 128 at a time by the waves whose turn it is, 16 at a time per
     // lane and straight from memory: nothing past K is read
-    const uint16_t* const xp = p.X + (int64_t)xlo * p.ldx;
+    const uint16_t* const xp = p.X + (int64_t)__shfl(xlo, mr, 64) * p.ldx;
     for (int k1 = whole * 512, turn = whole % p.waves; k1 < K; k1 += 128, turn = turn + 1 == p.waves ? 0 : turn + 1) {
       if (turn != wv) continue;
       const int k = k1 + 32 * g;
@@ -341,7 +382,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void matvec_kernel(MatvecArgs p) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         x[i] = make_uint4(0, 0, 0, 0);
-        if (xrow >= 0 && k + 8 * i < K) x[i] = *reinterpret_cast<const uint4*>(xp + k + 8 * i);
+        if (k + 8 * i < K) x[i] = *reinterpret_cast<const uint4*>(xp + k + 8 * i);
       }
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
@@ -361,7 +402,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void matvec_kernel(MatvecArgs p) {
           c.w = v.y;
           if (FMT == QF_FMT_NVFP4) s |= (uint32_t)sp[t][k / 16 + 1] << 8;
         }
-        multiply32<FMT>(c, s, x, acc[t]);
+        if constexpr (SMALL) multiply32_small(c, s, x, acc[t]);
+        else multiply32<FMT>(c, s, x, acc[t]);
       }
     }
   }
@@ -374,13 +416,18 @@ __global__ __launch_bounds__(64 * kMaxWaves) void matvec_kernel(MatvecArgs p) {
     for (int i = 0; i < 4; ++i) red[(wv * NT + t) * 256 + i * 64 + lane] = acc[t][i];
   __syncthreads();
   const float S = FMT == QF_FMT_NVFP4 ? p.w.S[e] : 1.0f;
-  for (int o = tid; o < NT * 256; o += p.waves * 64) {
-    const int ln = o & 63, i = (o >> 6) & 3, t = o >> 8;
-    const int64_t r = r0 + 4 * (ln >> 4) + i;
+  for (int o = tid; o < NT * (SMALL ? 64 : 256); o += p.waves * 64) {
+    // SMALL: (tile, row, column), else (tile, row % 4, row / 4, column)
+    const int ln = SMALL ? o & 15 : o & 63, i = (SMALL ? o >> 4 : o >> 6) & 3, t = SMALL ? o >> 6 : o >> 8;
+    const int64_t r = r0 + (SMALL ? i : 4 * (ln >> 4) + i);
     const int n = n0 + 16 * t + (ln & 15);
     if (r >= r1 || n >= N) continue;
+    const float* const part = red + t * 256 + i * 64 + ln;
     float v = 0.0f;
-    for (int w = 0; w < p.waves; ++w) v += red[w * NT * 256 + o];
+    for (int w = 0; w < p.waves; ++w) {
+      v += part[w * NT * 256];
+      if (SMALL) v += (part[w * NT * 256 + 16] + part[w * NT * 256 + 32]) + part[w * NT * 256 + 48];
+    }
     if (FMT == QF_FMT_NVFP4) v *= S;
     if (x_row(p, r) < 0) v = 0.0f;
     if (p.y_f32) static_cast<float*>(p.Y)[r * p.ldy + n] = v;
@@ -393,14 +440,18 @@ hipError_t launch_tiles(const MatvecArgs& a, hipStream_t s) {
   const int64_t blocks = (a.w.N + 16 * NT - 1) / (16 * NT) * a.items;
   if (blocks > INT32_MAX) return hipErrorInvalidValue;
   const size_t lds = (size_t)a.waves * (NT * kCodeBytes<FMT> + a.xmax * 1024);
-  hipLaunchKernelGGL((matvec_kernel<FMT, NT, COPY>), dim3((unsigned)blocks), dim3(64 * a.waves), lds, s, a);
+  const dim3 grid((unsigned)blocks), b(64 * a.waves);
+  if (FMT == QF_FMT_NVFP4 && a.xmax <= 4)
+    hipLaunchKernelGGL((matvec_kernel<FMT, NT, COPY, FMT == QF_FMT_NVFP4>), grid, b, lds, s, a);
+  else
+    hipLaunchKernelGGL((matvec_kernel<FMT, NT, COPY, false>), grid, b, lds, s, a);
   return hipGetLastError();
 }
 
 template <int FMT>
 hipError_t launch_fmt(const MatvecArgs& a, int nt, int copy, hipStream_t s) {
-  if (FMT == QF_FMT_NVFP4 && copy == kCopyWords)
-    return nt == 1 ? launch_tiles<QF_FMT_NVFP4, 1, kCopyWords>(a, s) : launch_tiles<QF_FMT_NVFP4, 2, kCopyWords>(a, s);
+  if constexpr (FMT == QF_FMT_NVFP4)
+    if (copy == kCopyWords) return nt == 1 ? launch_tiles<FMT, 1, kCopyWords>(a, s) : launch_tiles<FMT, 2, kCopyWords>(a, s);
   if (copy == kCopyNt) return nt == 1 ? launch_tiles<FMT, 1, kCopyNt>(a, s) : launch_tiles<FMT, 2, kCopyNt>(a, s);
   return nt == 1 ? launch_tiles<FMT, 1, kCopy>(a, s) : launch_tiles<FMT, 2, kCopy>(a, s);
 }
@@ -411,6 +462,7 @@ hipError_t launch_packed_matvec(const PackedOperand& w, const int64_t* off, int6
                                 const int32_t* rows, int64_t rows_div, int64_t M, const uint16_t* X,
                                 int64_t ldx, void* Y, int64_t ldy, int y_f32, hipStream_t s) {
   MatvecArgs a{w, X, ldx, M, Y, ldy, R, y_f32, off, rows, (int)rows_div, 0, 0, 0};
+
   if (M == 0) a.w.K = 0;                         // no X at all: zeros
   // Rows a workgroup takes.  Experts: more than the mean, since LDS for rows that most experts do not
   // have costs waves, and an expert with more rows is read again from the last-level cache (3072 x
@@ -421,24 +473,25 @@ hipError_t launch_packed_matvec(const PackedOperand& w, const int64_t* off, int6
   // row groups: of a dense call ceil(R / xmax); of E experts at most one more each
   const int64_t items = off ? std::min(w.E, R) + R / a.xmax : (R + a.xmax - 1) / a.xmax;
   a.items = (int)items;                          // (R < 2^30)
-  // Tile height and waves a tile: the least of rounds of resident workgroups x (slices a wave takes +
-  // 1 for start and end) x what a slice copies.  Measured against it, us: 24576 x 4096 NVFP4, 1 row, 8
-  // / 4 / 2 waves 15.4 / 14.8 / 15.4; 4096 x 4096 8 / 4 / 2 waves 5.1 / 5.8 / 7.4; 24576 x 4096, 16
-  // rows, one tile 4 waves / two tiles 4 / 2 waves 24.3 / 28.3 / 21.2; 64 rows x 4096 x 4096 MXFP4, 8 /
-  // 4 / 2 waves 15.9 / 12.9 / 11.4.
+  // Tile height and waves a tile: the least of rounds of resident workgroups (whole ones up to four,
+  // then as they overlap) x (slices a wave takes + 1 for start and end) x what a slice copies.
+  // Measured against it, us: 24576 x 4096 NVFP4, 1 row, 8 / 4 / 2 waves 15.4 / 14.8 / 15.4; 4096 x 4096 8
+  // / 4 / 2 waves 5.1 / 5.8 / 7.4; 24576 x 4096, 16 rows, one tile 4 waves / two tiles 4 / 2 waves 24.3 /
+  // 28.3 / 21.2; 64 rows x 4096 x 4096 MXFP4, 8 / 4 / 2 waves 15.9 / 12.9 / 11.4.
   const int64_t busy = off ? std::min(w.E, R) : items;       // row groups that are likely there
   const int64_t slices = std::max<int64_t>(1, (a.w.K + 511) / 512), cus = compute_units();
   const int64_t codes = w.fmt == QF_FMT_Q4K ? kCodeBytes<QF_FMT_Q4K> : kCodeBytes<QF_FMT_NVFP4>;
   int nt = 1;
-  int64_t least = INT64_MAX;
+  double least = 0;
   for (int t = 1; t <= 2; ++t) {
     const int64_t unit = t * codes + a.xmax * 1024, blocks = (w.N + 16 * t - 1) / (16 * t) * busy;
     for (int64_t most = std::min<int64_t>(kMaxWaves, slices); most > 0; --most) {
       const int64_t each = (slices + most - 1) / most, waves = (slices + each - 1) / each;
       if (waves * unit > kLdsBytes) continue;
       const int64_t resident = cus * std::min(kLdsBytes / (waves * unit), 32 / waves);
-      const int64_t cost = (blocks + resident - 1) / resident * (each + 1) * unit;
-      if (cost < least) {
+      const double rounds = blocks > 4 * resident ? (double)blocks / resident : (double)((blocks + resident - 1) / resident);
+      const double cost = rounds * (each + 1) * unit;
+      if (least == 0 || cost < least) {
         least = cost;
         nt = t;
         a.waves = (int)waves;
