@@ -622,7 +622,7 @@ QF_API qf_status qf_payload_write_header(int fmt, int64_t N, int64_t K, void* pa
  * "Mixture-of-experts adaptation"; the router itself stays unquantized).  With T tokens, E experts
  * and k choices a token, slot (t, j) is choice j of token t, flat index t k + j; "grouped" rows are
  * the slots sorted by expert, the order of the grouped layer above.
- * Limits: E <= 1024, 1 <= k <= min(E, 64), T k < 2^31.
+ * Limits: E <= 1024, 1 <= k <= min(E, 64), T < 2^24; with rows of H columns T ceil(H / 512) <= 2^26 - 4.
  * ------------------------------------------------------------------------------------ */
 typedef enum { QF_SCORE_SOFTMAX = 0, QF_SCORE_SIGMOID = 1 } qf_score;
 

@@ -1672,7 +1672,14 @@ qf_status check_moe(const char* fn, int64_t T, int64_t E, int64_t k) {
   if (E > 1024) return fail(QF_ENOTSUP, "%s: more than 1024 experts", fn);
   if (k < 1 || k > E) return fail(QF_ESHAPE, "%s: %lld choices among %lld experts", fn, (long long)k, (long long)E);
   if (k > 64) return fail(QF_ENOTSUP, "%s: more than 64 choices a token", fn);
-  if (T > INT32_MAX / k) return fail(QF_ENOTSUP, "%s: 2^31 slots or more", fn);
+  if (T >= 1 << 24) return fail(QF_ENOTSUP, "%s: 2^24 tokens or more", fn);   // (so T k < 2^30)
+  return QF_OK;
+}
+
+// A wave takes 512 columns of a token, and a launch has fewer than 2^32 lanes.
+qf_status check_columns(const char* fn, int64_t T, int64_t H) {
+  if (T > 0 && H > 0 && (H - 1) / 512 >= ((1 << 26) - 4) / T)
+    return fail(QF_ENOTSUP, "%s: %lld tokens of %lld columns are too many", fn, (long long)T, (long long)H);
   return QF_OK;
 }
 
@@ -1680,6 +1687,7 @@ qf_status check_moe(const char* fn, int64_t T, int64_t E, int64_t k) {
 qf_status check_rows(const char* fn, int64_t T, int64_t k, int64_t H, const int32_t* row_of) {
   if (H < 0) return fail(QF_ESHAPE, "%s: negative shape", fn);
   QF_TRY(check_moe(fn, T, 1024, k));
+  QF_TRY(check_columns(fn, T, H));
   if (T > 0 && !row_of) return fail(QF_EINVAL, "%s: null row_of", fn);
   return check_out("row_of", row_of);
 }
@@ -1749,6 +1757,7 @@ qf_status qf_moe_dispatch(const int32_t* ids, int64_t T, int64_t E, int64_t k, i
   QF_TRY(check_out("qf_moe_dispatch: slot_of", slot_of));
   if ((X == nullptr) != (Xg == nullptr) && T > 0) return fail(QF_EINVAL, "%s: X and Xg go together", fn);
   if (X) {
+    QF_TRY(check_columns(fn, T, H));
     QF_TRY(check_mat("qf_moe_dispatch: X", X, T, H, ldx, true));
     QF_TRY(check_mat("qf_moe_dispatch: Xg", Xg, T * k, H, H, true));
   }

@@ -4,12 +4,12 @@
 // A workgroup takes 16 NT weight rows against up to 16 rows of X, its waves take slices of 512 k in
 // turn, and their FP32 partial sums meet in LDS in wave order.  A slice's codes and X rows go straight
 // from memory to LDS, each wave into a region of its own, so nothing but the final sum waits for
-// another wave, and no registers are held while the copies are under way: up to 32 waves a compute
-// unit wait for 4 to 5 KB of codes each.  Copies are contiguous (256 bytes of four rows per
-// instruction) where loads in the shape of the matrix operand, 16 bytes of 16 rows, kept the L1's
-// address port busy four times as long (24576 x 4096 NVFP4 times one row: 18.2 us with such loads,
-// 14.3 with copies, the decode as it was).  A 16-byte chunk c of row r lies at c ^ r of its row in LDS, so the operand
-// reads, the same chunk of 16 rows, fall on different banks.
+// another wave, and no registers are held while the copies are under way: the 16 to 24 waves that a
+// compute unit's registers hold wait for 4 to 5 KB of codes each.  Copies are contiguous (256 bytes of
+// four rows per instruction) where loads in the shape of the matrix operand, 16 bytes of 16 rows, kept
+// the L1's address port busy four times as long (24576 x 4096 NVFP4 times one row: 18.2 us with such
+// loads, 14.3 with copies, the decode as it was).  A 16-byte chunk c of row r lies at c ^ r of its row
+// in LDS, so the operand reads, the same chunk of 16 rows, fall on different banks.
 //
 // On v_mfma_f32_16x16x32_bf16 X is the A operand (lane: row lane % 16, k 8 (lane / 16) + 0..7) and W
 // the B operand (lane: weight row lane % 16, the same k); any bijection of k is fine as long as both
@@ -100,7 +100,7 @@ __device__ __forceinline__ int64_t x_row(const MatvecArgs& p, int64_t r) {
 // Work item `item` of a grouped call: expert e and its rows [r0, r1), at most `chunk`; items count
 // the experts' chunks in order.  Every wave finds it by itself: lane l sums the chunks of its experts
 // (offsets cut to 0 .. R < 2^30), a prefix sum over the lanes finds whose the item is.  False past
-// the last one.
+// the last one; [r0, r1) lies in 0 .. R and is not empty whatever the offsets are.
 __device__ __forceinline__ bool find_item(const int64_t* off, int E, int64_t R, int item, int chunk,
                                           int& e, int64_t& r0, int64_t& r1) {
   const int lane = threadIdx.x & 63, per = (E + 63) / 64, e0 = lane * per;
@@ -143,7 +143,7 @@ __device__ __forceinline__ bool find_item(const int64_t* off, int E, int64_t R, 
   e = __builtin_amdgcn_readlane(e0 + i, owner);
   r0 = __builtin_amdgcn_readlane(lo, owner);
   r1 = __builtin_amdgcn_readlane(min(lo + chunk, o1), owner);
-  return true;
+  return r0 >= 0 && r0 < r1;                      // (offsets that fall can overflow the sums)
 }
 
 // ------------------------------------------------------------------------------- the formats
@@ -435,7 +435,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void matvec_kernel(MatvecArgs p) {
 template <int FMT, int NT, int COPY>
 hipError_t launch_tiles(const MatvecArgs& a, hipStream_t s) {
   const int64_t blocks = (a.w.N + 16 * NT - 1) / (16 * NT) * a.items;
-  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  if (blocks > UINT32_MAX / (64 * a.waves)) return hipErrorInvalidConfiguration;
   const size_t lds = (size_t)a.waves * (NT * kCodeBytes<FMT> + a.xmax * 1024);
   const dim3 grid((unsigned)blocks), b(64 * a.waves);
   if (FMT == QF_FMT_NVFP4 && a.xmax <= 4)

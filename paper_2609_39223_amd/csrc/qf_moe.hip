@@ -238,7 +238,7 @@ template <class Z, int L, int C>
 __global__ __launch_bounds__(kRouteThreads) void route_bwd_kernel(
     const Z* __restrict__ z, int64_t T, int E, int64_t ldz, int k, int score, int norm, float scale,
     const int32_t* __restrict__ ids, const float* __restrict__ dw, Z* __restrict__ dz, int64_t lddz) {
-  __shared__ float rows[kRouteThreads / L][8 * C * L];
+  __shared__ __align__(16) float rows[kRouteThreads / L][8 * C * L];
   const int lane = threadIdx.x % L;
   const int64_t t = (int64_t)blockIdx.x * (kRouteThreads / L) + threadIdx.x / L;
   float* const row = rows[threadIdx.x / L];
@@ -520,7 +520,7 @@ __device__ __forceinline__ void store_row(uint16_t* p, uint4 q) {
 bool rows_past_cache(int64_t n, int64_t H) { return n * H * 2 > (int64_t)128 << 20; }
 
 // Xg[row] = X[t] for the rows of token t's slots, zeros for dropped ones: a wave copies 512 columns.
-// Bound by writing the rows: 32768 tokens x 8 x 3072 377 us = 4.8 TB/s.
+// Bound by writing the rows: 32768 tokens x 8 x 3072 378 us = 4.8 TB/s.
 template <bool NT>
 __global__ __launch_bounds__(256) void gather_kernel(const int32_t* __restrict__ row_of, int64_t T,
                                                      int k, int64_t H, int64_t ldx, int segs,
@@ -563,7 +563,7 @@ struct Slots {
 
 // Y[t] = sum over j of w_j Yg[row_j]: a wave takes 512 columns of a token and has KB rows' loads in
 // flight (a slot without a row loads row 0 and leaves it: no branch between the loads).  Bound by
-// reading the rows: 32768 tokens x 8 x 3072 328 us = 5.5 TB/s.
+// reading the rows: 32768 tokens x 8 x 3072 312 us = 5.8 TB/s.
 template <int KB>
 __global__ __launch_bounds__(256) void combine_kernel(const int32_t* __restrict__ row_of,
                                                       const float* __restrict__ w, int64_t T, int k,
@@ -595,7 +595,7 @@ __global__ __launch_bounds__(256) void combine_kernel(const int32_t* __restrict_
 
 // dYg[row_j] = w_j dY[t] and dw_j = <dY[t], Yg[row_j]>: a workgroup of W waves takes a token, wave w
 // the 512-column pieces w, w + W, ..., KB rows at a time; dw's partial sums meet in LDS in wave
-// order.  Bound by the rows read and written: 32768 tokens x 8 x 3072 650 us = 5.3 TB/s.
+// order.  Bound by the rows read and written: 32768 tokens x 8 x 3072 682 us = 5.0 TB/s.
 template <int KB, int W, bool NT>
 __global__ __launch_bounds__(64 * W) void combine_bwd_kernel(
     const int32_t* __restrict__ row_of, const float* __restrict__ w, int64_t T, int k, int64_t H,

@@ -114,3 +114,19 @@ def test_packed_products(L):
     assert grouped(E=1025) == QF_ENOTSUP and grouped(R=-1) == QF_ESHAPE and grouped(M=-1) == QF_ESHAPE
     assert grouped(fmt=1) == QF_EINVAL                            # no tensor scales
     assert grouped(R=1 << 30) == QF_ENOTSUP
+
+
+def test_launch_limits(L):
+    """Fewer than 2^24 tokens, and fewer than 2^26 pieces of 512 columns, whatever k is."""
+    assert L.qf_moe_route(A, 0, I(1 << 24), I(16), I(16), I(1), 0, 1, F(1), None, B, C, None) == QF_ENOTSUP
+    assert b"2^24 tokens" in L.qf_last_error()
+    T, H = 1 << 22, 16 * 512                                      # 2^26 pieces
+    assert L.qf_moe_combine(A, B, I(T), I(1), I(H), C, D, I(H), None) == QF_ENOTSUP
+    assert b"too many" in L.qf_last_error()
+    assert L.qf_moe_dispatch_bwd(A, I(T), I(1), I(H), C, D, I(H), None) == QF_ENOTSUP
+    assert L.qf_moe_combine_bwd(A, B, I(T), I(1), I(H), C, I(H), D, A, B, None) == QF_ENOTSUP
+    assert L.qf_moe_dispatch(A, I(T), I(16), I(1), B, C, D, A, I(H), I(H), B, P(4096),
+                             ctypes.c_size_t(1 << 30), None) == QF_ENOTSUP
+    assert L.qf_moe_combine(A, B, I(T - 1), I(1), I(1 << 60), C, D, I(1 << 60), None) == QF_ENOTSUP
+    # one piece fewer passes this check (and fails the next one)
+    assert L.qf_moe_combine(A, B, I(T - 1), I(1), I(H), None, D, I(H), None) == QF_EINVAL
