@@ -86,6 +86,7 @@ struct MatvecArgs {
   const int32_t* rows;
   int rows_div;
   int xmax;               // rows of X a workgroup takes at most (1 .. 16)
+  int xrows;              // rows of X that lie in LDS at once: xmax, or 8 of 16
   int waves;              // waves that share a tile's slices
   int items;              // row groups the grid holds
 };
@@ -285,12 +286,17 @@ constexpr int kMaxWaves = 8;
 constexpr int kMaxRows = 16;
 constexpr int64_t kLdsBytes = 160 * 1024;
 
-// SMALL: xmax <= 4 and NVFP4 (multiply32_small); A operand rows are then lane % 4, and the four lane
-// groups hold partial sums of their own k.
-template <int FMT, int NT, int COPY, bool SMALL>
+// Rows of X.  kSmall: xmax <= 4 and NVFP4 (multiply32_small); A operand rows are then lane % 4, and the
+// four lane groups hold partial sums of their own k.  kTwice: up to 16 rows through LDS for 8: lanes
+// 0 .. 7 of each 16 take their operands of the whole slice into registers, then the other rows are
+// copied there; codes are copied and decoded once for all 16 where LDS for 16 rows would cost waves.
+// (Twice the registers, 160: a variant of its own.)
+enum Rows { kAll = 0, kSmall = 1, kTwice = 2 };
+template <int FMT, int NT, int COPY, int ROWS>
 __global__ __launch_bounds__(64 * kMaxWaves) void matvec_kernel(MatvecArgs p) {
   extern __shared__ __align__(256) char smem[];
   constexpr int CB = kCodeBytes<FMT>;
+  constexpr bool SMALL = ROWS == kSmall;
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4;
   const int N = (int)p.w.N, K = (int)p.w.K;
@@ -303,7 +309,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void matvec_kernel(MatvecArgs p) {
   // lane l16 knows X row l16 of the group; a row that does not exist reads row 0, and zeros are stored
   const int64_t xrow = l16 < xn ? x_row(p, r0 + l16) : -1;
   const int xlo = xrow < 0 ? 0 : (int)xrow;
-  char* const mine = smem + wv * (NT * CB + p.xmax * 1024);
+  char* const mine = smem + wv * (NT * CB + p.xrows * 1024);
   char* const xs = mine + NT * CB;
   const int am = SMALL ? lane & 3 : l16;          // A operand row
   const int mr = am < xn ? am : xn - 1;           // rows past the last repeat it and are not stored
@@ -327,7 +333,8 @@ __global__ __launch_bounds__(64 * kMaxWaves) void matvec_kernel(MatvecArgs p) {
   for (int sl = wv; sl < whole; sl += p.waves) {
     const bool half = FMT == QF_FMT_Q4K && K - sl * 512 < 512;
     uint2 s[NT];
-    for (int m = 0; m < xn; ++m) {
+    const int first = min(xn, p.xrows);
+    for (int m = 0; m < first; ++m) {
       const int c = lane ^ m;
       copy16(p.X + (int64_t)__builtin_amdgcn_readlane(xlo, m) * p.ldx + sl * 512 + 8 * (half ? c & 31 : c), xs + m * 1024);
     }
@@ -348,6 +355,33 @@ __global__ __launch_bounds__(64 * kMaxWaves) void matvec_kernel(MatvecArgs p) {
         const char* const row = mine + t * CB + l16 * 288;
         q4k_superblock(row, xl, mr, 0, g, acc[t]);
         if (!half) q4k_superblock(row + 144, xl, mr, 32, g, acc[t]);
+      }
+    } else if (ROWS == kTwice && xn > 8) {
+      uint4 x[4][4];
+      const char* const xa = xs + (l16 & 7) * 1024;
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        x[i >> 2][i & 3] = *reinterpret_cast<const uint4*>(xa + 16 * ((16 * g + i) ^ (l16 & 7)));
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      for (int m = 8; m < xn; ++m)
+        copy16(p.X + (int64_t)__builtin_amdgcn_readlane(xlo, m) * p.ldx + sl * 512 + 8 * (lane ^ (m - 8)),
+               xs + (m - 8) * 1024);
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(0x0F70);
+      asm volatile("" ::: "memory");
+      if (l16 >= 8) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)             // (past row xn: what lay there, in rows that are not stored)
+          x[i >> 2][i & 3] = *reinterpret_cast<const uint4*>(xa + 16 * ((16 * g + i) ^ (l16 & 7)));
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const uint4 c = *reinterpret_cast<const uint4*>(mine + t * CB + l16 * 256 + 16 * ((4 * g + q) ^ l16));
+          const uint32_t sv = FMT == QF_FMT_NVFP4 ? (q < 2 ? s[t].x : s[t].y) >> (16 * (q & 1)) : s[t].x >> (8 * q);
+          multiply32<FMT>(c, sv, x[q], acc[t]);
+        }
       }
     } else {
 #pragma unroll
@@ -436,12 +470,14 @@ template <int FMT, int NT, int COPY>
 hipError_t launch_tiles(const MatvecArgs& a, hipStream_t s) {
   const int64_t blocks = (a.w.N + 16 * NT - 1) / (16 * NT) * a.items;
   if (blocks > UINT32_MAX / (64 * a.waves)) return hipErrorInvalidConfiguration;
-  const size_t lds = (size_t)a.waves * (NT * kCodeBytes<FMT> + a.xmax * 1024);
+  const size_t lds = (size_t)a.waves * (NT * kCodeBytes<FMT> + a.xrows * 1024);
   const dim3 grid((unsigned)blocks), b(64 * a.waves);
   if (FMT == QF_FMT_NVFP4 && a.xmax <= 4)
-    hipLaunchKernelGGL((matvec_kernel<FMT, NT, COPY, FMT == QF_FMT_NVFP4>), grid, b, lds, s, a);
+    hipLaunchKernelGGL((matvec_kernel<FMT, NT, COPY, FMT == QF_FMT_NVFP4 ? kSmall : kAll>), grid, b, lds, s, a);
+  else if (FMT != QF_FMT_Q4K && a.xrows < a.xmax)
+    hipLaunchKernelGGL((matvec_kernel<FMT, NT, COPY, FMT != QF_FMT_Q4K ? kTwice : kAll>), grid, b, lds, s, a);
   else
-    hipLaunchKernelGGL((matvec_kernel<FMT, NT, COPY, false>), grid, b, lds, s, a);
+    hipLaunchKernelGGL((matvec_kernel<FMT, NT, COPY, kAll>), grid, b, lds, s, a);
   return hipGetLastError();
 }
 
@@ -458,7 +494,7 @@ hipError_t launch_fmt(const MatvecArgs& a, int nt, int copy, hipStream_t s) {
 hipError_t launch_packed_matvec(const PackedOperand& w, const int64_t* off, int64_t R,
                                 const int32_t* rows, int64_t rows_div, int64_t M, const uint16_t* X,
                                 int64_t ldx, void* Y, int64_t ldy, int y_f32, hipStream_t s) {
-  MatvecArgs a{w, X, ldx, M, Y, ldy, R, y_f32, off, rows, (int)rows_div, 0, 0, 0};
+  MatvecArgs a{w, X, ldx, M, Y, ldy, R, y_f32, off, rows, (int)rows_div, 0, 0, 0, 0};
 
   if (M == 0) a.w.K = 0;                         // no X at all: zeros
   // Rows a workgroup takes.  Experts: more than the mean, since LDS for rows that most experts do not
@@ -466,7 +502,16 @@ hipError_t launch_packed_matvec(const PackedOperand& w, const int64_t* off, int6
   // 3072 NVFP4, 32 tokens to 8 of 128: 4 rows 117 us, 8 rows 111; 2048 x 2048 Q4_K, 16 to 4 of 64: 4
   // rows 33.2, 8 rows 34.7; 3072 x 1536 MXFP4, 64 to 8 of 128: 8 rows 71.8, 16 rows 77.7).
   const int64_t xmax = off == nullptr ? kMaxRows : 2 * R <= 3 * w.E ? 4 : R <= 4 * w.E ? 8 : kMaxRows;
-  a.xmax = (int)std::min(R, xmax);
+  a.xmax = a.xrows = (int)std::min(R, xmax);
+  // 16 through LDS for 8, from 4 rows an expert on, or 2.5 of many experts, whose rows spread wider (us,
+  // 8 or 16 rows / 16 through 8: 3072 x 1536 MXFP4, 64 tokens to 8 of 128 64.6 / 60.4, 44 to 8 52.6 / 51.5, 36
+  // to 8 54.9 / 55.5 with 1536 x 3072; 14336 x 4096 MXFP4, 60 to 2 of 8 109.6 / 104.6, 16 to 2 60.1 / 57.6,
+  // 12 to 2 52.7 / 55.2; 1024 x 2048 NVFP4, 100 to 8 of 256 76.4 / 68.7).  Dense calls gain or lose by
+  // shape (MXFP4, 24576 x 4096, 40 rows 44.6 / 36.0; 4096 x 4096, 64 rows 11.4 / 13.3) and do without.
+  if (off != nullptr && w.fmt != QF_FMT_Q4K && R > 8 && (R >= 4 * w.E || (w.E >= 32 && 2 * R >= 5 * w.E))) {
+    a.xrows = 8;
+    a.xmax = (int)std::min<int64_t>(R, kMaxRows);
+  }
   // row groups: of a dense call ceil(R / xmax); of E experts at most one more each
   const int64_t items = off ? std::min(w.E, R) + R / a.xmax : (R + a.xmax - 1) / a.xmax;
   a.items = (int)items;                          // (R < 2^30)
@@ -481,7 +526,7 @@ hipError_t launch_packed_matvec(const PackedOperand& w, const int64_t* off, int6
   int nt = 1;
   double least = 0;
   for (int t = 1; t <= 2; ++t) {
-    const int64_t unit = t * codes + a.xmax * 1024, blocks = (w.N + 16 * t - 1) / (16 * t) * busy;
+    const int64_t unit = t * codes + a.xrows * 1024, blocks = (w.N + 16 * t - 1) / (16 * t) * busy;
     for (int64_t most = std::min<int64_t>(kMaxWaves, slices); most > 0; --most) {
       const int64_t each = (slices + most - 1) / most, waves = (slices + each - 1) / each;
       if (waves * unit > kLdsBytes) continue;

@@ -200,6 +200,16 @@ def test_grouped(qf, fmt, N, K, counts, f32):
         assert torch.equal(full, same)
 
 
+@pytest.mark.parametrize("fmt,N,K,counts", [
+    ("nvfp4", 48, 1072, [9, 16, 17, 0, 8, 40]), ("mxfp4", 80, 1184, [12, 1, 33, 16, 9, 25]),
+    ("mxfp4", 32, 512, [1] * 20 + [15] * 12), ("nvfp4", 33, 1536, [0] * 30 + [10, 64]),
+    ("nvfp4", 4112, 1024, [10, 11, 30]), ("mxfp4", 8208, 2048, [16, 9, 0, 24])])
+def test_grouped_many_rows(qf, fmt, N, K, counts):
+    """Experts of 9 to 16 rows a group over whole slices, a tail of k, and codes copied in words."""
+    test_grouped(qf, fmt, N, K, counts, False)
+    test_grouped(qf, fmt, N, K, counts, True)
+
+
 def test_grouped_offsets_out_of_range_and_no_x(qf):
     """Offsets that leave 0 .. R are cut to it; no X rows at all: zeros."""
     rng = np.random.default_rng(3)
