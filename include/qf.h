@@ -741,8 +741,8 @@ QF_API qf_status qf_packed_matvec(const qf_packed* w, int64_t M, const uint16_t*
 /*
  * qf_packed_matvec_grouped -- the same per expert: row r of Y in group_offsets[e] .. [e + 1] - 1 is
  * X[x(r)] W_e^T, x(r) = r, or rows[r] / rows_div with `rows` (the slot_of and k of a dispatch: the
- * token's row without a copy in expert order).  Any number of rows; meant for up to some dozens an
- * expert.
+ * token's row without a copy in expert order).  R < 2^30, launched in pieces where one grid does not
+ * hold them; meant for up to some dozens an expert.
  *   group_offsets  DEVICE int64 [E + 1], non-decreasing, within 0 .. R; rows of Y outside
  *                  group_offsets[0] .. [E] are left alone.  E <= 1024.
  *   X bf16 [M, K] (row stride ldx); an x(r) outside 0 .. M - 1 counts as a row of zeros.

@@ -34,6 +34,7 @@
 #include "qf.h"
 #include "qf_codecs.h"
 #include "qf_internal.h"
+#include "qf_matvec_plan.h"
 
 #define QF_LDS(p) ((__attribute__((address_space(3))) void*)(p))
 #define QF_GLOBAL(p) ((__attribute__((address_space(1))) void*)(p))
@@ -88,7 +89,7 @@ struct MatvecArgs {
   int xmax;               // rows of X a workgroup takes at most (1 .. 16)
   int xrows;              // rows of X that lie in LDS at once: xmax, or 8 of 16
   int waves;              // waves that share a tile's slices
-  int items;              // row groups the grid holds
+  int item0;              // experts: the launch's first row group
 };
 
 // The X row of row r of Y, -1 if there is none.
@@ -148,14 +149,10 @@ __device__ __forceinline__ bool find_item(const int64_t* off, int E, int64_t R, 
 }
 
 // ------------------------------------------------------------------------------- the formats
-template <int FMT>
-constexpr int kCodeBytes = FMT == QF_FMT_Q4K ? 5120 : 4096;   // LDS of 16 rows x 512 codes
-
 // Copies of 16 code rows (row i at base + min(i, last) pitch) of slice sl into l, in whole 64-lane
 // instructions; lanes with nothing to fetch fetch something that exists.  FP4: 16 rows of 256 bytes,
 // chunks exchanged as above; rows 8-byte aligned (K = 16 modulo 32) go in words.  Q4_K: two
 // super-blocks a row as they lie (16 rows of 288 bytes: rows 8 banks apart); `half`: only one is left.
-enum Copy { kCopy = 0, kCopyNt = 1, kCopyWords = 2 };
 template <int FMT, int COPY>
 __device__ __forceinline__ void copy_codes(const uint8_t* base, int64_t pitch, int last, int sl,
                                            bool half, char* l) {
@@ -282,20 +279,15 @@ __device__ __forceinline__ void q4k_superblock(const char* row, const char* xl, 
 }
 
 // -------------------------------------------------------------------------------- the kernel
-constexpr int kMaxWaves = 8;
-constexpr int kMaxRows = 16;
-constexpr int64_t kLdsBytes = 160 * 1024;
-
 // Rows of X.  kSmall: xmax <= 4 and NVFP4 (multiply32_small); A operand rows are then lane % 4, and the
 // four lane groups hold partial sums of their own k.  kTwice: up to 16 rows through LDS for 8: lanes
 // 0 .. 7 of each 16 take their operands of the whole slice into registers, then the other rows are
 // copied there; codes are copied and decoded once for all 16 where LDS for 16 rows would cost waves.
 // (Twice the registers, 160: a variant of its own.)
-enum Rows { kAll = 0, kSmall = 1, kTwice = 2 };
 template <int FMT, int NT, int COPY, int ROWS>
-__global__ __launch_bounds__(64 * kMaxWaves) void matvec_kernel(MatvecArgs p) {
+__global__ __launch_bounds__(64 * kMatvecMaxWaves) void matvec_kernel(MatvecArgs p) {
   extern __shared__ __align__(256) char smem[];
-  constexpr int CB = kCodeBytes<FMT>;
+  constexpr int CB = matvec_code_bytes(FMT);
   constexpr bool SMALL = ROWS == kSmall;
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4;
@@ -304,7 +296,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void matvec_kernel(MatvecArgs p) {
   const int item = (int)(blockIdx.x / tiles), n0 = (int)(blockIdx.x % tiles) * 16 * NT;
   int e = 0;
   int64_t r0 = (int64_t)item * p.xmax, r1 = min(r0 + p.xmax, p.R);
-  if (p.off != nullptr && !find_item(p.off, (int)p.w.E, p.R, item, p.xmax, e, r0, r1)) return;
+  if (p.off != nullptr && !find_item(p.off, (int)p.w.E, p.R, p.item0 + item, p.xmax, e, r0, r1)) return;
   const int xn = (int)(r1 - r0);
   // lane l16 knows X row l16 of the group; a row that does not exist reads row 0, and zeros are stored
   const int64_t xrow = l16 < xn ? x_row(p, r0 + l16) : -1;
@@ -466,27 +458,42 @@ __global__ __launch_bounds__(64 * kMaxWaves) void matvec_kernel(MatvecArgs p) {
   }
 }
 
+template <int FMT, int NT, int COPY, int ROWS>
+hipError_t launch_groups(MatvecArgs a, const MatvecPlan& p, hipStream_t s) {
+  const size_t lds = (size_t)p.waves * (NT * matvec_code_bytes(FMT) + p.xrows * 1024);
+  for (int64_t i = 0; i < p.items; i += p.per_launch) {
+    if (a.off) {
+      a.item0 = (int)i;                          // (items < 2^30)
+    } else if (i > 0) {                          // of a dense call the rows that are left
+      const int64_t done = p.per_launch * p.xmax;
+      a.X += done * a.ldx;
+      a.Y = static_cast<char*>(a.Y) + done * a.ldy * (a.y_f32 ? 4 : 2);
+      a.M -= done;
+      a.R -= done;
+    }
+    const dim3 grid((unsigned)(p.tiles * std::min(p.per_launch, p.items - i)));
+    hipLaunchKernelGGL((matvec_kernel<FMT, NT, COPY, ROWS>), grid, dim3(64 * p.waves), lds, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 template <int FMT, int NT, int COPY>
-hipError_t launch_tiles(const MatvecArgs& a, hipStream_t s) {
-  const int64_t blocks = (a.w.N + 16 * NT - 1) / (16 * NT) * a.items;
-  if (blocks > UINT32_MAX / (64 * a.waves)) return hipErrorInvalidConfiguration;
-  const size_t lds = (size_t)a.waves * (NT * kCodeBytes<FMT> + a.xrows * 1024);
-  const dim3 grid((unsigned)blocks), b(64 * a.waves);
-  if (FMT == QF_FMT_NVFP4 && a.xmax <= 4)
-    hipLaunchKernelGGL((matvec_kernel<FMT, NT, COPY, FMT == QF_FMT_NVFP4 ? kSmall : kAll>), grid, b, lds, s, a);
-  else if (FMT != QF_FMT_Q4K && a.xrows < a.xmax)
-    hipLaunchKernelGGL((matvec_kernel<FMT, NT, COPY, FMT != QF_FMT_Q4K ? kTwice : kAll>), grid, b, lds, s, a);
-  else
-    hipLaunchKernelGGL((matvec_kernel<FMT, NT, COPY, kAll>), grid, b, lds, s, a);
-  return hipGetLastError();
+hipError_t launch_rows(const MatvecArgs& a, const MatvecPlan& p, hipStream_t s) {
+  if constexpr (FMT == QF_FMT_NVFP4)
+    if (p.rows == kSmall) return launch_groups<FMT, NT, COPY, kSmall>(a, p, s);
+  if constexpr (FMT != QF_FMT_Q4K)
+    if (p.rows == kTwice) return launch_groups<FMT, NT, COPY, kTwice>(a, p, s);
+  return launch_groups<FMT, NT, COPY, kAll>(a, p, s);
 }
 
 template <int FMT>
-hipError_t launch_fmt(const MatvecArgs& a, int nt, int copy, hipStream_t s) {
+hipError_t launch_fmt(const MatvecArgs& a, const MatvecPlan& p, hipStream_t s) {
   if constexpr (FMT == QF_FMT_NVFP4)
-    if (copy == kCopyWords) return nt == 1 ? launch_tiles<FMT, 1, kCopyWords>(a, s) : launch_tiles<FMT, 2, kCopyWords>(a, s);
-  if (copy == kCopyNt) return nt == 1 ? launch_tiles<FMT, 1, kCopyNt>(a, s) : launch_tiles<FMT, 2, kCopyNt>(a, s);
-  return nt == 1 ? launch_tiles<FMT, 1, kCopy>(a, s) : launch_tiles<FMT, 2, kCopy>(a, s);
+    if (p.copy == kCopyWords) return p.nt == 1 ? launch_rows<FMT, 1, kCopyWords>(a, p, s) : launch_rows<FMT, 2, kCopyWords>(a, p, s);
+  if (p.copy == kCopyNt) return p.nt == 1 ? launch_rows<FMT, 1, kCopyNt>(a, p, s) : launch_rows<FMT, 2, kCopyNt>(a, p, s);
+  return p.nt == 1 ? launch_rows<FMT, 1, kCopy>(a, p, s) : launch_rows<FMT, 2, kCopy>(a, p, s);
 }
 
 }  // namespace
@@ -494,61 +501,14 @@ hipError_t launch_fmt(const MatvecArgs& a, int nt, int copy, hipStream_t s) {
 hipError_t launch_packed_matvec(const PackedOperand& w, const int64_t* off, int64_t R,
                                 const int32_t* rows, int64_t rows_div, int64_t M, const uint16_t* X,
                                 int64_t ldx, void* Y, int64_t ldy, int y_f32, hipStream_t s) {
-  MatvecArgs a{w, X, ldx, M, Y, ldy, R, y_f32, off, rows, (int)rows_div, 0, 0, 0, 0};
-
-  if (M == 0) a.w.K = 0;                         // no X at all: zeros
-  // Rows a workgroup takes.  Experts: more than the mean, since LDS for rows that most experts do not
-  // have costs waves, and an expert with more rows is read again from the last-level cache (3072 x
-  // 3072 NVFP4, 32 tokens to 8 of 128: 4 rows 117 us, 8 rows 111; 2048 x 2048 Q4_K, 16 to 4 of 64: 4
-  // rows 33.2, 8 rows 34.7; 3072 x 1536 MXFP4, 64 to 8 of 128: 8 rows 71.8, 16 rows 77.7).
-  const int64_t xmax = off == nullptr ? kMaxRows : 2 * R <= 3 * w.E ? 4 : R <= 4 * w.E ? 8 : kMaxRows;
-  a.xmax = a.xrows = (int)std::min(R, xmax);
-  // 16 through LDS for 8, from 4 rows an expert on, or 2.5 of many experts, whose rows spread wider (us,
-  // 8 or 16 rows / 16 through 8: 3072 x 1536 MXFP4, 64 tokens to 8 of 128 64.6 / 60.4, 44 to 8 52.6 / 51.5, 36
-  // to 8 54.9 / 55.5 with 1536 x 3072; 14336 x 4096 MXFP4, 60 to 2 of 8 109.6 / 104.6, 16 to 2 60.1 / 57.6,
-  // 12 to 2 52.7 / 55.2; 1024 x 2048 NVFP4, 100 to 8 of 256 76.4 / 68.7).  Dense calls gain or lose by
-  // shape (MXFP4, 24576 x 4096, 40 rows 44.6 / 36.0; 4096 x 4096, 64 rows 11.4 / 13.3) and do without.
-  if (off != nullptr && w.fmt != QF_FMT_Q4K && R > 8 && (R >= 4 * w.E || (w.E >= 32 && 2 * R >= 5 * w.E))) {
-    a.xrows = 8;
-    a.xmax = (int)std::min<int64_t>(R, kMaxRows);
-  }
-  // row groups: of a dense call ceil(R / xmax); of E experts at most one more each
-  const int64_t items = off ? std::min(w.E, R) + R / a.xmax : (R + a.xmax - 1) / a.xmax;
-  a.items = (int)items;                          // (R < 2^30)
-  // Tile height and waves a tile: the least of rounds of resident workgroups (whole ones up to four,
-  // then as they overlap) x (slices a wave takes + 1 for start and end) x what a slice copies.
-  // Measured against it, us: 24576 x 4096 NVFP4, 1 row, 8 / 4 / 2 waves 15.4 / 14.8 / 15.4; 4096 x 4096 8
-  // / 4 / 2 waves 5.1 / 5.8 / 7.4; 24576 x 4096, 16 rows, one tile 4 waves / two tiles 4 / 2 waves 24.3 /
-  // 28.3 / 21.2; 64 rows x 4096 x 4096 MXFP4, 8 / 4 / 2 waves 15.9 / 12.9 / 11.4.
-  const int64_t busy = off ? std::min(w.E, R) : items;       // row groups that are likely there
-  const int64_t slices = std::max<int64_t>(1, (a.w.K + 511) / 512), cus = compute_units();
-  const int64_t codes = w.fmt == QF_FMT_Q4K ? kCodeBytes<QF_FMT_Q4K> : kCodeBytes<QF_FMT_NVFP4>;
-  int nt = 1;
-  double least = 0;
-  for (int t = 1; t <= 2; ++t) {
-    const int64_t unit = t * codes + a.xrows * 1024, blocks = (w.N + 16 * t - 1) / (16 * t) * busy;
-    for (int64_t most = std::min<int64_t>(kMaxWaves, slices); most > 0; --most) {
-      const int64_t each = (slices + most - 1) / most, waves = (slices + each - 1) / each;
-      if (waves * unit > kLdsBytes) continue;
-      const int64_t resident = cus * std::min(kLdsBytes / (waves * unit), 32 / waves);
-      const double rounds = blocks > 4 * resident ? (double)blocks / resident : (double)((blocks + resident - 1) / resident);
-      const double cost = rounds * (each + 1) * unit;
-      if (least == 0 || cost < least) {
-        least = cost;
-        nt = t;
-        a.waves = (int)waves;
-      }
-    }
-  }
-  // Codes that are read once, and are many, past the caches (24576 x 4096 NVFP4, one row, 14.9 -> 14.4
-  // us; 12288-deep MXFP4 9.9 -> 9.5); small weights may still be there from before, and further row
-  // groups read them again (4096 x 4096: 16 rows 6.8 -> 7.0 us, 64 rows 13.5 -> 14.6).
-  const bool many = (double)busy * (double)w.N * (double)w.K >= (double)(1 << 25);
-  const int copy = (off != nullptr || items == 1) && many ? kCopyNt : kCopy;
+  const int64_t K = M == 0 ? 0 : w.K;             // no X at all: zeros
+  const MatvecPlan p = matvec_plan(w.fmt, off != nullptr, w.E, w.N, K, R, compute_units());
+  MatvecArgs a{w, X, ldx, M, Y, ldy, R, y_f32, off, rows, (int)rows_div, p.xmax, p.xrows, p.waves, 0};
+  a.w.K = K;
   switch (w.fmt) {
-    case QF_FMT_NVFP4: return launch_fmt<QF_FMT_NVFP4>(a, nt, w.K % 32 ? kCopyWords : copy, s);
-    case QF_FMT_MXFP4: return launch_fmt<QF_FMT_MXFP4>(a, nt, copy, s);
-    default: return launch_fmt<QF_FMT_Q4K>(a, nt, copy, s);
+    case QF_FMT_NVFP4: return launch_fmt<QF_FMT_NVFP4>(a, p, s);
+    case QF_FMT_MXFP4: return launch_fmt<QF_FMT_MXFP4>(a, p, s);
+    default: return launch_fmt<QF_FMT_Q4K>(a, p, s);
   }
 }
 

@@ -309,3 +309,44 @@ def test_refusals(qf):
         qf.packed_matvec_grouped(weight, torch.zeros(2, dtype=torch.int64, device="cuda"), X, Y, rows_div=0)
     torch.cuda.synchronize()
     assert bool((Y == 7).all())
+
+
+def test_more_row_groups_than_one_launch_holds(qf):
+    """33000 rows of 2^20 columns need more workgroups than a grid may have: several launches.  Every
+    row is one of 64 rows of X, whose products a dense call gives (same sums in the same order: one
+    wave a tile in both, and one MFMA deep)."""
+    N, K, M, R = 1 << 20, 32, 64, 33000
+    g = torch.Generator(device="cuda").manual_seed(8)
+    codes = torch.randint(0, 256, (N, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    scales = torch.randint(110, 130, (N, K // 32), generator=g, device="cuda", dtype=torch.uint8)
+    x = torch.randn(M, K, generator=g, device="cuda").to(torch.bfloat16)
+    rows = torch.randint(0, M, (R,), generator=g, device="cuda", dtype=torch.int32)
+    want = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+    qf.packed_matvec(qf.packed_weight("mxfp4", N, K, codes, scales), x, want)
+    Y = torch.full((R, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    off = torch.tensor([0, R - 2], device="cuda")
+    qf.packed_matvec_grouped(qf.packed_weight("mxfp4", N, K, codes, scales, E=1), off, x, Y, rows=rows)
+    for r in range(0, R - 2, 1000):
+        end = min(r + 1000, R - 2)
+        assert torch.equal(Y[r:end], want[rows[r:end].long()]), r
+    assert bool((Y[R - 2:] == 7).all())
+
+
+def test_more_columns_than_one_launch_holds(qf):
+    """64 rows of 2^29 + 40 columns: three row groups in one launch, the fourth in another.  The weight
+    is one of 2^20 rows over and over, whose products a call of its own gives."""
+    n, K, M, times = 1 << 20, 32, 64, 512
+    g = torch.Generator(device="cuda").manual_seed(9)
+    codes = torch.randint(0, 256, (n, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    scales = torch.randint(110, 130, (n, K // 32), generator=g, device="cuda", dtype=torch.uint8)
+    x = torch.randn(M, K, generator=g, device="cuda").to(torch.bfloat16)
+    want = torch.empty(M, n, dtype=torch.bfloat16, device="cuda")
+    qf.packed_matvec(qf.packed_weight("mxfp4", n, K, codes, scales), x, want)
+    N = n * times + 40
+    all_codes = torch.cat([codes.repeat(times, 1), codes[:40]])
+    all_scales = torch.cat([scales.repeat(times, 1), scales[:40]])
+    Y = torch.full((M, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    qf.packed_matvec(qf.packed_weight("mxfp4", N, K, all_codes, all_scales), x, Y)
+    for i in range(times):
+        assert torch.equal(Y[:, i * n:(i + 1) * n], want), i
+    assert torch.equal(Y[:, times * n:], want[:, :40])
