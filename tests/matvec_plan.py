@@ -36,7 +36,3 @@ class Rules:
         self.lib.plan(FMT[fmt], int(grouped), i(E), i(N), i(K), i(R), i(CUS), out)
         v = list(out)
         return Plan(v[0], COPY[v[1]], ROWS[v[2]], *v[3:])
-
-    def variant(self, fmt, grouped, E, N, K, R):
-        """(tiles a workgroup takes, copy, rows): with the format, one instance of the kernel."""
-        return self.plan(fmt, grouped, E, N, K, R)[:3]

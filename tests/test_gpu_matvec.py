@@ -12,6 +12,7 @@ import pytest
 
 import workloads
 from oracle import experts as ox
+from tests import matvec_cases
 from tests.helpers import bf16_to_f64, from_dev, to_dev
 
 pytestmark = pytest.mark.gpu
@@ -350,3 +351,72 @@ def test_more_columns_than_one_launch_holds(qf):
     for i in range(times):
         assert torch.equal(Y[:, i * n:(i + 1) * n], want), i
     assert torch.equal(Y[:, times * n:], want[:, :40])
+
+
+@pytest.mark.parametrize("fmt,instance,rows,N,K", matvec_cases.VARIANTS)
+def test_every_instance_of_the_kernel(qf, fmt, instance, rows, N, K):
+    """All columns against FP64 on the decode; the weight's rows are 2053 different ones over and over."""
+    rng = np.random.default_rng(N + K)
+    grouped, E, R = matvec_cases.sizes(rows)
+    P, M, div = 2053, 29 if grouped else R, 3
+    codes, scales, S = _codes(rng, fmt, P, K, E)
+    W = ox.decode(fmt, codes, scales, None if S is None else 1.0)
+    mag = torch.from_numpy(_magnitude(fmt, codes, W)).cuda()
+    W = torch.from_numpy(W).cuda()
+    pick = torch.arange(E * N, device="cuda") % P
+    weight = qf.packed_weight(fmt, N, K, to_dev(codes)[pick], None if scales is None else to_dev(scales)[pick],
+                              None if S is None else to_dev(S), E=E if grouped else None)
+    xh = workloads.normal_bf16(rng, (M, K))
+    wide = np.full((M, (K + 7) // 8 * 8 + 16), 0x7FC0, np.uint16)
+    wide[:, :K] = xh
+    X, xf = to_dev(wide)[:, :K], torch.from_numpy(bf16_to_f64(xh)).cuda()
+    if grouped:
+        off = _grouped(rng, rows)
+        of = rng.integers(0, M * div, R).astype(np.int32)
+        of[1] = -1
+        xf = torch.cat([xf, torch.zeros(1, K, dtype=torch.float64, device="cuda")])
+        x = xf[torch.from_numpy(np.where(of < 0, M, of // div)).cuda().long()]
+    else:
+        off, x = [0, R], xf
+    for f32 in (True, False):
+        full = _out(R, N, f32)
+        if grouped:
+            qf.packed_matvec_grouped(weight, to_dev(off), X, full[:, :N], rows=to_dev(of), rows_div=div)
+        else:
+            qf.packed_matvec(weight, X, full[:, :N])
+        for e in range(E):
+            a, b = int(off[e]), int(off[e + 1])
+            if a == b:
+                continue
+            p, s = pick[e * N:(e + 1) * N], 1.0 if S is None else float(S[e])
+            ref, most = x[a:b] @ W[p].t().contiguous() * s, x[a:b].abs() @ mag[p].t().contiguous() * s
+            bound = ((32 + K / 32 + 8) * 2.0 ** -23 + 2.0 ** -22) * most + (2.0 ** -24 if f32 else 2.0 ** -8) * ref.abs()
+            assert bool(((full[a:b, :N].double() - ref).abs() <= bound).all()), (e, f32)
+        assert bool((full[:, N:] == 7).all()) and bool((full[int(off[-1]):] == 7).all())
+
+
+@pytest.mark.parametrize("fmt,K", [("nvfp4", 1056), ("nvfp4", 1072), ("mxfp4", 1056)])
+def test_nan_scales_in_every_form(qf, fmt, K):
+    """A scale code that is NaN, in a whole slice or in the k past it, under codes that are zero too: its
+    weight row's outputs are NaN and no others, for few rows, up to 16, and experts of 9 to 16."""
+    rng = np.random.default_rng(K)
+    N, bad = 70, {"nvfp4": (0x7F, 0xFF), "mxfp4": (0xFF, 0xFF)}[fmt]
+    codes, scales, S = _codes(rng, fmt, 2 * N, K, 2)
+    codes[:, ::3] = 0
+    n, last = 5, scales.shape[1] - 1
+    scales[n, 3], scales[33, last], scales[N + 64, 0] = bad[0], bad[0], bad[1]
+    codes[n, 3 * BLOCK[fmt] // 2:4 * BLOCK[fmt] // 2] = 0
+    want = np.zeros((2, N), bool)
+    want[0, [n, 33]], want[1, 64] = True, True
+    want = torch.from_numpy(want).cuda()
+    for M in (2, 7, 16, 40):
+        x = to_dev(workloads.normal_bf16(rng, (M, K)))
+        Y = _out(M, N, True)[:, :N]
+        qf.packed_matvec(_weight(qf, fmt, N, K, codes[:N], scales[:N], None if S is None else S[:1]), x, Y)
+        assert torch.equal(torch.isnan(Y), want[:1].expand(M, N)), M
+    for counts in ([1, 2], [4, 5], [16, 11], [40, 20]):
+        R = sum(counts)
+        x = to_dev(workloads.normal_bf16(rng, (R, K)))
+        Y = _out(R, N, True)[:, :N]
+        qf.packed_matvec_grouped(_weight(qf, fmt, N, K, codes, scales, S, E=2), to_dev(_grouped(rng, counts)), x, Y)
+        assert torch.equal(torch.isnan(Y), want[torch.tensor([0] * counts[0] + [1] * counts[1], device="cuda")]), counts

@@ -4,6 +4,7 @@ import random
 
 import pytest
 
+from tests.matvec_cases import VARIANTS, instances, sizes
 from tests.matvec_plan import Rules
 
 BLOCK = {"nvfp4": 16, "mxfp4": 32, "q4k": 256}
@@ -63,3 +64,12 @@ def test_more_row_groups_than_one_launch_holds(rules):
         p = rules.plan(fmt, grouped, E, N, K, R)
         _launch_fits(p, fmt)
         assert p.per_launch < p.items
+
+
+def test_device_cases_reach_every_instance(rules):
+    seen = set()
+    for fmt, instance, rows, N, K in VARIANTS:
+        grouped, E, R = sizes(rows)
+        assert tuple(rules.plan(fmt, grouped, E, N, K, R)[:3]) == instance, (fmt, rows, N, K)
+        seen.add((fmt, instance))
+    assert seen == instances()
