@@ -22,6 +22,9 @@
 //          and a mask; with X1 = -16 sum x from one MFMA as the next one's addend, P = sum (16 + q) x
 //          + X1 = sum q x, and a super-block adds d sum s6 P + (dmin / 16) sum m6 X1.  (Sums of s6 x and
 //          m6 x on the matrix cores instead of vector operations: 13.0 -> 14.1 us, 14336 x 4096, five rows.)
+//          These sums are taken 2^-18 times as large, d and dmin 2^18 times: a super-block's are at most
+//          2^18 max |x|, and no finite x makes them infinite where the result is not.  What is lost
+//          are bits below 2^-149 of the scaled sums, which matter where all |x| are below 2^-108.
 // Bound by reading the weight once, 0.53 to 0.56 bytes an element (NVFP4, 24576 x 4096, one row: 56.7
 // MB in 12.1 us = 4.7 TB/s; the copies alone take 11.2), Q4_K by its decode (14336 x 4096, five rows:
 // 13.0 us, 9.9 without the arithmetic).  Small weights are bound by the launch and one trip to memory
@@ -238,21 +241,21 @@ __device__ __forceinline__ void multiply32_small(const uint4& c, uint32_t s, con
   }
 }
 
-// Two bf16 values 16 + q of the codes in the low (HIGH: high) nibbles of bytes 0 and 2 of w.
+// Two bf16 values 2^-18 (16 + q) of the codes in the low (HIGH: high) nibbles of bytes 0 and 2 of w.
 template <bool HIGH>
 __device__ __forceinline__ uint32_t q4k_pair(uint32_t w) {
-  return ((HIGH ? w >> 1 : w << 3) & 0x00780078u) | 0x41804180u;
+  return ((HIGH ? w >> 1 : w << 3) & 0x00780078u) | 0x38803880u;
 }
 // One super-block of this lane's weight row (144 bytes at `row`) against the X row at xl (chunks of 8
 // exchanged by xw, the super-block's first chunk c0).
 __device__ __forceinline__ void q4k_superblock(const char* row, const char* xl, int xw, int c0, int g,
                                                f32x4_t& acc) {
   const uint4 head = *reinterpret_cast<const uint4*>(row);
-  const float d = codec::f16_value(head.x & 0xFFFFu), dm = codec::f16_value(head.x >> 16);
+  const float d = codec::f16_value(head.x & 0xFFFFu) * 0x1p18f, dm = codec::f16_value(head.x >> 16) * 0x1p14f;
   const uint32_t s6[2] = {head.y & 0x3F3F3F3Fu, (head.w & 0x0F0F0F0Fu) | ((head.y >> 2) & 0x30303030u)};
   const uint32_t m6[2] = {head.z & 0x3F3F3F3Fu, ((head.w >> 4) & 0x0F0F0F0Fu) | ((head.z >> 2) & 0x30303030u)};
   const f32x4_t zero = {0.0f, 0.0f, 0.0f, 0.0f};
-  const uint4 minus16 = make_uint4(0xC180C180u, 0xC180C180u, 0xC180C180u, 0xC180C180u);
+  const uint4 minus16 = make_uint4(0xB880B880u, 0xB880B880u, 0xB880B880u, 0xB880B880u);
   f32x4_t ps = zero, pm = zero;
 #pragma unroll
   for (int c = 0; c < 4; ++c) {                   // sub-blocks 2 c (low nibbles) and 2 c + 1
@@ -275,7 +278,7 @@ __device__ __forceinline__ void q4k_superblock(const char* row, const char* xl, 
     }
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) acc[i] = __builtin_fmaf(dm * 0.0625f, pm[i], __builtin_fmaf(d, ps[i], acc[i]));
+  for (int i = 0; i < 4; ++i) acc[i] = __builtin_fmaf(dm, pm[i], __builtin_fmaf(d, ps[i], acc[i]));
 }
 
 // -------------------------------------------------------------------------------- the kernel

@@ -420,3 +420,38 @@ def test_nan_scales_in_every_form(qf, fmt, K):
         Y = _out(R, N, True)[:, :N]
         qf.packed_matvec_grouped(_weight(qf, fmt, N, K, codes, scales, S, E=2), to_dev(_grouped(rng, counts)), x, Y)
         assert torch.equal(torch.isnan(Y), want[torch.tensor([0] * counts[0] + [1] * counts[1], device="cuda")]), counts
+
+
+def test_q4k_activations_of_every_size(qf):
+    """Every finite activation has the definition's product, however near the type's largest it is, where
+    that is finite: d and dmin of 2^-24 or thrice it, so that it always is (2^128 x 3 x 2^-24 x 63 x 16 x
+    1280 < 2^127), while 16 sum x and sums of s6 (16 + q) x are far from it.  Activations of 2^-120 too: the
+    bound then has what sums kept to multiples of 2^-149 / 2^18 can be off by, once an addition, s6 or m6
+    times, twice."""
+    rng = np.random.default_rng(21)
+    N, K, M = 40, 1280, 9
+    codes, _, _ = _codes(rng, "q4k", N, K)
+    half = ((1 + 2 * rng.integers(0, 2, (N, K // 256, 2))) * 2.0 ** -24).astype(np.float16)
+    codes[..., :4] = half.view(np.uint8).reshape(N, K // 256, 4)
+    codes[7, 1, 4:] = 0xFF                                         # the largest scales, mins and codes
+    x = workloads.normal_bf16(rng, (M, K))
+    x[0] = 0x7F7F                                                  # the largest, all of one sign
+    x[1] = np.where(rng.random(K) < 0.5, 0x7F7F, 0xFF7F)
+    x[2] = (x[2] & 0x807F) | 0x7F00                                # 2^127 to 2^128
+    x[3] = (x[3] & 0x807F) | 0x7880                                # 2^114 to 2^115
+    x[4, ::2] = 0x7F7F                                             # beside ordinary ones
+    x[5] = (x[5] & 0x807F) | 0x2000                                # 2^-63 to 2^-62
+    x[6] = (x[6] & 0x807F) | 0x0380                                # 2^-120 to 2^-119
+    for big in (False, True):
+        if big:                                                    # steps of 2^14 for the small ones alone
+            codes[..., :4] = np.full((N, K // 256, 2), 2.0 ** 14, np.float16).view(np.uint8).reshape(N, K // 256, 4)
+            x[:5] = 0
+        W = ox.decode("q4k", codes)
+        Y = torch.empty(M, N, device="cuda")
+        qf.packed_matvec(qf.packed_weight("q4k", N, K, to_dev(codes)), to_dev(x), Y)
+        ref, bound = _bound(bf16_to_f64(x), W, _magnitude("q4k", codes, W), K, True)
+        assert np.abs(ref).max() < 3.4e38
+        step = 2.0 ** 14 if big else 3 * 2.0 ** -24
+        bound += 2 * (32 + K / 32 + 8) * 63 * step * 2.0 ** (18 - 149) + 2.0 ** -149
+        off = ~(np.abs(from_dev(Y) - ref) <= bound)
+        assert not off.any(), (big, np.argwhere(off)[:4].tolist())
