@@ -733,7 +733,8 @@ typedef struct {
  *   X bf16 [M, K] (row stride ldx); Y bf16 (y_f32 = 0) or FP32 (y_f32 = 1) [M, N] (row stride ldy).
  * A scale code that is NaN (E4M3 0x7F, E8M0 0xFF) makes the outputs of its weight row NaN.  NVFP4 sums
  * run without S, which multiplies the result: they have to stay finite before it.  Under Q4_K an
- * infinite activation makes its outputs NaN; a finite one, however large, does not.
+ * infinite activation makes its outputs NaN; finite ones, however large, do not while FP32 holds the
+ * sums of d s6 q x and of dmin m6 x.
  */
 QF_API qf_status qf_packed_matvec(const qf_packed* w, int64_t M, const uint16_t* X, int64_t ldx,
                                   void* Y, int64_t ldy, int y_f32, qf_stream_t stream);

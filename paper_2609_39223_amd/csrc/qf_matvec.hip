@@ -23,8 +23,8 @@
 //          + X1 = sum q x, and a super-block adds d sum s6 P + (dmin / 16) sum m6 X1.  (Sums of s6 x and
 //          m6 x on the matrix cores instead of vector operations: 13.0 -> 14.1 us, 14336 x 4096, five rows.)
 //          These sums are taken 2^-18 times as large, d and dmin 2^18 times: a super-block's are at most
-//          2^18 max |x|, and no finite x makes them infinite where the result is not.  What is lost
-//          are bits below 2^-149 of the scaled sums, which matter where all |x| are below 2^-108.
+//          2^18 max |x| before that, so no finite x makes them infinite.  What is lost are bits below
+//          2^-149 of the scaled sums, which matter where all |x| are below 2^-108.
 // Bound by reading the weight once, 0.53 to 0.56 bytes an element (NVFP4, 24576 x 4096, one row: 56.7
 // MB in 12.1 us = 4.7 TB/s; the copies alone take 11.2), Q4_K by its decode (14336 x 4096, five rows:
 // 13.0 us, 9.9 without the arithmetic).  Small weights are bound by the launch and one trip to memory
