@@ -365,3 +365,107 @@ def test_refusals_leave_outputs_alone(qf):
         qf.moe_combine(ids, empty_bf16((8, 8)), empty_bf16((4, 8)), w=w.double())
     torch.cuda.synchronize()
     assert bool((ids == 5).all())
+
+
+def test_route_non_finite_bf16_logits(qf):
+    """NaN of either sign above +inf, +inf above the largest finite logit, -inf never chosen and the
+    lowest finite logit chosen last: the choice on sorted keys (up to 512 experts) and past it."""
+    low, high = -3.3895313892515355e38, 3.3895313892515355e38
+    for E in (16, 200, 512, 1000):
+        z = torch.zeros(6, E, dtype=torch.bfloat16, device="cuda")
+        z[0, 5], z[0, 2], z[0, 9] = math.nan, math.inf, high
+        z[1, 3] = math.inf
+        z[2, E - 1] = -math.nan
+        z[2, 4] = math.nan
+        z[3] = -math.inf
+        z[3, E - 1], z[3, 1] = low, -0.0
+        z[4, 7], z[4, 11] = high, low
+        z[5, :E - 1] = math.nan
+        for norm in (True, False):
+            ids = torch.empty(6, 3, dtype=torch.int32, device="cuda")
+            w = torch.empty(6, 3, device="cuda")
+            qf.moe_route(z, ids, w, norm=norm)
+            assert from_dev(ids).tolist() == [[5, 2, 9], [3, 0, 1], [4, E - 1, 0], [1, E - 1, -1], [7, 0, 1], [0, 1, 2]]
+            a = from_dev(w)
+            assert np.isnan(a[[0, 2, 5]]).all() and np.isnan(a[1, 0])
+            assert a[3].tolist() == [1.0, 0.0, 0.0] and a[4].tolist() == [1.0, 0.0, 0.0]
+            qf.moe_route(z, ids, w, score="sigmoid", norm=norm)
+            assert from_dev(ids)[:2].tolist() == [[5, 2, 9], [3, 0, 1]]
+            a = from_dev(w)
+            assert np.isnan(a[0, 0])
+            assert np.allclose(a[1], [0.5, 0.25, 0.25] if norm else [1.0, 0.5, 0.5], atol=1e-6)
+            assert np.allclose(a[3], [1.0, 0.0, 0.0] if norm else [0.5, 0.0, 0.0], atol=1e-6)
+
+
+def _rows_of(qf, T, E, k, seed, drop):
+    """row_of of T tokens' distinct random choices, some dropped."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    ids = torch.rand(T, E, generator=g, device="cuda").topk(k, dim=1).indices.to(torch.int32)
+    if drop:
+        ids[torch.rand(T, k, generator=g, device="cuda") < drop] = -1
+        ids[T // 2] = -1
+    off, row_of, slot_of, _ = _sorted(qf, from_dev(ids), E)
+    return row_of, slot_of, g
+
+
+@pytest.mark.parametrize("T,E,k,H,drop", [
+    (70000, 8, 1, 1000, 0.1), (33000, 16, 2, 1032, 0.05), (33000, 16, 4, 512, 0.1), (8600, 64, 8, 1000, 0.1),
+    (17000, 32, 2, 2048, 0.0), (9000, 60, 6, 1544, 0.1), (200, 128, 64, 5632, 0.1)])
+def test_gradients_of_rows_past_128_mb(qf, T, E, k, H, drop):
+    """Expert rows of more than 128 MB, which are written past the caches: the sum, its gradients and the
+    copy, rows and weights of dropped slots NaN, against torch in 64 bits (bounds as above)."""
+    assert 2 * T * k * H > 128 << 20
+    row_of, slot_of, g = _rows_of(qf, T, E, k, T + k, drop)
+    Yg = torch.randn(T * k, H, generator=g, device="cuda").to(torch.bfloat16)
+    Yg[slot_of < 0] = math.nan
+    dY = torch.randn(T, H, generator=g, device="cuda").to(torch.bfloat16)
+    w = torch.randn(T, k, generator=g, device="cuda")
+    live = row_of >= 0
+    w[~live] = math.nan
+    Y, dYg = torch.full_like(dY, math.nan), torch.full_like(Yg, math.nan)
+    dw = torch.full_like(w, math.nan)
+    qf.moe_combine(row_of, Yg, Y, w=w)
+    qf.moe_combine_bwd(row_of, dY, dYg, Yg=Yg, w=w, dw=dw)
+    for t0 in range(0, T, 2000):
+        t = slice(t0, min(t0 + 2000, T))
+        rows, on, d = row_of[t].long(), live[t], dY[t].double()
+        y = torch.where(on[..., None], Yg[rows.clamp(min=0)].double(), 0.0)
+        wt = torch.where(on, w[t].double(), 0.0)
+        prod = wt[..., None] * y
+        ref, mag = prod.sum(1), prod.abs().sum(1)
+        assert bool(((Y[t].double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 2 * k * U * mag).all()), t0
+        dots = d[:, None] * y
+        assert bool(((dw[t].double() - dots.sum(2)).abs() <= (H / 256 + 16) * U * dots.abs().sum(2)).all()), t0
+        assert bool((dw[t][~on] == 0).all())
+        want = (wt.float()[..., None] * dY[t].float()[:, None]).to(torch.bfloat16)   # one product, rounded once
+        row = torch.where(on, rows, -1 - rows)
+        assert torch.equal(dYg[row], want), t0
+    assert not bool(dYg[slot_of < 0].any())
+
+
+def test_gradients_of_rows_past_32_bits_of_bytes(qf):
+    """The sum and its gradients where byte offsets of expert rows pass 2^32 (4.6 GB of them)."""
+    T, E, k, H = 35000, 4, 2, 32768
+    row_of, _, g = _rows_of(qf, T, E, k, 5, 0.0)
+    assert int(row_of.max()) == T * k - 1
+    Yg, dY = (torch.randint(0, 0x8000, (n, H), generator=g, device="cuda", dtype=torch.int16) for n in (T * k, T))
+    for a in (Yg, dY):                                             # finite, 2^-63 to 2^1, of either sign
+        a &= 0x1FFF
+        a |= 0x2000
+        a[:, ::3] |= -0x8000
+    Yg, dY = Yg.view(torch.bfloat16), dY.view(torch.bfloat16)
+    w = torch.randn(T, k, generator=g, device="cuda")
+    Y, dYg, dw = torch.empty_like(dY), torch.empty_like(Yg), torch.empty_like(w)
+    qf.moe_combine(row_of, Yg, Y, w=w)
+    qf.moe_combine_bwd(row_of, dY, dYg, Yg=Yg, w=w, dw=dw)
+    for t0 in range(0, T, 500):
+        t = slice(t0, min(t0 + 500, T))
+        want = (w[t][..., None] * dY[t].float()[:, None]).to(torch.bfloat16)
+        assert torch.equal(dYg[row_of[t].long()], want), t0
+    last = (row_of >= T * k - 20).any(1).nonzero()[:, 0]           # tokens of the highest rows, and others
+    t = torch.cat([last, torch.tensor([0, 1, T // 2, T - 1], device="cuda")])
+    y, wt, d = Yg[row_of[t].long()].double(), w[t].double(), dY[t].double()
+    prod, dots = wt[..., None] * y, d[:, None] * y
+    ref = prod.sum(1)
+    assert bool(((Y[t].double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 2 * k * U * prod.abs().sum(1) + 1e-38).all())
+    assert bool(((dw[t].double() - dots.sum(2)).abs() <= (H / 256 + 16) * U * dots.abs().sum(2)).all())
