@@ -22,7 +22,7 @@
  *    on error nothing is launched and qf_last_error() returns a message (thread-local).
  *    Non-finite data is never an error; it propagates as each format defines.
  *  - Alignment: every tensor base pointer must be 16-byte aligned and every leading
- *    dimension a multiple of 8 elements (QF_EALIGN otherwise).
+ *    dimension a multiple of 8 elements unless the call says otherwise (QF_EALIGN).
  *  - Nibble order: two 4-bit codes per byte, element 2i in the LOW nibble.  Code layout:
  *    bit 3 = sign, bits 0-2 = E2M1 magnitude index into {0, .5, 1, 1.5, 2, 3, 4, 6}.
  *  - Scale layout: plain row-major [R, K/block] bytes (E4M3 for NVFP4, E8M0 for MXFP4).
@@ -628,7 +628,8 @@ typedef enum { QF_SCORE_SOFTMAX = 0, QF_SCORE_SIGMOID = 1 } qf_score;
 
 /*
  * qf_moe_route -- the k largest logits of every token and their weights.
- *   z      bf16 (z_f32 = 0) or FP32 (z_f32 = 1) logits [T, E], row stride ldz (a multiple of 8).
+ *   z      bf16 (z_f32 = 0) or FP32 (z_f32 = 1) logits [T, E], row stride ldz: a multiple of 8, or E
+ *          whatever it is (rows back to back).
  *   mask   uint8 [T] or NULL; 0: the token (padding) chooses nothing.  No alignment needed.
  *   ids    int32 [T, k]: the experts by falling logit, equal logits by rising expert; -1 where a
  *          token has no further expert (masked, or every logit left is -inf).
@@ -646,7 +647,7 @@ QF_API qf_status qf_moe_route(const void* z, int z_f32, int64_t T, int64_t E, in
                               float* w, qf_stream_t stream);
 
 /*
- * qf_moe_route_bwd -- dz [T, E] (the type of z, row stride lddz; overwritten) from dw FP32 [T, k]:
+ * qf_moe_route_bwd -- dz [T, E] (the type of z, row stride lddz as ldz; overwritten) from dw FP32 [T, k]:
  * the gradient of qf_moe_route's w with the choice held fixed, zero for experts not chosen except
  * with unnormalized softmax.  z, score, norm, scale as in the forward, ids as it wrote them (an id
  * outside 0 .. E - 1 is no choice; its dw is not used).

@@ -1692,9 +1692,10 @@ qf_status check_rows(const char* fn, int64_t T, int64_t k, int64_t H, const int3
   return check_out("row_of", row_of);
 }
 
-// Logits or their gradient: [T, E] bf16 or FP32.
+// Logits or their gradient: [T, E] bf16 or FP32.  Rows back to back, as a product leaves them, may have
+// any length.
 qf_status check_logits(const char* name, const void* p, int64_t T, int64_t E, int64_t ld) {
-  return check_mat(name, p, T, E, ld, true);
+  return check_mat(name, p, T, E, ld == E ? pad8(E) : ld, true);
 }
 
 qf_status check_score(const char* fn, int z_f32, int score, int norm) {

@@ -106,10 +106,13 @@ __device__ __forceinline__ void store8(float* p, const float v[8]) {
 __device__ __forceinline__ void store1(uint16_t* p, float v) { *p = (uint16_t)codec::bf16_rne(v); }
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 
+// Experts whose logits may move in whole chunks: none where rows do not start at one (rows back to back
+// may have any length).
+__device__ __forceinline__ int in_chunks(int E, int64_t ld) { return ld % 8 == 0 ? E : 0; }
 // This lane's chunk c of a row (experts e0 .. e0 + 7; -inf past E, which is never read).
 template <class Z>
-__device__ __forceinline__ void load_chunk(const Z* row, int e0, int E, float v[8]) {
-  if (e0 + 8 <= E) {
+__device__ __forceinline__ void load_chunk(const Z* row, int e0, int E, int Ec, float v[8]) {
+  if (e0 + 8 <= Ec) {
     load_logits8(row + e0, v);
   } else {
 #pragma unroll
@@ -196,7 +199,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     if (live) {
-      load_chunk(z + t * ldz, 8 * (c * L + lane), E, x + 8 * c);
+      load_chunk(z + t * ldz, 8 * (c * L + lane), E, in_chunks(E, ldz), x + 8 * c);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[8 * c + i] = -INFINITY;
@@ -259,7 +262,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_bwd_kernel(
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       if (t < T) {
-        load_chunk(z + t * ldz, 8 * (c * L + lane), E, x + 8 * c);
+        load_chunk(z + t * ldz, 8 * (c * L + lane), E, in_chunks(E, ldz), x + 8 * c);
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[8 * c + i] = -INFINITY;
@@ -308,7 +311,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_bwd_kernel(
       if (whole) o[i] = none ? 0.0f : expf(x[8 * c + i] - m) / s * (o[i] - dot);
     }
     Z* const out = dz + t * lddz + e0;
-    if (e0 + 8 <= E) {
+    if (e0 + 8 <= in_chunks(E, lddz)) {
       store8(out, o);
     } else {
 #pragma unroll

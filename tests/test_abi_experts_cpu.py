@@ -130,3 +130,18 @@ def test_launch_limits(L):
     assert L.qf_moe_combine(A, B, I(T - 1), I(1), I(1 << 60), C, D, I(1 << 60), None) == QF_ENOTSUP
     # one piece fewer passes this check (and fails the next one)
     assert L.qf_moe_combine(A, B, I(T - 1), I(1), I(H), None, D, I(H), None) == QF_EINVAL
+
+
+def test_logits_with_rows_back_to_back(L):
+    """A row stride of E is fine whatever E is; another stride has to be a multiple of 8, and the base is
+    aligned in either case."""
+    def fwd(E=20, ld=20, z=A):
+        return L.qf_moe_route(z, 1, I(4), I(E), I(ld), I(2), 0, 1, F(1), None, None, None, None)
+
+    def bwd(ldz=20, lddz=20, dz=D):
+        return L.qf_moe_route_bwd(A, 0, I(4), I(20), I(ldz), I(2), 0, 1, F(1), None, B, dz, I(lddz), None)
+    assert fwd() == QF_EINVAL and b"null output" in L.qf_last_error()
+    assert fwd(ld=22) == QF_EALIGN and fwd(ld=19) == QF_ESHAPE and fwd(z=P(264)) == QF_EALIGN
+    assert bwd() == QF_EINVAL and b"null ids" in L.qf_last_error()
+    assert bwd(lddz=24) == QF_EINVAL and bwd(lddz=21) == QF_EALIGN and bwd(ldz=21) == QF_EALIGN
+    assert bwd(dz=P(8)) == QF_EALIGN

@@ -469,3 +469,32 @@ def test_gradients_of_rows_past_32_bits_of_bytes(qf):
     ref = prod.sum(1)
     assert bool(((Y[t].double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 2 * k * U * prod.abs().sum(1) + 1e-38).all())
     assert bool(((dw[t].double() - dots.sum(2)).abs() <= (H / 256 + 16) * U * dots.abs().sum(2)).all())
+
+
+@pytest.mark.parametrize("T,E,k", [(33, 60, 4), (64, 129, 8), (23, 5, 5), (19, 1, 1), (40, 252, 9), (17, 509, 33), (9, 1001, 64)])
+@pytest.mark.parametrize("score,norm", [("softmax", True), ("softmax", False), ("sigmoid", True)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_route_on_dense_rows_of_any_length(qf, T, E, k, score, norm, dtype):
+    """Logits and gradients as a product leaves them, rows back to back whatever E is: the bits of padded
+    rows, and nothing past the last row written."""
+    rng = np.random.default_rng(E)
+    raw, _ = _logits(rng, T, E, dtype)
+    dw = to_dev(rng.normal(size=(T, k)).astype(np.float32))
+    mask = to_dev((rng.random(T) < 0.8).astype(np.uint8))
+    padded, dense = _padded(raw, 8, 0), to_dev(raw)
+    out = []
+    for z in (padded, dense):
+        ids, w = torch.full((T, k), 77, dtype=torch.int32, device="cuda"), torch.full((T, k), 77.0, device="cuda")
+        qf.moe_route(z, ids, w, score=score, norm=norm, scale=1.5, mask=mask)
+        out.append((ids, w))
+    assert torch.equal(out[0][0], out[1][0])
+    assert np.array_equal(from_dev(out[0][1].view(torch.int32)), from_dev(out[1][1].view(torch.int32)))
+    ids = out[0][0]
+    want = _padded(np.full((T, E), 1, raw.dtype), 8, 0)
+    qf.moe_route_bwd(padded, ids, dw, want, score=score, norm=norm, scale=1.5)
+    for z, out_dense in ((dense, True), (padded, True), (dense, False)):
+        flat = torch.full((T * E + 64,), 1, dtype=want.dtype, device="cuda")
+        dz = flat[:T * E].view(T, E) if out_dense else _padded(np.full((T, E), 1, raw.dtype), 16, 0)
+        qf.moe_route_bwd(z, ids, dw, dz, score=score, norm=norm, scale=1.5)
+        assert torch.equal(dz, want)
+        assert not out_dense or bool((flat[T * E:] == 1).all())
