@@ -526,9 +526,12 @@ def _logits(z):
 
 
 def moe_route(z, ids, w, score="softmax", norm=True, scale=1.0, mask=None):
-    """The ids.shape[1] largest logits of every row of z [T, E] (ids int32, w float32 [T, k])."""
+    """The ids.shape[1] largest logits of every row of z [T, E] (ids int32, w float32 [T, k]); mask: bool
+    or uint8 [T], false for padding."""
     T, E, ld, f32 = _logits(z)
     k = ids.shape[1]
+    if mask is not None and mask.dtype == torch.bool:
+        mask = mask.view(torch.uint8)
     _check(lib().qf_moe_route(_ptr(z), f32, T, E, ld, k, SCORE[score], int(norm), float(scale),
                               _typed(mask, torch.uint8, "mask", (T,)),
                               _typed(ids, torch.int32, "ids", (T, k)),

@@ -498,3 +498,12 @@ def test_route_on_dense_rows_of_any_length(qf, T, E, k, score, norm, dtype):
         qf.moe_route_bwd(z, ids, dw, dz, score=score, norm=norm, scale=1.5)
         assert torch.equal(dz, want)
         assert not out_dense or bool((flat[T * E:] == 1).all())
+
+
+def test_route_takes_a_boolean_mask(qf):
+    z = torch.randn(37, 60, device="cuda")
+    mask = torch.arange(37, device="cuda") % 3 != 0
+    got = [qf.moe_route(z, torch.empty(37, 4, dtype=torch.int32, device="cuda"), torch.empty(37, 4, device="cuda"), mask=m)
+           for m in (mask, mask.to(torch.uint8))]
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    assert bool((got[0][0][~mask] == -1).all()) and bool((got[0][0][mask] >= 0).all())
