@@ -20,7 +20,7 @@ VARIANTS = [
     ("nvfp4", (2, "cached", "small"), [1, 2, 0, 1] * 32, 645, 96),
     ("nvfp4", (2, "cached", "twice"), [9, 4, 2, 7, 0] * 12, 885, 160),
     ("nvfp4", (2, "streamed", "all"), 10, 5145, 6752),
-    ("nvfp4", (2, "streamed", "all"), [2, 3, 0, 1, 2, 3, 0, 3], 18817, 224),
+    ("nvfp4", (2, "streamed", "all"), [3, 3, 0, 2, 2, 3, 1, 4], 18817, 224),
     ("nvfp4", (2, "streamed", "small"), [1, 0, 2, 1] * 15, 1449, 416),
     ("nvfp4", (2, "streamed", "twice"), [30, 11, 0, 50, 9, 16] * 10, 927, 608),
     ("nvfp4", (2, "words", "all"), 49, 8501, 176),
