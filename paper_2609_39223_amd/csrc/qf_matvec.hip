@@ -26,9 +26,9 @@
 //          2^18 max |x| before that, so no finite x makes them infinite.  What is lost are bits below
 //          2^-149 of the scaled sums, which matter where all |x| are below 2^-108.
 // Bound by reading the weight once, 0.53 to 0.56 bytes an element (NVFP4, 24576 x 4096, one row: 56.7
-// MB in 12.1 us = 4.7 TB/s; the copies alone take 11.2), Q4_K by its decode (14336 x 4096, five rows:
-// 13.0 us, 9.9 without the arithmetic).  Small weights are bound by the launch and one trip to memory
-// (4096 x 4096: 4.7 us).
+// MB in 12.3 us = 4.6 TB/s; the copies alone take 11.2), Q4_K by its decode, which is that of 16 rows
+// whatever their number (14336 x 4096, five rows: 13.1 us, 9.9 without the arithmetic; one row 12.1).  Small
+// weights are bound by the launch and one trip to memory (4096 x 4096: 5.0 us).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

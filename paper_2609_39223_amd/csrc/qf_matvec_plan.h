@@ -41,7 +41,8 @@ inline MatvecPlan matvec_plan(int fmt, bool grouped, int64_t E, int64_t N, int64
   MatvecPlan p{};
   // Rows a workgroup takes, 16 of a dense call.  Of experts more than the mean: LDS for rows that most of
   // them do not have costs waves, and an expert with more rows is read again from the last-level cache.
-  // All us below: graph replays over inputs that exceed the last-level cache.
+  // All us below: graph replays over sets of inputs in turn, 230 MB of 4096 x 4096, else more than the
+  // last-level cache holds; experts' rows of X read through the sort.
   //   4 or 8 rows at 1.5 / 2 / 3 rows an expert.  MXFP4, 3072 x 3072, 128 experts: 81, 78 / 97, 89 / 128,
   //   108; 4096 x 4096, 8 experts: 14.9, 16.3 / 16.5, 16.7 / 18.6, 17.9.  Q4_K: 121, 122 / 148, 140 / 194,
   //   172; 21.3, 26.8 / 23.9, 27.1 / 28.8, 28.6.  NVFP4 has a cheaper form for 4 rows; at 2 / 2.5 / 3: 95,

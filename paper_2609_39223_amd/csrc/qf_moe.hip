@@ -127,8 +127,10 @@ __device__ __forceinline__ float log_sigmoid(float x) {
 
 // Lane j < k of the group ends up with choice j (expert id, -1: none left; its logit v).
 //
-// FP32 logits: a round finds the largest key of the row, the first lane that has it and that lane's
-// first expert with it, which is struck out.
+// FP32 logits, and more than 512 experts: a round finds the largest key of the row, the first lane that
+// has it and that lane's first expert with it, which is struck out: two reductions and three passes over
+// the lane's keys (32768 tokens, 8 choices: 128 experts 10.5 us where bf16 takes 7.2, 256 17.9 / 12.3, 1024
+// 54 either way).
 template <int L, int C>
 __device__ __forceinline__ void choose(uint32_t key[8 * C], int lane, int k, int& id, float& v) {
   id = -1;
