@@ -755,6 +755,130 @@ QF_API qf_status qf_packed_matvec_grouped(const qf_packed* w, const int64_t* gro
                                           int64_t M, const uint16_t* X, int64_t ldx, void* Y,
                                           int64_t ldy, int y_f32, qf_stream_t stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Around the packed products of a decode step: the 4-bit cache of keys and values, the attention that
+ * reads it, and the low-rank adapters of many requests (Sec. 3.2.3's formats, Sec. 3.3's adapters, in
+ * the engine that Sec. 3.4 and 3.5 export to)
+ * ------------------------------------------------------------------------------------ */
+/*
+ * A cache of keys and values in pages.
+ *   pages    pages in the pool; page: tokens a page, a power of two from 16 to 1024.
+ *   H, D     heads of keys and values; D is 64, 128 or 256; H D < 2^20.
+ *   fmt      QF_FMT_NVFP4 or QF_FMT_MXFP4, blocks along D, codes and scales as the quantizers write them:
+ *   k_codes, v_codes    [pages, H, page, D/2] bytes, element 2i in the low nibble.
+ *   k_scales, v_scales  [pages, H, page, D/16] E4M3 (NVFP4) or [pages, H, page, D/32] E8M0 (MXFP4).
+ *   k_S, v_S FP32 [H], NVFP4 only: the heads' tensor decode scales (a calibrated amax / 2688), positive
+ *            and fixed while the cache lives.  No alignment needed.
+ * Codes and scales are 16-byte aligned.
+ */
+typedef struct {
+    int64_t pages, page;
+    int64_t H, D;
+    int32_t fmt;
+    uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+    const float *k_S, *v_S;
+} qf_kv_cache;
+
+/*
+ * The sequences of a call, in DEVICE arrays that the host never reads.
+ *   B        sequences.
+ *   offsets  int64 [B + 1], non-decreasing from 0, or NULL: rows offsets[b] .. offsets[b + 1] - 1 of the
+ *            call's T rows are sequence b's; NULL: row b is sequence b's (then T = B).  Rows from
+ *            offsets[B] on belong to nobody.
+ *   lens     int32 [B]: tokens of the sequence, those of this call, which are its last ones, included:
+ *            row offsets[b] + i is the token at position lens[b] - n + i of its n rows.
+ *   table    int32 [B, cols]: the page of tokens j page .. j page + page - 1 of sequence b in table[b][j].
+ *            Entries that a sequence does not reach are not read; one outside 0 .. pages - 1 is no page.
+ *   max_len  no sequence is longer (the caller's word, so that launches need not provide for more).
+ * lens and table 4-byte aligned, offsets 8-byte aligned.  Limits: T < 2^28, B < 2^28, max_len < 2^30.
+ */
+typedef struct {
+    int64_t B;
+    const int64_t* offsets;
+    const int32_t* lens;
+    const int32_t* table;
+    int64_t cols;
+    int64_t max_len;
+} qf_kv_seqs;
+
+/*
+ * qf_kv_write -- quantizes the rows' keys and values into the cache: K, V bf16 [T, H D] (row strides ldk,
+ * ldv), head h in columns h D .. h D + D - 1.  The codes and scales are those of qf_fakequant_mxfp4 and,
+ * with S given, of qf_fakequant_nvfp4, bit for bit (NVFP4 blocks past 448 S 6 saturate, infinities too; a
+ * NaN gives its block the NaN scale).  A row whose position is negative or has no page is not kept.
+ * Rows of one call must not share a place (sequences that share a page write to it one call apart).
+ */
+QF_API qf_status qf_kv_write(const qf_kv_cache* c, const qf_kv_seqs* q, int64_t T, const uint16_t* K,
+                             int64_t ldk, const uint16_t* V, int64_t ldv, qf_stream_t stream);
+
+/*
+ * qf_kv_read -- the inverse: the rows' keys and values as the cache holds them, x_hat of the quantizers bit
+ * for bit, zeros for a row without a place; rows that belong to nobody are left alone.  K or V may be
+ * NULL.  With offsets the prefix sums of lens, whole sequences.  max_len is not used.
+ */
+QF_API qf_status qf_kv_read(const qf_kv_cache* c, const qf_kv_seqs* q, int64_t T, uint16_t* K,
+                            int64_t ldk, uint16_t* V, int64_t ldv, qf_stream_t stream);
+
+/*
+ * qf_kv_attention -- causal attention of the rows' queries over their sequences' cached tokens (the rows'
+ * own, which qf_kv_write has put there, included).
+ *   Q      bf16 [T, Hq D] (row stride ldq), Hq a multiple of H: heads j Hq / H .. of Q read head j of
+ *          the cache.
+ *   z_t = scale q . k_t for positions t up to the row's own and, with window > 0, later than its own -
+ *   window;  O = sum softmax(z)_t v_t  (bf16 [T, Hq D], row stride ldo, rounded once);
+ *   lse    FP32 [T, Hq] or NULL: log sum_t exp(z_t).
+ * A row that sees nothing (no tokens, positions below zero, pages that are none) gets zeros and -inf.
+ * Tokens without a page are not seen, positions from max_len on neither; rows that belong to nobody are
+ * left alone.  K and V count as their codes decode (not rounded to bf16); sums, maxima and normalizers are
+ * FP32, probabilities are rounded to FP16 relative to the row's largest (2^-12 each, 2^-39 absolute).
+ * A NaN or infinity in q makes its row NaN; NaN scales reach the rows that see their tokens, and no others.
+ * MXFP4 values of 2^100 or more may come out infinite; blocks of V with scale code 0 count as zeros.
+ *   ws     qf_kv_attention_workspace_size bytes of the same cache sizes, sequences' sizes (B, cols, max_len,
+ *          with or without offsets), T, Hq and window, 256-byte aligned; may be NULL where that is 0.
+ * Limits: T Hq < 2^30, Hq / H <= 512.  Deterministic: the order of the sums depends on these sizes alone.
+ */
+QF_API qf_status qf_kv_attention_workspace_size(const qf_kv_cache* c, const qf_kv_seqs* q, int64_t T,
+                                                int64_t Hq, int64_t window, size_t* bytes);
+QF_API qf_status qf_kv_attention(const qf_kv_cache* c, const qf_kv_seqs* q, int64_t T, const uint16_t* Q,
+                                 int64_t ldq, int64_t Hq, float scale, int64_t window, uint16_t* O,
+                                 int64_t ldo, float* lse, void* ws, size_t ws_bytes, qf_stream_t stream);
+
+/*
+ * The adapters of many requests beside one shared weight [N, K] (Eq. qad-lora's factors, not merged).
+ *   n       adapters; r: the rank they are stored with, a multiple of 8 up to 256.
+ *   A       bf16 [n, r, K], B bf16 [n, N, r] (the trained factors rounded), dense, 16-byte aligned; K a
+ *           multiple of 8.
+ *   scale   FP32 [n] (alpha / r).
+ *   ranks   int32 [n] or NULL (all r): adapter a uses the first ranks[a] rows of A[a] and columns of B[a],
+ *           whatever the others hold.
+ * scale and ranks need no alignment.
+ */
+typedef struct {
+    int64_t n, r, N, K;
+    const uint16_t* A;
+    const uint16_t* B;
+    const float* scale;
+    const int32_t* ranks;
+} qf_adapters;
+
+/*
+ * qf_lora_rows -- Y[m] = base[m] + scale[a] (X[m] A_a^T) B_a^T with a = ids[m].
+ *   ids    int32 [M]; a row whose id is outside 0 .. n - 1 has no adapter: Y[m] = base[m].
+ *   X      bf16 [M, K] (row stride ldx).
+ *   base   [M, N] (row stride ldb) of Y's type, the shared projection's output, or NULL (zeros).  It may be
+ *          Y itself (same stride): then rows without an adapter are left alone.  Otherwise the two must
+ *          not overlap.
+ *   Y      bf16 (y_f32 = 0) or FP32 (y_f32 = 1) [M, N] (row stride ldy).
+ *   ws     qf_lora_rows_workspace_size bytes, 256-byte aligned.
+ * Rows of an adapter may lie anywhere; they cost least side by side.  FP32 sums in a fixed order; X A^T is
+ * taken into the second product as the sum of two bf16 halves (2^-17 relative), Y rounded once.
+ * Limits: M < 2^24, N and K < 2^30, n < 2^30.
+ */
+QF_API qf_status qf_lora_rows_workspace_size(const qf_adapters* a, int64_t M, size_t* bytes);
+QF_API qf_status qf_lora_rows(const qf_adapters* a, const int32_t* ids, int64_t M, const uint16_t* X,
+                              int64_t ldx, const void* base, int64_t ldb, void* Y, int64_t ldy, int y_f32,
+                              void* ws, size_t ws_bytes, qf_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -67,6 +67,24 @@ class Packed(ctypes.Structure):
                 ("S", ctypes.c_void_p)]
 
 
+class KvCache(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int64), ("page", ctypes.c_int64), ("H", ctypes.c_int64),
+                ("D", ctypes.c_int64), ("fmt", ctypes.c_int32), ("k_codes", ctypes.c_void_p),
+                ("k_scales", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p), ("k_S", ctypes.c_void_p), ("v_S", ctypes.c_void_p)]
+
+
+class KvSeqs(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int64), ("offsets", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+                ("table", ctypes.c_void_p), ("cols", ctypes.c_int64), ("max_len", ctypes.c_int64)]
+
+
+class Adapters(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("r", ctypes.c_int64), ("N", ctypes.c_int64),
+                ("K", ctypes.c_int64), ("A", ctypes.c_void_p), ("B", ctypes.c_void_p),
+                ("scale", ctypes.c_void_p), ("ranks", ctypes.c_void_p)]
+
+
 _lib = None
 _P = ctypes.c_void_p
 _I = ctypes.c_int64
@@ -172,6 +190,18 @@ def lib() -> ctypes.CDLL:
                                  ctypes.c_int),
             "qf_packed_matvec_grouped": ([ctypes.POINTER(Packed), _P, _I, _P, _I, _I, _P, _I, _P, _I,
                                           ctypes.c_int, _P], ctypes.c_int),
+            "qf_kv_write": ([ctypes.POINTER(KvCache), ctypes.POINTER(KvSeqs), _I, _P, _I, _P, _I, _P],
+                            ctypes.c_int),
+            "qf_kv_read": ([ctypes.POINTER(KvCache), ctypes.POINTER(KvSeqs), _I, _P, _I, _P, _I, _P],
+                           ctypes.c_int),
+            "qf_kv_attention_workspace_size": ([ctypes.POINTER(KvCache), ctypes.POINTER(KvSeqs), _I, _I,
+                                                _I, ctypes.POINTER(ctypes.c_size_t)], ctypes.c_int),
+            "qf_kv_attention": ([ctypes.POINTER(KvCache), ctypes.POINTER(KvSeqs), _I, _P, _I, _I,
+                                 ctypes.c_float, _I, _P, _I, _P, _P, ctypes.c_size_t, _P], ctypes.c_int),
+            "qf_lora_rows_workspace_size": ([ctypes.POINTER(Adapters), _I,
+                                             ctypes.POINTER(ctypes.c_size_t)], ctypes.c_int),
+            "qf_lora_rows": ([ctypes.POINTER(Adapters), _P, _I, _P, _I, _P, _I, _P, _I, ctypes.c_int, _P,
+                              ctypes.c_size_t, _P], ctypes.c_int),
         }
         for name, (args, res) in sig.items():
             f = getattr(L, name)
@@ -669,6 +699,147 @@ def packed_matvec_grouped(weight: Packed, offsets, X, Y, rows=None, rows_div=1):
                                           _typed(offsets, torch.int64, "offsets", (weight.E + 1,)),
                                           R, _typed(rows, torch.int32, "rows", (R,)), rows_div, M,
                                           _ptr(X), ldx, _ptr(Y), ldy, f32, _stream()))
+    return Y
+
+
+# -------------------------------------------- the 4-bit cache of keys and values, its attention
+def _dense(t, dtype, name, shape=None):
+    """As _typed, for a tensor that has to be there."""
+    if t is None:
+        raise ValueError(f"{name} is missing")
+    return _typed(t, dtype, name, shape)
+
+
+def kv_cache(fmt, k_codes, k_scales, v_codes, v_scales, k_S=None, v_S=None) -> KvCache:
+    """Descriptor of a cache in pages: codes uint8 [pages, H, page, D/2], scales uint8 [pages, H, page, D/16]
+    (nvfp4, with the heads' tensor scales k_S, v_S float32 [H]) or [pages, H, page, D/32] (mxfp4).  It holds
+    references to the tensors, so their device memory stays allocated while the descriptor is alive."""
+    block = {"nvfp4": 16, "mxfp4": 32}[fmt]
+    if k_codes.dim() != 4:
+        raise ValueError("codes must be [pages, H, page, D/2]")
+    pages, H, page, half = k_codes.shape
+    D = 2 * half
+    codes, scales = (pages, H, page, half), (pages, H, page, D // block)
+    if fmt == "nvfp4":
+        S = _dense(k_S, torch.float32, "k_S", (H,)), _dense(v_S, torch.float32, "v_S", (H,))
+    else:
+        S = None, None
+    c = KvCache(pages, page, H, D, FMT[fmt], _dense(k_codes, torch.uint8, "k_codes", codes),
+                _dense(k_scales, torch.uint8, "k_scales", scales),
+                _dense(v_codes, torch.uint8, "v_codes", codes),
+                _dense(v_scales, torch.uint8, "v_scales", scales), *S)
+    c._tensors = (k_codes, k_scales, v_codes, v_scales, k_S, v_S)
+    return c
+
+
+def kv_sequences(lens, table, offsets=None, max_len=None) -> KvSeqs:
+    """Descriptor of the sequences of a call: lens int32 [B] tokens of each, the call's included; table int32
+    [B, cols] their pages; offsets int64 [B+1] their rows of the call (None: one each); max_len a bound on lens
+    (None: what the table's rows hold, known when a cache is).  Holds references to the tensors, whose values
+    may change between calls."""
+    B, cols = table.shape
+    q = KvSeqs(B, _typed(offsets, torch.int64, "offsets", (B + 1,)), _dense(lens, torch.int32, "lens", (B,)),
+               _dense(table, torch.int32, "table"), cols, -1 if max_len is None else max_len)
+    q._tensors = (offsets, lens, table)
+    return q
+
+
+def _bounded(cache, seqs):
+    """seqs with max_len filled in."""
+    if seqs.max_len >= 0:
+        return seqs
+    return KvSeqs(seqs.B, seqs.offsets, seqs.lens, seqs.table, seqs.cols, min(seqs.cols * cache.page, (1 << 30) - 1))
+
+
+def _heads(x, name, width=None):
+    R, C, ld = _mat(_bf16(x))
+    if width is not None and C != width:
+        raise ValueError(f"{name} must have {width} columns")
+    return R, C, ld
+
+
+def kv_write(cache: KvCache, seqs: KvSeqs, K, V):
+    """Quantizes the new tokens' K, V [T, H D] into their sequences' pages."""
+    T, C, ldk = _heads(K, "K", cache.H * cache.D)
+    T2, _, ldv = _heads(V, "V", C)
+    if T2 != T:
+        raise ValueError("K and V must have a row for every token")
+    _check(lib().qf_kv_write(ctypes.byref(cache), ctypes.byref(_bounded(cache, seqs)), T, _ptr(K), ldk, _ptr(V), ldv,
+                             _stream()))
+
+
+def kv_read(cache: KvCache, seqs: KvSeqs, K=None, V=None):
+    """The tokens' K, V [T, H D] (either may be None) as the cache holds them."""
+    T, ld = None, [0, 0]
+    for i, (x, name) in enumerate(((K, "K"), (V, "V"))):
+        if x is not None:
+            R, _, ld[i] = _heads(x, name, cache.H * cache.D)
+            if T not in (None, R):
+                raise ValueError("K and V must have a row for every token")
+            T = R
+    if T is None:
+        return K, V
+    _check(lib().qf_kv_read(ctypes.byref(cache), ctypes.byref(_bounded(cache, seqs)), T, _ptr(K), ld[0], _ptr(V), ld[1],
+                            _stream()))
+    return K, V
+
+
+def kv_attention_workspace(cache: KvCache, seqs: KvSeqs, T, Hq, window=0, device="cuda"):
+    n = ctypes.c_size_t()
+    _check(lib().qf_kv_attention_workspace_size(ctypes.byref(cache), ctypes.byref(_bounded(cache, seqs)), T, Hq, window,
+                                                ctypes.byref(n)))
+    return torch.empty(max(n.value, 256), dtype=torch.uint8, device=device)
+
+
+def kv_attention(cache: KvCache, seqs: KvSeqs, Q, O, ws, scale=None, window=0, lse=None):
+    """Causal attention of Q [T, Hq D] over the cached tokens into O [T, Hq D] and lse float32 [T, Hq]; scale
+    None: 1 / sqrt D; window > 0: only the last `window` positions up to a token's own."""
+    T, C, ldq = _heads(Q, "Q")
+    T2, _, ldo = _heads(O, "O", C)
+    if T2 != T:
+        raise ValueError("O must have the shape of Q")
+    if C % cache.D:
+        raise ValueError("Q must be [T, Hq D]")
+    Hq = C // cache.D
+    _check(lib().qf_kv_attention(ctypes.byref(cache), ctypes.byref(_bounded(cache, seqs)), T, _ptr(Q), ldq, Hq,
+                                 cache.D ** -0.5 if scale is None else float(scale), window, _ptr(O), ldo,
+                                 _typed(lse, torch.float32, "lse", (T, Hq)), _ptr(ws), ws.numel() * ws.element_size(),
+                                 _stream()))
+    return O
+
+
+# ------------------------------------------------- adapters of many requests, not merged
+def adapters(A, B, scale, ranks=None) -> Adapters:
+    """Descriptor of n adapters beside one weight [N, K]: A bf16 [n, r, K], B bf16 [n, N, r], scale float32 [n],
+    ranks int32 [n] (None: all r).  Holds references to the tensors."""
+    n, r, K = A.shape
+    N = B.shape[1]
+    a = Adapters(n, r, N, K, _dense(_bf16(A), A.dtype, "A"), _dense(_bf16(B), B.dtype, "B", (n, N, r)),
+                 _dense(scale, torch.float32, "scale", (n,)), _typed(ranks, torch.int32, "ranks", (n,)))
+    a._tensors = (A, B, scale, ranks)
+    return a
+
+
+def lora_rows_workspace(a: Adapters, M, device="cuda"):
+    n = ctypes.c_size_t()
+    _check(lib().qf_lora_rows_workspace_size(ctypes.byref(a), M, ctypes.byref(n)))
+    return torch.empty(max(n.value, 256), dtype=torch.uint8, device=device)
+
+
+def lora_rows(a: Adapters, ids, X, Y, ws, base=None):
+    """Y [M, N] (bf16 or float32) = base + scale[a] (X A_a^T) B_a^T with a = ids[m] (int32 [M], outside 0 .. n - 1:
+    none).  base: of Y's type, may be Y itself; None: zeros."""
+    M, K, ldx = _mat(_bf16(X))
+    R, N, ldy, f32 = _products(Y)
+    if (R, N, K) != (M, a.N, a.K):
+        raise ValueError("X must be [M, K] and Y [M, N]")
+    ldb = 0
+    if base is not None:
+        R2, N2, ldb, f2 = _products(base)
+        if (R2, N2, f2) != (R, N, f32):
+            raise ValueError("base must have the shape and type of Y")
+    _check(lib().qf_lora_rows(ctypes.byref(a), _dense(ids, torch.int32, "ids", (M,)), M, _ptr(X), ldx, _ptr(base), ldb,
+                              _ptr(Y), ldy, f32, _ptr(ws), ws.numel() * ws.element_size(), _stream()))
     return Y
 
 

@@ -10,6 +10,7 @@
 
 #include "qf.h"
 #include "qf_internal.h"
+#include "qf_kv.h"
 
 namespace {
 
@@ -1868,6 +1869,173 @@ qf_status qf_packed_matvec_grouped(const qf_packed* w, const int64_t* group_offs
   QF_TRY(check_packed_call(fn, w, R, M, X, ldx, Y, ldy, y_f32));
   QF_TRY(dev(qf::launch_packed_matvec(packed_op(w), group_offsets, R, rows, rows_div, M, X, ldx, Y,
                                       ldy, y_f32, S(stream)), fn));
+  return ok();
+}
+
+// ------------------------------------------- the 4-bit cache, its attention, and many adapters
+namespace {
+
+bool aligned_to(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+
+qf_status check_cache(const char* fn, const qf_kv_cache* c) {
+  if (!c) return fail(QF_EINVAL, "%s: null cache", fn);
+  if (c->fmt != QF_FMT_NVFP4 && c->fmt != QF_FMT_MXFP4) return fail(QF_EINVAL, "%s: bad format %d", fn, c->fmt);
+  if (c->pages < 0 || c->H < 0) return fail(QF_ESHAPE, "%s: negative shape", fn);
+  if (c->page < 16 || c->page > 1024 || (c->page & (c->page - 1)))
+    return fail(QF_ENOTSUP, "%s: pages of %lld tokens, not 16, 32 .. 1024", fn, (long long)c->page);
+  if (c->D != 64 && c->D != 128 && c->D != 256)
+    return fail(QF_ENOTSUP, "%s: heads of %lld, not 64, 128 or 256", fn, (long long)c->D);
+  if (c->H >= (1 << 20) / c->D) return fail(QF_ENOTSUP, "%s: 2^20 columns of keys or more", fn);
+  if (c->pages > INT32_MAX) return fail(QF_ENOTSUP, "%s: 2^31 pages or more", fn);
+  return QF_OK;
+}
+
+// The cache's tensors and the sequences' arrays (of a call that has rows).
+qf_status check_kv_call(const char* fn, const qf_kv_cache* c, const qf_kv_seqs* q) {
+  if (c->pages > 0) {
+    if (!c->k_codes || !c->k_scales || !c->v_codes || !c->v_scales) return fail(QF_EINVAL, "%s: null codes or scales", fn);
+    for (const void* p : {(const void*)c->k_codes, (const void*)c->k_scales, (const void*)c->v_codes, (const void*)c->v_scales})
+      QF_TRY(check_out(fn, p));
+  }
+  if (c->fmt == QF_FMT_NVFP4 && (!c->k_S || !c->v_S)) return fail(QF_EINVAL, "%s: NVFP4 needs the heads' scales k_S and v_S", fn);
+  if (!q->lens || (q->cols > 0 && !q->table)) return fail(QF_EINVAL, "%s: null lens or table", fn);
+  if (!aligned_to(q->lens, 4) || !aligned_to(q->table, 4) || !aligned_to(q->offsets, 8))
+    return fail(QF_EALIGN, "%s: lens, table or offsets not aligned to their elements", fn);
+  return QF_OK;
+}
+
+qf_status check_seqs(const char* fn, const qf_kv_seqs* q, int64_t T) {
+  if (!q) return fail(QF_EINVAL, "%s: null sequences", fn);
+  if (T < 0 || q->B < 0 || q->cols < 0 || q->max_len < 0) return fail(QF_ESHAPE, "%s: negative shape", fn);
+  if (T >= 1 << 28 || q->B >= 1 << 28) return fail(QF_ENOTSUP, "%s: 2^28 rows or sequences or more", fn);
+  if (q->cols > INT32_MAX) return fail(QF_ENOTSUP, "%s: 2^31 pages a sequence or more", fn);
+  if (q->max_len >= 1 << 30) return fail(QF_ENOTSUP, "%s: sequences of 2^30 tokens or more", fn);
+  if (!q->offsets && T != q->B)
+    return fail(QF_ESHAPE, "%s: %lld rows for %lld sequences without offsets", fn, (long long)T, (long long)q->B);
+  return QF_OK;
+}
+
+qf::KvCache cache_of(const qf_kv_cache* c) {
+  int log = 4;
+  while (((int64_t)1 << log) < c->page) ++log;
+  return {{c->k_codes, c->v_codes}, {c->k_scales, c->v_scales}, {c->k_S, c->v_S}, c->pages, (int)c->H, (int)c->D, log, c->fmt};
+}
+qf::KvSeqs seqs_of(const qf_kv_seqs* q, int64_t T) { return {q->offsets, q->lens, q->table, q->cols, q->B, T}; }
+
+qf_status check_attention(const char* fn, const qf_kv_cache* c, const qf_kv_seqs* q, int64_t T, int64_t Hq, int64_t window) {
+  QF_TRY(check_cache(fn, c));
+  QF_TRY(check_seqs(fn, q, T));
+  if (Hq < 0 || window < 0) return fail(QF_ESHAPE, "%s: negative shape", fn);
+  if (c->H == 0 ? Hq != 0 : Hq % c->H != 0)
+    return fail(QF_ESHAPE, "%s: %lld heads of queries over %lld of keys", fn, (long long)Hq, (long long)c->H);
+  if (c->H > 0 && Hq / c->H > 512) return fail(QF_ENOTSUP, "%s: more than 512 heads of queries to one of keys", fn);
+  if (Hq > 0 && T >= (1 << 30) / Hq) return fail(QF_ENOTSUP, "%s: 2^30 rows of queries or more", fn);
+  return QF_OK;
+}
+
+}  // namespace
+
+qf_status qf_kv_write(const qf_kv_cache* c, const qf_kv_seqs* q, int64_t T, const uint16_t* K, int64_t ldk,
+                      const uint16_t* V, int64_t ldv, qf_stream_t stream) {
+  const char* fn = "qf_kv_write";
+  QF_TRY(check_cache(fn, c));
+  QF_TRY(check_seqs(fn, q, T));
+  QF_TRY(check_mat("qf_kv_write: K", K, T, c->H * c->D, ldk, true));
+  QF_TRY(check_mat("qf_kv_write: V", V, T, c->H * c->D, ldv, true));
+  if (T == 0 || c->H == 0 || q->B == 0) return ok();
+  QF_TRY(check_kv_call(fn, c, q));
+  QF_TRY(dev(qf::launch_kv_write(cache_of(c), seqs_of(q, T), K, ldk, V, ldv, S(stream)), fn));
+  return ok();
+}
+
+qf_status qf_kv_read(const qf_kv_cache* c, const qf_kv_seqs* q, int64_t T, uint16_t* K, int64_t ldk, uint16_t* V,
+                     int64_t ldv, qf_stream_t stream) {
+  const char* fn = "qf_kv_read";
+  QF_TRY(check_cache(fn, c));
+  QF_TRY(check_seqs(fn, q, T));
+  QF_TRY(check_mat("qf_kv_read: K", K, T, c->H * c->D, ldk, false));
+  QF_TRY(check_mat("qf_kv_read: V", V, T, c->H * c->D, ldv, false));
+  if (T == 0 || c->H == 0 || q->B == 0 || (!K && !V)) return ok();
+  QF_TRY(check_kv_call(fn, c, q));
+  QF_TRY(dev(qf::launch_kv_read(cache_of(c), seqs_of(q, T), K, ldk, V, ldv, S(stream)), fn));
+  return ok();
+}
+
+qf_status qf_kv_attention_workspace_size(const qf_kv_cache* c, const qf_kv_seqs* q, int64_t T, int64_t Hq,
+                                         int64_t window, size_t* bytes) {
+  const char* fn = "qf_kv_attention_workspace_size";
+  QF_TRY(check_attention(fn, c, q, T, Hq, window));
+  if (!bytes) return fail(QF_EINVAL, "%s: null output", fn);
+  *bytes = 0;
+  if (T > 0 && Hq > 0 && q->B > 0)
+    *bytes = up(qf::kv_attention_ws_bytes(cache_of(c), seqs_of(q, T), {nullptr, 0, nullptr, 0, nullptr, Hq, q->max_len, window, 0.0f}));
+  return ok();
+}
+
+qf_status qf_kv_attention(const qf_kv_cache* c, const qf_kv_seqs* q, int64_t T, const uint16_t* Q, int64_t ldq,
+                          int64_t Hq, float scale, int64_t window, uint16_t* O, int64_t ldo, float* lse, void* ws,
+                          size_t ws_bytes, qf_stream_t stream) {
+  const char* fn = "qf_kv_attention";
+  QF_TRY(check_attention(fn, c, q, T, Hq, window));
+  QF_TRY(check_mat("qf_kv_attention: Q", Q, T, Hq * c->D, ldq, true));
+  QF_TRY(check_mat("qf_kv_attention: O", O, T, Hq * c->D, ldo, true));
+  QF_TRY(check_out("qf_kv_attention: lse", lse));
+  if (T == 0 || Hq == 0 || q->B == 0) return ok();
+  QF_TRY(check_kv_call(fn, c, q));
+  const qf::KvCache kc = cache_of(c);
+  const qf::KvSeqs ks = seqs_of(q, T);
+  const qf::AttendCall call{Q, ldq, O, ldo, lse, Hq, q->max_len, window, scale};
+  const size_t need = qf::kv_attention_ws_bytes(kc, ks, call);
+  if (need > 0) QF_TRY(check_ws(fn, need, ws, ws_bytes));
+  QF_TRY(dev(qf::launch_kv_attention(kc, ks, call, static_cast<float*>(ws), S(stream)), fn));
+  return ok();
+}
+
+namespace {
+
+qf_status check_adapters(const char* fn, const qf_adapters* a, int64_t M) {
+  if (!a) return fail(QF_EINVAL, "%s: null adapters", fn);
+  if (a->n < 0 || a->N < 0 || a->K < 0 || M < 0) return fail(QF_ESHAPE, "%s: negative shape", fn);
+  if (a->r < 8 || a->r > 256 || a->r % 8) return fail(QF_ENOTSUP, "%s: rank %lld, not a multiple of 8 up to 256", fn, (long long)a->r);
+  if (a->K % 8) return fail(QF_ESHAPE, "%s: K=%lld is not a multiple of 8", fn, (long long)a->K);
+  if (M >= 1 << 24) return fail(QF_ENOTSUP, "%s: 2^24 rows or more", fn);
+  if (a->N >= 1 << 30 || a->K >= 1 << 30 || a->n >= 1 << 30) return fail(QF_ENOTSUP, "%s: N, K or n of 2^30 or more", fn);
+  return QF_OK;
+}
+
+qf::AdapterSet adapter_set(const qf_adapters* a) { return {a->n, a->N, a->K, (int)a->r, a->A, a->B, a->scale, a->ranks}; }
+
+}  // namespace
+
+qf_status qf_lora_rows_workspace_size(const qf_adapters* a, int64_t M, size_t* bytes) {
+  const char* fn = "qf_lora_rows_workspace_size";
+  QF_TRY(check_adapters(fn, a, M));
+  if (!bytes) return fail(QF_EINVAL, "%s: null output", fn);
+  *bytes = M == 0 ? 0 : up(qf::lora_rows_ws_bytes(adapter_set(a), M));
+  return ok();
+}
+
+qf_status qf_lora_rows(const qf_adapters* a, const int32_t* ids, int64_t M, const uint16_t* X, int64_t ldx,
+                       const void* base, int64_t ldb, void* Y, int64_t ldy, int y_f32, void* ws, size_t ws_bytes,
+                       qf_stream_t stream) {
+  const char* fn = "qf_lora_rows";
+  QF_TRY(check_adapters(fn, a, M));
+  if (y_f32 != 0 && y_f32 != 1) return fail(QF_EINVAL, "%s: y_f32 must be 0/1", fn);
+  QF_TRY(check_mat("qf_lora_rows: X", X, M, a->K, ldx, true));
+  QF_TRY(check_mat("qf_lora_rows: base", base, M, a->N, ldb, false));
+  QF_TRY(check_mat("qf_lora_rows: Y", Y, M, a->N, ldy, true));
+  if (M == 0 || a->N == 0) return ok();
+  if (base == Y && ldb != ldy) return fail(QF_EINVAL, "%s: base is Y with another row stride", fn);
+  if (!ids) return fail(QF_EINVAL, "%s: null ids", fn);
+  if (!aligned_to(ids, 4) || !aligned_to(a->scale, 4) || !aligned_to(a->ranks, 4))
+    return fail(QF_EALIGN, "%s: ids, scale or ranks not aligned to their elements", fn);
+  if (a->n > 0) {
+    if ((a->K > 0 && !a->A) || !a->B || !a->scale) return fail(QF_EINVAL, "%s: null factors or scale", fn);
+    QF_TRY(check_out("qf_lora_rows: A", a->A));
+    QF_TRY(check_out("qf_lora_rows: B", a->B));
+  }
+  QF_TRY(check_ws(fn, qf::lora_rows_ws_bytes(adapter_set(a), M), ws, ws_bytes));
+  QF_TRY(dev(qf::launch_lora_rows(adapter_set(a), ids, M, X, ldx, base, ldb, Y, ldy, y_f32, static_cast<float*>(ws), S(stream)), fn));
   return ok();
 }
 

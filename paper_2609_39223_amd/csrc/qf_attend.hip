@@ -1,0 +1,740 @@
+// Attention of new tokens over the 4-bit cache of keys and values (qf_kv.h):
+//   z_t = scale q . k_t,  O = sum exp(z_t - lse) v_t,  lse = log sum exp z_t
+// over the positions t that the query sees, in one pass with a running maximum and sum.
+//
+// A workgroup takes 16 NQ rows, the queries of tpt tokens and Gg heads that share a head of the cache,
+// and a piece of the tokens they see; each of its four waves takes a quarter of the piece on its own, 64
+// tokens at a time, and their sums meet in LDS.  Pieces of one row meet in a second kernel (merge).
+// On v_mfma_f32_16x16x32 both products are taken transposed, Z^T = K Q^T and O^T = V^T P^T: a row's
+// scores, maximum, sum and outputs then all belong to lane % 16, so P goes from the first product
+// into the second without leaving its registers.
+//   K  lane (token l16, group g) holds d = g D / 4 ..: a token's bytes as they lie in memory, four
+//      groups side by side.  (Any bijection of d is fine as long as Q uses it.)
+//   V  64 tokens' codes go through LDS and are read back transposed (ds_read_b64_tr_b4): lane (d l16,
+//      g) gets the 16 tokens 16 u + 4 g + i, which are the ones whose P it holds.
+// What is exact:  NVFP4  V s in FP16 (E2M1 has 2 significant bits, E4M3 4; 2^-10 <= |V s| <= 2688); the
+// head's S multiplies scores and outputs.  Queries are FP16 (MXFP4: bf16), each row times a power of two that
+// takes its largest element to 2^14 .. 2^15: bits below 2^-38 of that are lost, less than FP32 sums lose.
+//                 MXFP4  keys V 2^p in bf16.  Values V 2^(p + 6) in FP16 for
+// -20 <= p <= 7; blocks with any other scale (but 0, the code of a block of zeros), and under both
+// formats blocks with NaN scales, are "special" and added one by one in FP32, which also keeps an
+// infinity or NaN away from the rows that do not see it.
+// Probabilities are rounded to FP16 as 2^14 exp(z - max): relative 2^-12 down to 2^-28 of the row's
+// largest and absolute 2^-39 of it below, so that many small ones still sum.  The sum of
+// probabilities is of the unrounded ones, in FP32.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "qf.h"
+#include "qf_codecs.h"
+#include "qf_internal.h"
+#include "qf_kv.h"
+
+#define QF_LDS(T, p) ((__attribute__((address_space(3))) T*)(p))
+
+namespace qf {
+namespace {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef int v2i_t __attribute__((ext_vector_type(2)));
+
+constexpr int kWaves = 4, kTile = 64;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
+constexpr float kUp = 14.0f;                 // probabilities are held 2^14 times as large
+
+struct AttendArgs {
+  KvCache c;
+  KvSeqs q;
+  AttendCall a;
+  int G, Gg, groups;                         // queries' heads to a cache head, of them in a row tile
+  int tpt;                                   // tokens in a row tile
+  int splits, chunk;                         // pieces a row tile's tokens may have, their size
+  int most, window;                          // positions from `most` on are not looked at
+  int item0;
+  float* part;                               // [splits, T Hq, D], then (m, l) [splits, T Hq, 2]
+};
+
+__device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
+
+// The sequence of row tile `item` and the tile's index in it: tiles of sequence b are those from
+// off[b] / tpt + b on, which leaves one too many at most.  Every wave finds it by itself, 64 steps at a
+// time.  False if the tile does not exist.
+__device__ __forceinline__ bool find_tile(const KvSeqs& q, int tpt, int item, int& b, int& tok0, int& first, int& n) {
+  if (q.off == nullptr) {
+    b = tok0 = item;
+    first = 0;
+    n = 1;
+    return item < q.B;
+  }
+  const int lane = threadIdx.x & 63;
+  auto off = [&](int i) { return (int)min(max(q.off[i], (int64_t)0), q.T); };
+  int lo = 0, hi = (int)q.B;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 63) / 64, i = lo + lane * step;
+    const bool below = i < hi && off(i) / tpt + i <= item;
+    const int k = __popcll(__ballot(below));
+    if (k == 0) return false;
+    lo += (k - 1) * step;
+    hi = min(lo + step, hi);
+  }
+  b = __builtin_amdgcn_readfirstlane(lo);
+  const int o = __builtin_amdgcn_readfirstlane(off(b));
+  n = __builtin_amdgcn_readfirstlane(off(b + 1)) - o;
+  first = (item - (o / tpt + b)) * tpt;
+  tok0 = o + first;
+  return b < q.B && first >= 0 && first < n;
+}
+
+// The positions [lo, hi) that any row of a tile sees; lo is a multiple of 16.
+struct Reach {
+  int lo, hi;
+};
+__device__ __forceinline__ Reach reach_of(const AttendArgs& p, int len, int pos0, int pos1) {
+  Reach r;
+  r.hi = min(min(pos1 + 1, len), p.most);
+  r.lo = p.window > 0 ? max(pos0 - p.window + 1, 0) & ~15 : 0;
+  return r;
+}
+__device__ __forceinline__ int live_pieces(const Reach& r, int chunk) {
+  return r.hi > r.lo ? (r.hi - r.lo - 1) / chunk + 1 : 0;
+}
+
+template <int FMT>
+__device__ __forceinline__ f32x4_t mfma_z(uint4 a, uint4 b, f32x4_t c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  if constexpr (FMT == QF_FMT_NVFP4)
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+#else
+  return c;
+#endif
+}
+__device__ __forceinline__ f32x4_t mfma_o(uint4 a, uint4 b, f32x4_t c) {
+  return mfma_z<QF_FMT_NVFP4>(a, b, c);
+}
+
+// Eight codes as FP16, pairs times the scale pairs s[0..3].
+__device__ __forceinline__ uint4 decode_f16(uint32_t cw, const f16x2_t s[4]) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const f16x2_t v0 = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(cw, 1.0f, 0)) * s[0];
+  const f16x2_t v1 = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(cw, 1.0f, 1)) * s[1];
+  const f16x2_t v2 = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(cw, 1.0f, 2)) * s[2];
+  const f16x2_t v3 = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(cw, 1.0f, 3)) * s[3];
+  return make_uint4(__builtin_bit_cast(uint32_t, v0), __builtin_bit_cast(uint32_t, v1), __builtin_bit_cast(uint32_t, v2),
+                    __builtin_bit_cast(uint32_t, v3));
+#else
+  return make_uint4(0, 0, 0, 0);
+#endif
+}
+// The E4M3 values of the low two bytes of w.
+__device__ __forceinline__ f16x2_t e4m3_f16(uint32_t w) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_bit_cast(f16x2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, false));
+#else
+  return f16x2_t{};
+#endif
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const f32x2_t v = {a, b};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2_t));
+}
+
+// Scale codes of V that the products do not take.
+template <int FMT>
+__device__ __forceinline__ bool is_special(uint32_t e) {
+  return FMT == QF_FMT_NVFP4 ? (e & 0x7Fu) == 0x7Fu : e != 0u && (e < 107u || e > 134u);
+}
+
+// What one lane holds of 64 tokens on their way in: a quarter of the bytes of 4 x 16 tokens.
+template <int FMT, int D>
+struct Tile {
+  static constexpr int W = D / 32;           // words of codes of a token's quarter
+  static constexpr int KS = FMT == QF_FMT_NVFP4 ? D / 64 : D == 256 ? 2 : 1;     // scale bytes of it
+  static constexpr int VS = FMT == QF_FMT_NVFP4 ? D / 16 : D / 32;               // scale bytes of a token
+  uint32_t k[4][W], v[4][W], ks[4], vs[4];
+};
+
+template <int W>
+__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w) {
+  if constexpr (W == 2) {
+    const uint2 x = *reinterpret_cast<const uint2*>(p);
+    w[0] = x.x;
+    w[1] = x.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < W / 4; ++i) {
+      const uint4 x = *reinterpret_cast<const uint4*>(p + 16 * i);
+      w[4 * i] = x.x;
+      w[4 * i + 1] = x.y;
+      w[4 * i + 2] = x.z;
+      w[4 * i + 3] = x.w;
+    }
+  }
+}
+
+// V's codes in LDS: row r (16 u + 4 g + i) of D / 2 bytes, its 8-byte unit c at c ^ swap(r).  A
+// transposed read takes one unit of 16 rows, four consecutive ones of each u: with the units
+// exchanged by u (and, where four rows pass 256 bytes, by i) they lie on different banks.
+template <int D>
+__device__ __forceinline__ int v_swap(int r) {
+  const int u = r >> 4;
+  return D == 64 ? u : D == 128 ? u << 1 : (u << 1) ^ ((r & 2) << 2);
+}
+
+template <int FMT, int D, int NQ>
+__global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs p) {
+  typedef Tile<FMT, D> T;
+  constexpr int NB = T::VS, CS = D / 32, DT = D / 16;   // V's blocks, steps of a score, tiles of d
+  constexpr int kCodes = kTile * D / 2, kStage = kCodes + NB * kTile * 2;   // a wave's LDS: codes, scales in FP16
+  constexpr int kSum = NQ * DT * 64 * 16;               // a wave's outputs on their way to another's
+  __shared__ __align__(16) char smem[std::max(kWaves * kStage, 2 * kSum)];
+  __shared__ float rows_m[kWaves][16 * NQ], rows_l[kWaves][16 * NQ];
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, g = lane >> 4;
+  const KvCache& c = p.c;
+  uint32_t bid = blockIdx.x;
+  const int h = (int)(bid % (uint32_t)c.H);
+  bid /= (uint32_t)c.H;
+  const int grp = (int)(bid % (uint32_t)p.groups);
+  bid /= (uint32_t)p.groups;
+  const int split = (int)(bid % (uint32_t)p.splits);
+  int b, tok0, first, n;
+  if (!find_tile(p.q, p.tpt, p.item0 + (int)(bid / (uint32_t)p.splits), b, tok0, first, n)) return;
+
+  const int page_log = c.page_log;
+  const int len = max(p.q.lens[b], 0), pos0 = len - n + first, toks = min(p.tpt, n - first);
+  const Reach reach = reach_of(p, len, pos0, pos0 + toks - 1);
+  const int live = live_pieces(reach, p.chunk);
+  if (split >= live && p.splits > 1) return;            // (the merge leaves such pieces out)
+
+  // this lane's row of each 16
+  int row_at[NQ], row_pos[NQ];                          // row of [T, Hq]; position
+  bool row_ok[NQ];
+  uint4 qf[NQ][CS];
+  float cz[NQ];                                         // times this scores are in units of log 2; positive
+  const float S_k = FMT == QF_FMT_NVFP4 ? c.S[0][h] : 1.0f;
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    const int r = 16 * j + l16, i = r / p.Gg, gh = grp * p.Gg + r % p.Gg;
+    row_ok[j] = i < toks && gh < p.G;
+    row_pos[j] = pos0 + (row_ok[j] ? i : toks - 1);     // (what a row that is none sees is not stored)
+    const int t = tok0 + (row_ok[j] ? i : 0), hq = h * p.G + (row_ok[j] ? gh : 0);
+    row_at[j] = t * (int)p.a.Hq + hq;
+    const uint16_t* const src = p.a.Q + t * p.a.ldq + (int64_t)hq * D + g * (D / 4);
+    const uint32_t flip = p.a.scale * S_k < 0.0f ? 0x80008000u : 0u;
+    uint32_t top = 0;
+#pragma unroll
+    for (int s = 0; s < CS; ++s) {
+      qf[j][s] = *reinterpret_cast<const uint4*>(src + 8 * s);
+      uint32_t w[8];
+      codec::unpack8(qf[j][s], w);
+      top = max(top, codec::max_abs_bits8(w));
+      qf[j][s] = make_uint4(qf[j][s].x ^ flip, qf[j][s].y ^ flip, qf[j][s].z ^ flip, qf[j][s].w ^ flip);
+    }
+    top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+    float f = __builtin_fabsf(p.a.scale * S_k) * kLog2e;
+    const int e = (int)(top >> 7) - 127 - 14;           // (zeros and subnormals: any factor will do)
+#pragma unroll
+    for (int s = 0; s < CS; ++s) {
+      const uint32_t w[4] = {qf[j][s].x, qf[j][s].y, qf[j][s].z, qf[j][s].w};
+      uint32_t o[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float lo = __builtin_ldexpf(codec::as_f32(w[k] << 16), -e), hi = __builtin_ldexpf(codec::as_f32(w[k] & 0xFFFF0000u), -e);
+        o[k] = FMT == QF_FMT_NVFP4 ? pack_f16(lo, hi) : codec::bf16x2_rne_nonnan(lo, hi);
+      }
+      qf[j][s] = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+    f = __builtin_ldexpf(f, e);
+    // a query with an infinity or NaN: NaN; never zero, so that hidden scores stay -inf
+    cz[j] = top >= 0x7F80u ? __builtin_nanf("") : f < 0x1p-126f ? 0x1p-126f : f;
+  }
+
+  float m[NQ], l[NQ];
+  f32x4_t acc[NQ][DT];
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    m[j] = neg_inf();
+    l[j] = 0.0f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[j][d] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+
+  // this wave's tokens
+  const int a0 = reach.lo + split * p.chunk, a1 = min(a0 + p.chunk, reach.hi);
+  const int per = (max(a1 - a0, 0) + kWaves * kTile - 1) / (kWaves * kTile) * kTile;
+  const int w0 = a0 + wv * per, todo = max(min(w0 + per, a1) - w0, 0);
+
+  char* const mine = smem + wv * kStage;
+  _Float16* const vscale = reinterpret_cast<_Float16*>(mine + kCodes);
+
+  if (todo > 0) {
+    // ids of 64 pages in the lanes of one register, -1 for a bad one
+    const int page_first = w0 >> page_log, page_last = (w0 + todo - 1) >> page_log;
+    const int32_t* const table = p.q.table + b * p.q.cols;
+    int page_base = page_first, ids = -1;
+    auto fetch_ids = [&](int base) {
+      const int id = table[min(base + lane, page_last)];
+      page_base = base;
+      ids = id >= 0 && id < c.pages ? id : -1;
+    };
+    fetch_ids(page_first);
+
+    T x;
+    uint32_t bad_now = 0, bad_next = 0;                 // bit u: the tile's tokens 16 u .. have no page
+    constexpr int SB = T::VS;                           // scale bytes of a token
+    const uint32_t row_k = l16 * (D / 2) + g * (D / 8), row_v = (lane >> 2) * (D / 2) + (lane & 3) * (D / 8);
+    auto quarter = [&](int q4) { return FMT == QF_FMT_MXFP4 && D == 64 ? q4 >> 1 : q4 * T::KS; };
+    const uint32_t row_ks = l16 * SB + quarter(g), row_vs = (lane >> 2) * SB + quarter(lane & 3);
+    auto load_scales = [&](const uint8_t* sp) -> uint32_t {
+      return T::KS == 4 ? *reinterpret_cast<const uint32_t*>(sp) : T::KS == 2 ? *reinterpret_cast<const uint16_t*>(sp) : *sp;
+    };
+
+    // where the 16 tokens from w0 + t on lie, counted in tokens; past the end the last ones again
+    auto place = [&](int t) -> int64_t {
+      const int pos = w0 + min(t, (todo - 1) & ~15);
+      const int id = __builtin_amdgcn_readlane(ids, (pos >> page_log) - page_base);
+      return id < 0 ? -1 : (((int64_t)id * c.H + h) << page_log) + (pos & ((1 << page_log) - 1));
+    };
+    auto load_k = [&](int t) {
+      if (((w0 + min(t + 48, (todo - 1) & ~15)) >> page_log) - page_base >= 64) fetch_ids((w0 + t) >> page_log);
+      bad_next = 0;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        int64_t at = place(t + 16 * u);
+        if (at < 0) {
+          bad_next |= 1u << u;
+          at = 0;
+        }
+        load_words<T::W>(c.codes[0] + at * (D / 2) + row_k, x.k[u]);
+        x.ks[u] = load_scales(c.scales[0] + at * SB + row_ks);
+      }
+    };
+    auto load_v = [&](int t) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int64_t at = max(place(t + 16 * u), (int64_t)0);
+        load_words<T::W>(c.codes[1] + at * (D / 2) + row_v, x.v[u]);
+        x.vs[u] = load_scales(c.scales[1] + at * SB + row_vs);
+      }
+    };
+
+    load_k(0);
+    load_v(0);
+    for (int t0 = 0; t0 < todo; t0 += kTile) {
+      bad_now = bad_next;
+      // ---- scores
+      float z[NQ][16];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        f32x4_t zz[NQ];
+#pragma unroll
+        for (int j = 0; j < NQ; ++j) zz[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        f16x2_t s2[2] = {};
+#pragma unroll
+        for (int s = 0; s < CS; ++s) {
+          uint4 a;
+          if constexpr (FMT == QF_FMT_NVFP4) {
+            if ((s & 3) == 0) {                         // scale bytes of 32 elements
+              const f16x2_t v = e4m3_f16(x.ks[u] >> (8 * (s >> 1)));
+              s2[0] = f16x2_t{v[0], v[0]};
+              s2[1] = f16x2_t{v[1], v[1]};
+            }
+            const f16x2_t q2 = s2[(s >> 1) & 1], q4[4] = {q2, q2, q2, q2};
+            a = decode_f16(x.k[u][s], q4);
+          } else {
+            uint32_t w[4];
+            codec::fp4_decode8(x.k[u][s], codec::e8m0_scale((x.ks[u] >> (8 * (s >> 2))) & 0xFFu), w);
+            a = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+#pragma unroll
+          for (int j = 0; j < NQ; ++j) zz[j] = mfma_z<FMT>(a, qf[j][s], zz[j]);
+        }
+        uint32_t nan_rows = 0;                          // MXFP4: tokens with a NaN scale
+        if constexpr (FMT == QF_FMT_MXFP4) {
+          const bool bad = (x.ks[u] & 0xFFu) == 0xFFu || (T::KS == 2 && (x.ks[u] >> 8) == 0xFFu);
+          const uint64_t all = __ballot(bad);
+          nan_rows = (uint32_t)(all | (all >> 16) | (all >> 32) | (all >> 48)) & 0xFFFFu;
+        }
+#pragma unroll
+        for (int j = 0; j < NQ; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            z[j][4 * u + i] = zz[j][i];
+            if (nan_rows && ((nan_rows >> (4 * g + i)) & 1u)) z[j][4 * u + i] = __builtin_nanf("");
+          }
+      }
+      // ---- V's codes to LDS, and the loads of the next 64 tokens
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int r = 16 * u + (lane >> 2), sw = v_swap<D>(r);
+        char* const to = mine + r * (D / 2);
+        if constexpr (D == 64) {
+          *reinterpret_cast<uint2*>(to + 8 * ((lane & 3) ^ sw)) = make_uint2(x.v[u][0], x.v[u][1]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < D / 128; ++i)
+            *reinterpret_cast<uint4*>(to + 8 * (((lane & 3) * (D / 64) + 2 * i) ^ sw)) =
+                make_uint4(x.v[u][4 * i], x.v[u][4 * i + 1], x.v[u][4 * i + 2], x.v[u][4 * i + 3]);
+        }
+      }
+      // the scales, in the order in which the products take them; zeros for tokens that no row sees and
+      // for special ones
+      uint32_t special = 0;                             // bit u: one of this quarter of token 16 u + lane / 4
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const bool seen = t0 + 16 * u + (lane >> 2) < todo && !((bad_now >> u) & 1u);
+        uint32_t sv = seen ? x.vs[u] : 0u;
+#pragma unroll
+        for (int k = 0; k < T::KS; ++k)
+          if (is_special<FMT>((sv >> (8 * k)) & 0xFFu)) {
+            sv &= ~(0xFFu << (8 * k));
+            special |= 1u << u;
+          }
+        // token 16 u + 4 gg + i % 4 lies at i = 4 u + i % 4 of the lanes of group gg
+        _Float16* const to = vscale + (quarter(lane & 3) * 4 + (lane >> 4)) * 16 + 4 * u + ((lane >> 2) & 3);
+#pragma unroll
+        for (int k = 0; k < T::KS; k += 2) {
+          uint32_t w;
+          if constexpr (FMT == QF_FMT_NVFP4) {
+            w = __builtin_bit_cast(uint32_t, e4m3_f16(sv >> (8 * k)));
+          } else {                                      // 2^(e - 127 + 6): exponent field e - 106
+            const uint32_t lo = (sv >> (8 * k)) & 0xFFu, hi = (sv >> (8 * k + 8)) & 0xFFu;
+            w = (lo ? (lo - 106u) << 10 : 0u) | (hi ? (hi - 106u) << 26 : 0u);
+          }
+          to[k * 64] = __builtin_bit_cast(f16x2_t, w)[0];
+          if (k + 1 < T::KS) to[k * 64 + 64] = __builtin_bit_cast(f16x2_t, w)[1];
+        }
+      }
+      if (t0 + kTile < todo) {
+        load_k(t0 + kTile);
+        load_v(t0 + kTile);
+      }
+      // ---- which positions a row sees, its maximum, its probabilities
+      const int base = w0 + t0;
+      const bool whole = t0 + kTile <= todo && bad_now == 0;
+      uint32_t pw[NQ][8];
+#pragma unroll
+      for (int j = 0; j < NQ; ++j) {
+        // this lane's tokens are 16 u + 4 g + i; it sees them from `from` to below `to`
+        const int to = min(row_pos[j] + 1 - base, todo - t0);
+        const int from = p.window > 0 ? row_pos[j] - p.window + 1 - base : 0;
+        if (!(whole && __all(to >= kTile && from <= 0))) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int t = 16 * (i >> 2) + 4 * g + (i & 3);
+            if (t < from || t >= to || ((bad_now >> (i >> 2)) & 1u)) z[j][i] = neg_inf();
+          }
+        }
+        float top = z[j][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, z[j][i]);
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        // the reference is a whole number, so that adding it to 14 and powers of two of it are exact
+        top = fmaxf(__builtin_ceilf(top * cz[j]), m[j]);
+        if (__any(top > m[j])) {
+          const float down = __builtin_amdgcn_exp2f(m[j] - (top == neg_inf() ? 0.0f : top));
+          l[j] *= down;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) acc[j][d] *= down;
+          m[j] = top;
+        }
+        const float up = top == neg_inf() ? 0.0f : kUp - top;   // (nothing seen yet: probabilities of zero)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          z[j][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][i], cz[j], up));
+          l[j] += z[j][i];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) pw[j][i] = pack_f16(z[j][2 * i], z[j][2 * i + 1]);
+      }
+      // ---- outputs
+      asm volatile("" ::: "memory");                    // (one wave's LDS accesses keep their order)
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const int rr = 16 * (l16 >> 2) + 4 * g + (l16 & 3);
+        const char* const from = mine + rr * (D / 2) + 8 * (d ^ v_swap<D>(rr));
+#if defined(__HIP_DEVICE_COMPILE__)
+        const v2i_t cw = __builtin_amdgcn_ds_read_tr4_b64_v2i32(QF_LDS(v2i_t, const_cast<char*>(from)));
+#else
+        const v2i_t cw = {};
+        (void)from;
+#endif
+        const uint4* const sp = reinterpret_cast<const uint4*>(vscale + ((FMT == QF_FMT_NVFP4 ? d : d >> 1) * 4 + g) * 16);
+        const uint4 sa = sp[0], sb = sp[1];
+        const f16x2_t s0[4] = {__builtin_bit_cast(f16x2_t, sa.x), __builtin_bit_cast(f16x2_t, sa.y),
+                               __builtin_bit_cast(f16x2_t, sa.z), __builtin_bit_cast(f16x2_t, sa.w)};
+        const f16x2_t s1[4] = {__builtin_bit_cast(f16x2_t, sb.x), __builtin_bit_cast(f16x2_t, sb.y),
+                               __builtin_bit_cast(f16x2_t, sb.z), __builtin_bit_cast(f16x2_t, sb.w)};
+        const uint4 v0 = decode_f16((uint32_t)cw[0], s0), v1 = decode_f16((uint32_t)cw[1], s1);
+#pragma unroll
+        for (int j = 0; j < NQ; ++j) {
+          acc[j][d] = mfma_o(v0, make_uint4(pw[j][0], pw[j][1], pw[j][2], pw[j][3]), acc[j][d]);
+          acc[j][d] = mfma_o(v1, make_uint4(pw[j][4], pw[j][5], pw[j][6], pw[j][7]), acc[j][d]);
+        }
+      }
+      // ---- blocks with special scales
+      if (__any(special != 0)) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const uint64_t those = __ballot((special >> (i >> 2)) & 1u);
+#pragma unroll 1
+          for (int gg = 0; gg < 4; ++gg) {
+            const int r = 4 * gg + (i & 3), t = 16 * (i >> 2) + r, pos = base + t;
+            if (!((those >> (4 * r)) & 15u)) continue;
+            const int id = table[pos >> page_log];      // (a good page: it was seen)
+            const uint8_t* const sp = c.scales[1] + ((((int64_t)id * c.H + h) << page_log) + (pos & ((1 << page_log) - 1))) * SB;
+            const char* const codes = mine + t * (D / 2);
+#pragma unroll
+            for (int j = 0; j < NQ; ++j) {
+              const f16x2_t two_p = __builtin_bit_cast(f16x2_t, (uint32_t)__shfl((int)pw[j][i >> 1], 16 * gg + l16, 64));
+              const float pr = (float)two_p[i & 1];
+              const bool sees = pos <= row_pos[j] && (p.window <= 0 || pos > row_pos[j] - p.window);
+              if (!sees) continue;
+#pragma unroll
+              for (int d = 0; d < DT; ++d) {
+                const uint32_t sc = sp[FMT == QF_FMT_NVFP4 ? d : d >> 1];
+                if (!is_special<FMT>(sc)) continue;
+                const uint32_t two = *reinterpret_cast<const uint16_t*>(codes + 8 * (d ^ v_swap<D>(t)) + 2 * g);
+                float f;
+                if constexpr (FMT == QF_FMT_NVFP4) f = __builtin_amdgcn_cvt_f32_fp8((int)sc, 0);
+                else f = sc == 0xFFu ? __builtin_nanf("") : __builtin_ldexpf(1.0f, (int)sc - 127 + 6);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  const uint32_t code = (two >> (4 * k)) & 15u;
+                  const float v = codec::e2m1_value(code & 7u) * f;
+                  acc[j][d][k] = __builtin_fmaf(pr, code & 8u ? -v : v, acc[j][d][k]);
+                }
+              }
+            }
+          }
+        }
+      }
+      asm volatile("" ::: "memory");
+    }
+  }
+
+  // ---- the four waves' sums
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    l[j] += __shfl_xor(l[j], 16, 64);
+    l[j] += __shfl_xor(l[j], 32, 64);
+    if (g == 0) {
+      rows_m[wv][16 * j + l16] = m[j];
+      rows_l[wv][16 * j + l16] = l[j];
+    }
+  }
+  __syncthreads();
+  float lt[NQ], mt[NQ];
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    const int r = 16 * j + l16;
+    float top = rows_m[0][r];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, rows_m[w][r]);
+    const float ref = top == neg_inf() ? 0.0f : top;
+    float sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) sum += rows_l[w][r] * __builtin_amdgcn_exp2f(rows_m[w][r] - ref);
+    lt[j] = sum;
+    mt[j] = top;
+    const float f = __builtin_amdgcn_exp2f(m[j] - ref);
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[j][d] *= f;
+  }
+  auto give = [&](char* to) {
+#pragma unroll
+    for (int j = 0; j < NQ; ++j)
+#pragma unroll
+      for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4_t*>(to + ((j * DT + d) * 64 + lane) * 16) = acc[j][d];
+  };
+  auto take = [&](const char* from) {
+#pragma unroll
+    for (int j = 0; j < NQ; ++j)
+#pragma unroll
+      for (int d = 0; d < DT; ++d) acc[j][d] += *reinterpret_cast<const f32x4_t*>(from + ((j * DT + d) * 64 + lane) * 16);
+  };
+  if (wv >= 2) give(smem + (wv - 2) * kSum);
+  __syncthreads();
+  if (wv < 2) take(smem + wv * kSum);
+  __syncthreads();
+  if (wv == 1) give(smem);
+  __syncthreads();
+  if (wv != 0) return;
+  take(smem);
+
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    if (!row_ok[j]) continue;
+    if (p.splits > 1) {
+      const int64_t at = (int64_t)split * (p.q.T * p.a.Hq) + row_at[j];
+      float* const to = p.part + at * D + 4 * g;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4_t*>(to + 16 * d) = acc[j][d];
+      if (g == 0) {
+        float* const ml = p.part + (int64_t)p.splits * (p.q.T * p.a.Hq) * D + at * 2;
+        *reinterpret_cast<f32x2_t*>(ml) = f32x2_t{mt[j], lt[j]};
+      }
+    } else {
+      const float f = lt[j] == 0.0f ? 0.0f : (FMT == QF_FMT_NVFP4 ? c.S[1][h] : 0x1p-6f) / lt[j];
+      const int t = row_at[j] / (int)p.a.Hq;
+      uint16_t* const to = p.a.O + t * p.a.ldo + (int64_t)(row_at[j] - t * (int)p.a.Hq) * D + 4 * g;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = codec::bf16_rne(lt[j] == 0.0f ? 0.0f : acc[j][d][k] * f);
+        *reinterpret_cast<uint2*>(to + 16 * d) = make_uint2(w[0] | (w[1] << 16), w[2] | (w[3] << 16));
+      }
+      if (p.a.lse && g == 0) p.a.lse[row_at[j]] = lt[j] == 0.0f ? neg_inf() : (mt[j] + (__builtin_log2f(lt[j]) - kUp)) * kLn2;
+    }
+  }
+}
+
+// One workgroup a row: the live pieces' sums, brought to the largest maximum.  A lane takes 4 of the
+// row's elements of every (256 / (D / 4))-th piece, whose loads do not depend on each other.
+template <int FMT, int D>
+__global__ __launch_bounds__(256) void merge_kernel(AttendArgs p) {
+  constexpr int L = D / 4, P = 256 / L;
+  __shared__ f32x4_t sum[P][L];
+  __shared__ float top_of[4], l_of[P];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int64_t row = (int64_t)p.item0 + blockIdx.x, t = row / p.a.Hq, R = p.q.T * p.a.Hq;
+  const int hq = (int)(row - t * p.a.Hq);
+  // the row's sequence, and the reach of the tile that it was part of
+  int64_t b = t, n = 1, at = 0;
+  if (p.q.off) {
+    int64_t lo = 0, hi = p.q.B;
+    while (lo < hi) {
+      const int64_t mid = (lo + hi) >> 1;
+      if (p.q.off[mid + 1] > t) hi = mid;
+      else lo = mid + 1;
+    }
+    b = lo;
+    if (b >= p.q.B || p.q.off[b] > t) return;
+    n = min(p.q.off[b + 1], p.q.T) - max(p.q.off[b], (int64_t)0);
+    at = t - max(p.q.off[b], (int64_t)0);
+  }
+  const int len = max(p.q.lens[b], 0), first = (int)(at / p.tpt) * p.tpt, pos0 = len - (int)n + first;
+  const Reach reach = reach_of(p, len, pos0, pos0 + min(p.tpt, (int)n - first) - 1);
+  const int live = min(live_pieces(reach, p.chunk), p.splits);
+  const float* const ml = p.part + (int64_t)p.splits * R * D;
+  float top = neg_inf();
+  for (int s = tid; s < live; s += 256) top = fmaxf(top, ml[((int64_t)s * R + row) * 2]);
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
+  if (lane == 0) top_of[tid >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(top_of[0], top_of[1]), fmaxf(top_of[2], top_of[3]));
+  const float ref = top == neg_inf() ? 0.0f : top;
+  const int e = tid % L, part = tid / L;
+  f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  float l = 0.0f;
+#pragma unroll 4
+  for (int s = part; s < live; s += P) {
+    const int64_t r = (int64_t)s * R + row;
+    const f32x2_t w = *reinterpret_cast<const f32x2_t*>(ml + r * 2);
+    const f32x4_t v = *reinterpret_cast<const f32x4_t*>(p.part + r * D + 4 * e);
+    const float f = __builtin_amdgcn_exp2f(w[0] - ref);
+    l += f * w[1];
+    acc += f * v;
+  }
+  sum[part][e] = acc;
+  if (e == 0) l_of[part] = l;
+  __syncthreads();
+  if (tid >= L) return;
+  acc = sum[0][tid];
+  l = l_of[0];
+#pragma unroll
+  for (int i = 1; i < P; ++i) {
+    acc += sum[i][tid];
+    l += l_of[i];
+  }
+  const float f = l == 0.0f ? 0.0f : (FMT == QF_FMT_NVFP4 ? p.c.S[1][hq / p.G] : 0x1p-6f) / l;
+  uint32_t w[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) w[k] = codec::bf16_rne(l == 0.0f ? 0.0f : acc[k] * f);
+  *reinterpret_cast<uint2*>(p.a.O + t * p.a.ldo + (int64_t)hq * D + 4 * tid) = make_uint2(w[0] | (w[1] << 16), w[2] | (w[3] << 16));
+  if (p.a.lse && tid == 0) p.a.lse[row] = l == 0.0f ? neg_inf() : (top + (__builtin_log2f(l) - kUp)) * kLn2;
+}
+
+// ------------------------------------------------------------------------------ the launch rules
+struct Plan {
+  int nq, G, Gg, groups, tpt, splits, chunk, most;
+  int64_t items;
+};
+
+Plan plan_of(const KvCache& c, const KvSeqs& q, const AttendCall& a) {
+  Plan p;
+  p.G = (int)(a.Hq / c.H);
+  p.groups = (p.G + 15) / 16;
+  p.Gg = (p.G + p.groups - 1) / p.groups;
+  // 32 rows a wave where a sequence has them: keys and values are decoded once for both halves
+  p.nq = q.off && q.T > q.B && (q.T / std::max<int64_t>(q.B, 1)) * p.Gg > 16 ? 2 : 1;
+  p.tpt = 16 * p.nq / p.Gg;
+  p.items = q.off ? q.T / p.tpt + q.B : q.B;
+  // pieces of the tokens: enough workgroups for the card, none of less than one tile a wave
+  p.most = c.pages == 0 ? 0 : (int)std::min(a.max_len, q.cols << c.page_log);
+  const int64_t longest = std::max<int64_t>(1, a.window > 0 ? std::min<int64_t>(p.most, a.window + p.tpt + 15) : p.most);
+  const int64_t tiles = std::max<int64_t>(1, p.items * p.groups * c.H), want = (4 * compute_units() + tiles - 1) / tiles;
+  const int64_t least = kWaves * kTile;
+  const int64_t chunk = (longest + want - 1) / want;
+  p.chunk = (int)((chunk + least - 1) / least * least);
+  p.splits = (int)((longest + p.chunk - 1) / p.chunk);
+  return p;
+}
+
+template <int FMT, int D, int NQ>
+hipError_t launch(AttendArgs a, const Plan& p, hipStream_t s) {
+  const int64_t each = (int64_t)p.splits * p.groups * a.c.H, most = std::max<int64_t>(1, ((int64_t)1 << 23) / each);
+  for (int64_t i = 0; i < p.items; i += most) {
+    a.item0 = (int)i;
+    hipLaunchKernelGGL((attend_kernel<FMT, D, NQ>), dim3((unsigned)(std::min(most, p.items - i) * each)), dim3(64 * kWaves), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (p.splits == 1) return hipSuccess;
+  const int64_t R = a.q.T * a.a.Hq, step = (int64_t)1 << 23;
+  for (int64_t r = 0; r < R; r += step) {
+    a.item0 = (int)r;
+    hipLaunchKernelGGL((merge_kernel<FMT, D>), dim3((unsigned)std::min(step, R - r)), dim3(256), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+template <int FMT, int D>
+hipError_t launch_nq(const AttendArgs& a, const Plan& p, hipStream_t s) {
+  return p.nq == 2 ? launch<FMT, D, 2>(a, p, s) : launch<FMT, D, 1>(a, p, s);
+}
+
+template <int FMT>
+hipError_t launch_d(const AttendArgs& a, const Plan& p, hipStream_t s) {
+  return a.c.D == 64 ? launch_nq<FMT, 64>(a, p, s) : a.c.D == 128 ? launch_nq<FMT, 128>(a, p, s) : launch_nq<FMT, 256>(a, p, s);
+}
+
+}  // namespace
+
+size_t kv_attention_ws_bytes(const KvCache& c, const KvSeqs& q, const AttendCall& a) {
+  const Plan p = plan_of(c, q, a);
+  return p.splits == 1 ? 0 : (size_t)p.splits * q.T * a.Hq * (c.D + 2) * 4;
+}
+
+hipError_t launch_kv_attention(const KvCache& c, const KvSeqs& q, const AttendCall& a, float* ws, hipStream_t s) {
+  const Plan p = plan_of(c, q, a);
+  const AttendArgs args{c, q, a, p.G, p.Gg, p.groups, p.tpt, p.splits, p.chunk, p.most,
+                        (int)std::min<int64_t>(a.window, INT32_MAX / 2), 0, ws};
+  return c.fmt == QF_FMT_NVFP4 ? launch_d<QF_FMT_NVFP4>(args, p, s) : launch_d<QF_FMT_MXFP4>(args, p, s);
+}
+
+}  // namespace qf

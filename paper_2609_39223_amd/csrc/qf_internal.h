@@ -244,6 +244,21 @@ hipError_t launch_packed_matvec(const PackedOperand& w, const int64_t* off, int6
                                 const int32_t* rows, int64_t rows_div, int64_t M, const uint16_t* X,
                                 int64_t ldx, void* Y, int64_t ldy, int y_f32, hipStream_t s);
 
+// ---- adapters of many requests (qf_adapters.hip) -----------------------------------------------
+// A bf16 [n, r, K] and B bf16 [n, N, r] (dense), scale [n], ranks [n] or null; r a multiple of 8 up to 256.
+struct AdapterSet {
+  int64_t n, N, K;
+  int r;
+  const uint16_t* A;
+  const uint16_t* B;
+  const float* scale;
+  const int32_t* ranks;
+};
+size_t lora_rows_ws_bytes(const AdapterSet& s, int64_t M);
+hipError_t launch_lora_rows(const AdapterSet& s, const int32_t* ids, int64_t M, const uint16_t* X, int64_t ldx,
+                            const void* base, int64_t ldb, void* Y, int64_t ldy, int y_f32, float* ws,
+                            hipStream_t stream);
+
 // ---- QAD distillation loss (qf_kl.hip) ---------------------------------------------------------
 // Per row of bf16 logits [L, V] (V % 8 == 0): row_kl[t], optional loss (mean), grad
 // (gscale (p_S - p_T), bf16) and agree (top-1 equality).
