@@ -158,43 +158,60 @@ struct Tile {
   static constexpr int W = D / 32;           // words of codes of a token's quarter
   static constexpr int KS = FMT == QF_FMT_NVFP4 ? D / 64 : D == 256 ? 2 : 1;     // scale bytes of it
   static constexpr int VS = FMT == QF_FMT_NVFP4 ? D / 16 : D / 32;               // scale bytes of a token
-  uint32_t k[4][W], v[4][W], ks[4], vs[4];
+  uint32_t k[4][W], ks[4], vs[4];
 };
 
+// A wave's address p and a lane's offset, left apart: the load takes one from scalar and the other from vector
+// registers (as one 64-bit address a lane they cost additions and twice the registers).
+typedef const __attribute__((address_space(1))) uint8_t global_byte;
+__device__ __forceinline__ global_byte* lane_at(const uint8_t* p, uint32_t offset) {
+  global_byte* g = (global_byte*)p;
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+s"(g), "+v"(offset));
+#endif
+  return g + offset;
+}
+template <class U>
+__device__ __forceinline__ U load_as(global_byte* p) {
+  return *(const __attribute__((address_space(1))) U*)p;
+}
+
 template <int W>
-__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w) {
-  if constexpr (W == 2) {
-    const uint2 x = *reinterpret_cast<const uint2*>(p);
-    w[0] = x.x;
-    w[1] = x.y;
-  } else {
+__device__ __forceinline__ void load_words(global_byte* p, uint32_t* w) {
+  typedef uint32_t words __attribute__((ext_vector_type(W < 4 ? W : 4)));
 #pragma unroll
-    for (int i = 0; i < W / 4; ++i) {
-      const uint4 x = *reinterpret_cast<const uint4*>(p + 16 * i);
-      w[4 * i] = x.x;
-      w[4 * i + 1] = x.y;
-      w[4 * i + 2] = x.z;
-      w[4 * i + 3] = x.w;
-    }
+  for (int i = 0; i < W; i += 4) {
+    const words x = load_as<words>(p + 4 * i);
+#pragma unroll
+    for (int k = 0; k < (W < 4 ? W : 4); ++k) w[i + k] = x[k];
   }
 }
 
-// V's codes in LDS: row r (16 u + 4 g + i) of D / 2 bytes, its 8-byte unit c at c ^ swap(r).  A
-// transposed read takes one unit of 16 rows, four consecutive ones of each u: with the units
-// exchanged by u (and, where four rows pass 256 bytes, by i) they lie on different banks.
+// V's codes in LDS: row r (16 u + 4 g + i) of D / 2 bytes, its 16-byte chunk c at c ^ v_swap(r).  A transposed
+// read takes 8 bytes of 16 rows, four consecutive ones of each u: with the chunks exchanged by u (and, where
+// four rows pass 256 bytes, by i) they lie on different banks (D = 64: on half as many as there are).
 template <int D>
 __device__ __forceinline__ int v_swap(int r) {
   const int u = r >> 4;
-  return D == 64 ? u : D == 128 ? u << 1 : (u << 1) ^ ((r & 2) << 2);
+  return D == 64 ? u & 1 : D == 128 ? u : u ^ ((r & 2) << 1);
+}
+
+// A copy from memory to LDS: lane i's 16 bytes at g go to l + 16 i.
+__device__ __forceinline__ void copy16(global_byte* g, char* l) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)g,
+                                   (__attribute__((address_space(3))) void*)l, 16, 0, 0);
+#endif
 }
 
 template <int FMT, int D, int NQ>
-__global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs p) {
+__global__ __launch_bounds__(64 * kWaves, NQ == 2 && D == 256 ? 1 : NQ == 2 || D == 256 ? 2 : 4) void attend_kernel(AttendArgs p) {
   typedef Tile<FMT, D> T;
   constexpr int NB = T::VS, CS = D / 32, DT = D / 16;   // V's blocks, steps of a score, tiles of d
   constexpr int kCodes = kTile * D / 2, kStage = kCodes + NB * kTile * 2;   // a wave's LDS: codes, scales in FP16
-  constexpr int kSum = NQ * DT * 64 * 16;               // a wave's outputs on their way to another's
+  constexpr int kSum = DT * 64 * 16;                    // a wave's outputs of 16 rows on their way to another
   __shared__ __align__(16) char smem[std::max(kWaves * kStage, 2 * kSum)];
+  __shared__ uint4 queries[NQ][CS][64];                 // the rows of Q as the products take them
   __shared__ float rows_m[kWaves][16 * NQ], rows_l[kWaves][16 * NQ];
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4;
@@ -209,15 +226,97 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs p) {
   if (!find_tile(p.q, p.tpt, p.item0 + (int)(bid / (uint32_t)p.splits), b, tok0, first, n)) return;
 
   const int page_log = c.page_log;
-  const int len = max(p.q.lens[b], 0), pos0 = len - n + first, toks = min(p.tpt, n - first);
+  const int len = max(__builtin_amdgcn_readfirstlane(p.q.lens[b]), 0), pos0 = len - n + first, toks = min(p.tpt, n - first);
   const Reach reach = reach_of(p, len, pos0, pos0 + toks - 1);
   const int live = live_pieces(reach, p.chunk);
   if (split >= live && p.splits > 1) return;            // (the merge leaves such pieces out)
 
+  // this wave's tokens
+  const int a0 = reach.lo + split * p.chunk, a1 = min(a0 + p.chunk, reach.hi);
+  const int per = (max(a1 - a0, 0) + kWaves * kTile - 1) / (kWaves * kTile) * kTile;
+  const int w0 = a0 + wv * per, todo = max(min(w0 + per, a1) - w0, 0);
+
+  char* const mine = smem + wv * kStage;
+  _Float16* const vscale = reinterpret_cast<_Float16*>(mine + kCodes);
+
+  // ids of 64 pages in the lanes of one register, -1 for a bad one
+  const int page_first = w0 >> page_log, page_last = (w0 + todo - 1) >> page_log;
+  const int32_t* const table = p.q.table + b * p.q.cols;
+  int page_base = page_first, ids = -1;
+  auto fetch_ids = [&](int base) {
+    const int id = table[min(base + lane, page_last)];
+    page_base = base;
+    ids = id >= 0 && id < c.pages ? id : -1;
+  };
+
+  T x;
+  uint32_t bad_now = 0, bad_next = 0;                 // bit u: the tile's tokens 16 u .. have no page
+  constexpr int SB = T::VS;                           // scale bytes of a token
+  const uint32_t row_k = l16 * (D / 2) + g * (D / 8);
+  auto quarter = [&](int q4) { return FMT == QF_FMT_MXFP4 && D == 64 ? q4 >> 1 : q4 * T::KS; };
+  const uint32_t row_ks = l16 * SB + quarter(g), row_vs = (lane >> 2) * SB + quarter(lane & 3);
+  auto load_scales = [&](global_byte* sp) -> uint32_t {
+    return T::KS == 4 ? load_as<uint32_t>(sp) : T::KS == 2 ? load_as<uint16_t>(sp) : *sp;
+  };
+
+  // where the 16 tokens from w0 + t on lie, counted in tokens, and whether they have a page; past the end
+  // the last ones again
+  auto place = [&](int t, uint32_t& bad) -> int64_t {
+    const int pos = w0 + min(t, (todo - 1) & ~15);
+    const int id = __builtin_amdgcn_readlane(ids, (pos >> page_log) - page_base);
+    bad = (uint32_t)id >> 31;
+    return (((int64_t)max(id, 0) * c.H + h) << page_log) + (pos & ((1 << page_log) - 1));
+  };
+  auto load_k = [&](int t) {
+    if (((w0 + min(t + 48, (todo - 1) & ~15)) >> page_log) - page_base >= 64) fetch_ids((w0 + t) >> page_log);
+    bad_next = 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      uint32_t bad;
+      const int64_t at = place(t + 16 * u, bad);
+      bad_next |= bad << u;
+      load_words<T::W>(lane_at(c.codes[0] + at * (D / 2), row_k), x.k[u]);
+      x.ks[u] = load_scales(lane_at(c.scales[0] + at * SB, row_ks));
+    }
+  };
+  // V's codes to LDS, rows back to back as the copies lay them down; the scales of token 16 u + lane / 4
+  auto load_v = [&](int t) {
+    int64_t at[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      uint32_t bad;
+      at[u] = place(t + 16 * u, bad);
+      x.vs[u] = load_scales(lane_at(c.scales[1] + at[u] * SB, row_vs));
+    }
+    if constexpr (D == 64) {                            // 32 rows a copy
+#pragma unroll
+      for (int u = 0; u < 4; u += 2) {
+        const int r = 16 * u + (lane >> 1);
+        copy16((global_byte*)c.codes[1] + (lane < 32 ? at[u] : at[u + 1]) * (D / 2) + (uint32_t)((r & 15) * (D / 2) + 16 * ((lane & 1) ^ v_swap<D>(r))),
+               mine + u * 512);
+      }
+    } else {
+      constexpr int C = D / 32, R = 64 / C;             // chunks of a row, rows a copy
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int k = 0; k < 16 / R; ++k) {
+          const int r = k * R + lane / C;
+          copy16(lane_at(c.codes[1] + at[u] * (D / 2), r * (D / 2) + 16 * ((lane % C) ^ v_swap<D>(16 * u + r))),
+                 mine + (16 * u + k * R) * (D / 2));
+        }
+    }
+  };
+
+  if (todo > 0) {
+    fetch_ids(page_first);
+    load_k(0);
+    load_v(0);
+  }
+
   // this lane's row of each 16
   int row_at[NQ], row_pos[NQ];                          // row of [T, Hq]; position
   bool row_ok[NQ];
-  uint4 qf[NQ][CS];
   float cz[NQ];                                         // times this scores are in units of log 2; positive
   const float S_k = FMT == QF_FMT_NVFP4 ? c.S[0][h] : 1.0f;
 #pragma unroll
@@ -229,14 +328,15 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs p) {
     row_at[j] = t * (int)p.a.Hq + hq;
     const uint16_t* const src = p.a.Q + t * p.a.ldq + (int64_t)hq * D + g * (D / 4);
     const uint32_t flip = p.a.scale * S_k < 0.0f ? 0x80008000u : 0u;
+    uint4 qf[CS];
     uint32_t top = 0;
 #pragma unroll
     for (int s = 0; s < CS; ++s) {
-      qf[j][s] = *reinterpret_cast<const uint4*>(src + 8 * s);
+      qf[s] = *reinterpret_cast<const uint4*>(src + 8 * s);
       uint32_t w[8];
-      codec::unpack8(qf[j][s], w);
+      codec::unpack8(qf[s], w);
       top = max(top, codec::max_abs_bits8(w));
-      qf[j][s] = make_uint4(qf[j][s].x ^ flip, qf[j][s].y ^ flip, qf[j][s].z ^ flip, qf[j][s].w ^ flip);
+      qf[s] = make_uint4(qf[s].x ^ flip, qf[s].y ^ flip, qf[s].z ^ flip, qf[s].w ^ flip);
     }
     top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
     top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
@@ -244,19 +344,21 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs p) {
     const int e = (int)(top >> 7) - 127 - 14;           // (zeros and subnormals: any factor will do)
 #pragma unroll
     for (int s = 0; s < CS; ++s) {
-      const uint32_t w[4] = {qf[j][s].x, qf[j][s].y, qf[j][s].z, qf[j][s].w};
+      const uint32_t w[4] = {qf[s].x, qf[s].y, qf[s].z, qf[s].w};
       uint32_t o[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const float lo = __builtin_ldexpf(codec::as_f32(w[k] << 16), -e), hi = __builtin_ldexpf(codec::as_f32(w[k] & 0xFFFF0000u), -e);
         o[k] = FMT == QF_FMT_NVFP4 ? pack_f16(lo, hi) : codec::bf16x2_rne_nonnan(lo, hi);
       }
-      qf[j][s] = make_uint4(o[0], o[1], o[2], o[3]);
+      if (s % kWaves == wv) queries[j][s][lane] = make_uint4(o[0], o[1], o[2], o[3]);
     }
     f = __builtin_ldexpf(f, e);
     // a query with an infinity or NaN: NaN; never zero, so that hidden scores stay -inf
     cz[j] = top >= 0x7F80u ? __builtin_nanf("") : f < 0x1p-126f ? 0x1p-126f : f;
   }
+
+  __syncthreads();
 
   float m[NQ], l[NQ];
   f32x4_t acc[NQ][DT];
@@ -268,87 +370,26 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs p) {
     for (int d = 0; d < DT; ++d) acc[j][d] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
   }
 
-  // this wave's tokens
-  const int a0 = reach.lo + split * p.chunk, a1 = min(a0 + p.chunk, reach.hi);
-  const int per = (max(a1 - a0, 0) + kWaves * kTile - 1) / (kWaves * kTile) * kTile;
-  const int w0 = a0 + wv * per, todo = max(min(w0 + per, a1) - w0, 0);
-
-  char* const mine = smem + wv * kStage;
-  _Float16* const vscale = reinterpret_cast<_Float16*>(mine + kCodes);
-
   if (todo > 0) {
-    // ids of 64 pages in the lanes of one register, -1 for a bad one
-    const int page_first = w0 >> page_log, page_last = (w0 + todo - 1) >> page_log;
-    const int32_t* const table = p.q.table + b * p.q.cols;
-    int page_base = page_first, ids = -1;
-    auto fetch_ids = [&](int base) {
-      const int id = table[min(base + lane, page_last)];
-      page_base = base;
-      ids = id >= 0 && id < c.pages ? id : -1;
-    };
-    fetch_ids(page_first);
-
-    T x;
-    uint32_t bad_now = 0, bad_next = 0;                 // bit u: the tile's tokens 16 u .. have no page
-    constexpr int SB = T::VS;                           // scale bytes of a token
-    const uint32_t row_k = l16 * (D / 2) + g * (D / 8), row_v = (lane >> 2) * (D / 2) + (lane & 3) * (D / 8);
-    auto quarter = [&](int q4) { return FMT == QF_FMT_MXFP4 && D == 64 ? q4 >> 1 : q4 * T::KS; };
-    const uint32_t row_ks = l16 * SB + quarter(g), row_vs = (lane >> 2) * SB + quarter(lane & 3);
-    auto load_scales = [&](const uint8_t* sp) -> uint32_t {
-      return T::KS == 4 ? *reinterpret_cast<const uint32_t*>(sp) : T::KS == 2 ? *reinterpret_cast<const uint16_t*>(sp) : *sp;
-    };
-
-    // where the 16 tokens from w0 + t on lie, counted in tokens; past the end the last ones again
-    auto place = [&](int t) -> int64_t {
-      const int pos = w0 + min(t, (todo - 1) & ~15);
-      const int id = __builtin_amdgcn_readlane(ids, (pos >> page_log) - page_base);
-      return id < 0 ? -1 : (((int64_t)id * c.H + h) << page_log) + (pos & ((1 << page_log) - 1));
-    };
-    auto load_k = [&](int t) {
-      if (((w0 + min(t + 48, (todo - 1) & ~15)) >> page_log) - page_base >= 64) fetch_ids((w0 + t) >> page_log);
-      bad_next = 0;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        int64_t at = place(t + 16 * u);
-        if (at < 0) {
-          bad_next |= 1u << u;
-          at = 0;
-        }
-        load_words<T::W>(c.codes[0] + at * (D / 2) + row_k, x.k[u]);
-        x.ks[u] = load_scales(c.scales[0] + at * SB + row_ks);
-      }
-    };
-    auto load_v = [&](int t) {
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int64_t at = max(place(t + 16 * u), (int64_t)0);
-        load_words<T::W>(c.codes[1] + at * (D / 2) + row_v, x.v[u]);
-        x.vs[u] = load_scales(c.scales[1] + at * SB + row_vs);
-      }
-    };
-
-    load_k(0);
-    load_v(0);
     for (int t0 = 0; t0 < todo; t0 += kTile) {
       bad_now = bad_next;
       // ---- scores
-      float z[NQ][16];
+      f32x4_t zz[NQ][4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        f32x4_t zz[NQ];
+      for (int j = 0; j < NQ; ++j)
 #pragma unroll
-        for (int j = 0; j < NQ; ++j) zz[j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-        f16x2_t s2[2] = {};
+        for (int u = 0; u < 4; ++u) zz[j][u] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int s = 0; s < CS; ++s) {
+      for (int s = 0; s < CS; ++s) {
+        uint4 q[NQ];
+#pragma unroll
+        for (int j = 0; j < NQ; ++j) q[j] = queries[j][s][lane];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
           uint4 a;
           if constexpr (FMT == QF_FMT_NVFP4) {
-            if ((s & 3) == 0) {                         // scale bytes of 32 elements
-              const f16x2_t v = e4m3_f16(x.ks[u] >> (8 * (s >> 1)));
-              s2[0] = f16x2_t{v[0], v[0]};
-              s2[1] = f16x2_t{v[1], v[1]};
-            }
-            const f16x2_t q2 = s2[(s >> 1) & 1], q4[4] = {q2, q2, q2, q2};
+            const f16x2_t v = e4m3_f16(x.ks[u] >> (8 * (s >> 2 << 1)));   // scales of 32 elements
+            const f16x2_t q2 = (s >> 1) & 1 ? f16x2_t{v[1], v[1]} : f16x2_t{v[0], v[0]}, q4[4] = {q2, q2, q2, q2};
             a = decode_f16(x.k[u][s], q4);
           } else {
             uint32_t w[4];
@@ -356,8 +397,12 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs p) {
             a = make_uint4(w[0], w[1], w[2], w[3]);
           }
 #pragma unroll
-          for (int j = 0; j < NQ; ++j) zz[j] = mfma_z<FMT>(a, qf[j][s], zz[j]);
+          for (int j = 0; j < NQ; ++j) zz[j][u] = mfma_z<FMT>(a, q[j], zz[j][u]);
         }
+      }
+      float z[NQ][16];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
         uint32_t nan_rows = 0;                          // MXFP4: tokens with a NaN scale
         if constexpr (FMT == QF_FMT_MXFP4) {
           const bool bad = (x.ks[u] & 0xFFu) == 0xFFu || (T::KS == 2 && (x.ks[u] >> 8) == 0xFFu);
@@ -368,23 +413,9 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs p) {
         for (int j = 0; j < NQ; ++j)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            z[j][4 * u + i] = zz[j][i];
+            z[j][4 * u + i] = zz[j][u][i];
             if (nan_rows && ((nan_rows >> (4 * g + i)) & 1u)) z[j][4 * u + i] = __builtin_nanf("");
           }
-      }
-      // ---- V's codes to LDS, and the loads of the next 64 tokens
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int r = 16 * u + (lane >> 2), sw = v_swap<D>(r);
-        char* const to = mine + r * (D / 2);
-        if constexpr (D == 64) {
-          *reinterpret_cast<uint2*>(to + 8 * ((lane & 3) ^ sw)) = make_uint2(x.v[u][0], x.v[u][1]);
-        } else {
-#pragma unroll
-          for (int i = 0; i < D / 128; ++i)
-            *reinterpret_cast<uint4*>(to + 8 * (((lane & 3) * (D / 64) + 2 * i) ^ sw)) =
-                make_uint4(x.v[u][4 * i], x.v[u][4 * i + 1], x.v[u][4 * i + 2], x.v[u][4 * i + 3]);
-        }
       }
       // the scales, in the order in which the products take them; zeros for tokens that no row sees and
       // for special ones
@@ -413,10 +444,6 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs p) {
           to[k * 64] = __builtin_bit_cast(f16x2_t, w)[0];
           if (k + 1 < T::KS) to[k * 64 + 64] = __builtin_bit_cast(f16x2_t, w)[1];
         }
-      }
-      if (t0 + kTile < todo) {
-        load_k(t0 + kTile);
-        load_v(t0 + kTile);
       }
       // ---- which positions a row sees, its maximum, its probabilities
       const int base = w0 + t0;
@@ -458,11 +485,14 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs p) {
         for (int i = 0; i < 8; ++i) pw[j][i] = pack_f16(z[j][2 * i], z[j][2 * i + 1]);
       }
       // ---- outputs
-      asm volatile("" ::: "memory");                    // (one wave's LDS accesses keep their order)
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(0x0F70);               // vmcnt(0): this wave's copies of V are in its region
+      asm volatile("" ::: "memory");
+      if (t0 + kTile < todo) load_k(t0 + kTile);
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         const int rr = 16 * (l16 >> 2) + 4 * g + (l16 & 3);
-        const char* const from = mine + rr * (D / 2) + 8 * (d ^ v_swap<D>(rr));
+        const char* const from = mine + rr * (D / 2) + 8 * (d ^ (v_swap<D>(rr) << 1));
 #if defined(__HIP_DEVICE_COMPILE__)
         const v2i_t cw = __builtin_amdgcn_ds_read_tr4_b64_v2i32(QF_LDS(v2i_t, const_cast<char*>(from)));
 #else
@@ -482,44 +512,54 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs p) {
           acc[j][d] = mfma_o(v1, make_uint4(pw[j][4], pw[j][5], pw[j][6], pw[j][7]), acc[j][d]);
         }
       }
-      // ---- blocks with special scales
+      // ---- blocks with special scales, one token after the other
       if (__any(special != 0)) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const uint64_t those = __ballot((special >> (i >> 2)) & 1u);
 #pragma unroll 1
-          for (int gg = 0; gg < 4; ++gg) {
-            const int r = 4 * gg + (i & 3), t = 16 * (i >> 2) + r, pos = base + t;
-            if (!((those >> (4 * r)) & 15u)) continue;
+        for (int u = 0; u < 4; ++u) {
+          uint64_t those = __ballot((special >> u) & 1u);
+#pragma unroll 1
+          while (those) {
+            const int r = __builtin_ctzll(those) >> 2, t = 16 * u + r, pos = base + t;
+            those &= ~(15ull << (4 * r));
             const int id = table[pos >> page_log];      // (a good page: it was seen)
             const uint8_t* const sp = c.scales[1] + ((((int64_t)id * c.H + h) << page_log) + (pos & ((1 << page_log) - 1))) * SB;
-            const char* const codes = mine + t * (D / 2);
+            const char* const codes = mine + t * (D / 2) + 2 * g;
+            const int i = 4 * u + (r & 3);              // its place among the probabilities of group r / 4
+            float pr[NQ];
+            bool sees[NQ];
 #pragma unroll
             for (int j = 0; j < NQ; ++j) {
-              const f16x2_t two_p = __builtin_bit_cast(f16x2_t, (uint32_t)__shfl((int)pw[j][i >> 1], 16 * gg + l16, 64));
-              const float pr = (float)two_p[i & 1];
-              const bool sees = pos <= row_pos[j] && (p.window <= 0 || pos > row_pos[j] - p.window);
-              if (!sees) continue;
+              uint32_t w = pw[j][0];
 #pragma unroll
-              for (int d = 0; d < DT; ++d) {
-                const uint32_t sc = sp[FMT == QF_FMT_NVFP4 ? d : d >> 1];
-                if (!is_special<FMT>(sc)) continue;
-                const uint32_t two = *reinterpret_cast<const uint16_t*>(codes + 8 * (d ^ v_swap<D>(t)) + 2 * g);
-                float f;
-                if constexpr (FMT == QF_FMT_NVFP4) f = __builtin_amdgcn_cvt_f32_fp8((int)sc, 0);
-                else f = sc == 0xFFu ? __builtin_nanf("") : __builtin_ldexpf(1.0f, (int)sc - 127 + 6);
+              for (int k = 1; k < 8; ++k) w = i >> 1 == k ? pw[j][k] : w;
+              w = (uint32_t)__shfl((int)w, 16 * (r >> 2) + l16, 64);
+              pr[j] = (float)__builtin_bit_cast(f16x2_t, w >> (16 * (i & 1)))[0];
+              sees[j] = pos <= row_pos[j] && (p.window <= 0 || pos > row_pos[j] - p.window);
+            }
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                  const uint32_t code = (two >> (4 * k)) & 15u;
-                  const float v = codec::e2m1_value(code & 7u) * f;
-                  acc[j][d][k] = __builtin_fmaf(pr, code & 8u ? -v : v, acc[j][d][k]);
-                }
+            for (int d = 0; d < DT; ++d) {
+              const uint32_t sc = sp[FMT == QF_FMT_NVFP4 ? d : d >> 1];
+              if (!is_special<FMT>(sc)) continue;
+              const uint32_t four = *reinterpret_cast<const uint16_t*>(codes + 8 * (d ^ (v_swap<D>(t) << 1)));
+              float f;
+              if constexpr (FMT == QF_FMT_NVFP4) f = __builtin_nanf("");
+              else f = sc == 0xFFu ? __builtin_nanf("") : __builtin_ldexpf(1.0f, (int)sc - 127 + 6);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const uint32_t code = (four >> (4 * k)) & 15u;
+                const float v = codec::e2m1_value(code & 7u) * f;
+#pragma unroll
+                for (int j = 0; j < NQ; ++j)
+                  if (sees[j]) acc[j][d][k] = __builtin_fmaf(pr[j], code & 8u ? -v : v, acc[j][d][k]);
               }
             }
           }
         }
       }
-      asm volatile("" ::: "memory");
+      if (t0 + kTile < todo) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before the next copies land
+        load_v(t0 + kTile);
+      }
     }
   }
 
@@ -551,26 +591,26 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs p) {
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[j][d] *= f;
   }
-  auto give = [&](char* to) {
 #pragma unroll
-    for (int j = 0; j < NQ; ++j)
+  for (int j = 0; j < NQ; ++j) {
+    auto give = [&](char* to) {
 #pragma unroll
-      for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4_t*>(to + ((j * DT + d) * 64 + lane) * 16) = acc[j][d];
-  };
-  auto take = [&](const char* from) {
+      for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4_t*>(to + (d * 64 + lane) * 16) = acc[j][d];
+    };
+    auto take = [&](const char* from) {
 #pragma unroll
-    for (int j = 0; j < NQ; ++j)
-#pragma unroll
-      for (int d = 0; d < DT; ++d) acc[j][d] += *reinterpret_cast<const f32x4_t*>(from + ((j * DT + d) * 64 + lane) * 16);
-  };
-  if (wv >= 2) give(smem + (wv - 2) * kSum);
-  __syncthreads();
-  if (wv < 2) take(smem + wv * kSum);
-  __syncthreads();
-  if (wv == 1) give(smem);
-  __syncthreads();
+      for (int d = 0; d < DT; ++d) acc[j][d] += *reinterpret_cast<const f32x4_t*>(from + (d * 64 + lane) * 16);
+    };
+    if (wv >= 2) give(smem + (wv - 2) * kSum);
+    __syncthreads();
+    if (wv < 2) take(smem + wv * kSum);
+    __syncthreads();
+    if (wv == 1) give(smem);
+    __syncthreads();
+    if (wv == 0) take(smem);
+    if (j + 1 < NQ) __syncthreads();
+  }
   if (wv != 0) return;
-  take(smem);
 
 #pragma unroll
   for (int j = 0; j < NQ; ++j) {
@@ -679,13 +719,13 @@ Plan plan_of(const KvCache& c, const KvSeqs& q, const AttendCall& a) {
   p.groups = (p.G + 15) / 16;
   p.Gg = (p.G + p.groups - 1) / p.groups;
   // 32 rows a wave where a sequence has them: keys and values are decoded once for both halves
-  p.nq = q.off && q.T > q.B && (q.T / std::max<int64_t>(q.B, 1)) * p.Gg > 16 ? 2 : 1;
+  p.nq = q.off && q.T / std::max<int64_t>(q.B, 1) * p.Gg > 16 ? 2 : 1;
   p.tpt = 16 * p.nq / p.Gg;
   p.items = q.off ? q.T / p.tpt + q.B : q.B;
   // pieces of the tokens: enough workgroups for the card, none of less than one tile a wave
   p.most = c.pages == 0 ? 0 : (int)std::min(a.max_len, q.cols << c.page_log);
   const int64_t longest = std::max<int64_t>(1, a.window > 0 ? std::min<int64_t>(p.most, a.window + p.tpt + 15) : p.most);
-  const int64_t tiles = std::max<int64_t>(1, p.items * p.groups * c.H), want = (4 * compute_units() + tiles - 1) / tiles;
+  const int64_t tiles = std::max<int64_t>(1, p.items * p.groups * c.H), want = (2 * compute_units() + tiles - 1) / tiles;
   const int64_t least = kWaves * kTile;
   const int64_t chunk = (longest + want - 1) / want;
   p.chunk = (int)((chunk + least - 1) / least * least);
