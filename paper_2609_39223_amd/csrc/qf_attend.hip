@@ -105,6 +105,12 @@ __device__ __forceinline__ int live_pieces(const Reach& r, int chunk) {
   return r.hi > r.lo ? (r.hi - r.lo - 1) / chunk + 1 : 0;
 }
 
+// The maximum and sum of a row's piece in the workspace, behind the pieces' outputs.
+__device__ __forceinline__ f32x2_t& row_sums(const AttendArgs& p, int split, int64_t row, int D) {
+  const int64_t R = p.q.T * p.a.Hq;
+  return *reinterpret_cast<f32x2_t*>(p.part + p.splits * R * D + (split * R + row) * 2);
+}
+
 template <int FMT>
 __device__ __forceinline__ f32x4_t mfma_z(uint4 a, uint4 b, f32x4_t c) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -205,7 +211,7 @@ __device__ __forceinline__ void copy16(global_byte* g, char* l) {
 }
 
 template <int FMT, int D, int NQ>
-__global__ __launch_bounds__(64 * kWaves, NQ == 2 && D == 256 ? 1 : NQ == 2 || D == 256 ? 2 : 4) void attend_kernel(AttendArgs p) {
+__global__ __launch_bounds__(64 * kWaves, NQ == 2 && D == 256 ? 1 : NQ == 2 || D == 256 ? 2 : 3) void attend_kernel(AttendArgs p) {
   typedef Tile<FMT, D> T;
   constexpr int NB = T::VS, CS = D / 32, DT = D / 16;   // V's blocks, steps of a score, tiles of d
   constexpr int kCodes = kTile * D / 2, kStage = kCodes + NB * kTile * 2;   // a wave's LDS: codes, scales in FP16
@@ -228,9 +234,24 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 && D == 256 ? 1 : NQ == 2 || D
   const int page_log = c.page_log;
   const int len = max(__builtin_amdgcn_readfirstlane(p.q.lens[b]), 0), pos0 = len - n + first, toks = min(p.tpt, n - first);
   const Reach reach = reach_of(p, len, pos0, pos0 + toks - 1);
-  const int live = live_pieces(reach, p.chunk);
-  if (split >= live && p.splits > 1) return;            // (the merge leaves such pieces out)
 
+  // this lane's row of each 16
+  int row_at[NQ], row_pos[NQ];                          // row of [T, Hq]; position
+  bool row_ok[NQ];
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    const int r = 16 * j + l16, i = r / p.Gg, gh = grp * p.Gg + r % p.Gg;
+    row_ok[j] = i < toks && gh < p.G;
+    row_pos[j] = pos0 + (row_ok[j] ? i : toks - 1);     // (what a row that is none sees is not stored)
+    row_at[j] = (tok0 + (row_ok[j] ? i : 0)) * (int)p.a.Hq + h * p.G + (row_ok[j] ? gh : 0);
+  }
+  if (p.splits > 1 && split >= live_pieces(reach, p.chunk)) {   // a piece that the sequence does not have
+    if (wv == 0 && g == 0)
+#pragma unroll
+      for (int j = 0; j < NQ; ++j)
+        if (row_ok[j]) row_sums(p, split, row_at[j], D) = f32x2_t{neg_inf(), 0.0f};
+    return;
+  }
   // this wave's tokens
   const int a0 = reach.lo + split * p.chunk, a1 = min(a0 + p.chunk, reach.hi);
   const int per = (max(a1 - a0, 0) + kWaves * kTile - 1) / (kWaves * kTile) * kTile;
@@ -314,20 +335,13 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 && D == 256 ? 1 : NQ == 2 || D
     load_v(0);
   }
 
-  // this lane's row of each 16
-  int row_at[NQ], row_pos[NQ];                          // row of [T, Hq]; position
-  bool row_ok[NQ];
   float cz[NQ];                                         // times this scores are in units of log 2; positive
   const float S_k = FMT == QF_FMT_NVFP4 ? c.S[0][h] : 1.0f;
+  const uint32_t flip = p.a.scale * S_k < 0.0f ? 0x80008000u : 0u;
 #pragma unroll
   for (int j = 0; j < NQ; ++j) {
-    const int r = 16 * j + l16, i = r / p.Gg, gh = grp * p.Gg + r % p.Gg;
-    row_ok[j] = i < toks && gh < p.G;
-    row_pos[j] = pos0 + (row_ok[j] ? i : toks - 1);     // (what a row that is none sees is not stored)
-    const int t = tok0 + (row_ok[j] ? i : 0), hq = h * p.G + (row_ok[j] ? gh : 0);
-    row_at[j] = t * (int)p.a.Hq + hq;
+    const int t = row_at[j] / (int)p.a.Hq, hq = row_at[j] - t * (int)p.a.Hq;
     const uint16_t* const src = p.a.Q + t * p.a.ldq + (int64_t)hq * D + g * (D / 4);
-    const uint32_t flip = p.a.scale * S_k < 0.0f ? 0x80008000u : 0u;
     uint4 qf[CS];
     uint32_t top = 0;
 #pragma unroll
@@ -620,10 +634,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 && D == 256 ? 1 : NQ == 2 || D
       float* const to = p.part + at * D + 4 * g;
 #pragma unroll
       for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4_t*>(to + 16 * d) = acc[j][d];
-      if (g == 0) {
-        float* const ml = p.part + (int64_t)p.splits * (p.q.T * p.a.Hq) * D + at * 2;
-        *reinterpret_cast<f32x2_t*>(ml) = f32x2_t{mt[j], lt[j]};
-      }
+      if (g == 0) row_sums(p, split, row_at[j], D) = f32x2_t{mt[j], lt[j]};
     } else {
       const float f = lt[j] == 0.0f ? 0.0f : (FMT == QF_FMT_NVFP4 ? c.S[1][h] : 0x1p-6f) / lt[j];
       const int t = row_at[j] / (int)p.a.Hq;
@@ -640,64 +651,56 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 && D == 256 ? 1 : NQ == 2 || D
   }
 }
 
-// One workgroup a row: the live pieces' sums, brought to the largest maximum.  A lane takes 4 of the
-// row's elements of every (256 / (D / 4))-th piece, whose loads do not depend on each other.
+// One workgroup a row: its pieces' sums, brought to the largest maximum.  A lane takes 4 of the row's elements of
+// every (256 / (D / 4))-th piece with a running maximum of its own, so no load waits for another.
 template <int FMT, int D>
 __global__ __launch_bounds__(256) void merge_kernel(AttendArgs p) {
   constexpr int L = D / 4, P = 256 / L;
   __shared__ f32x4_t sum[P][L];
-  __shared__ float top_of[4], l_of[P];
-  const int tid = threadIdx.x, lane = tid & 63;
+  __shared__ float top_of[P], l_of[P];
+  const int tid = threadIdx.x, e = tid % L, part = tid / L;
   const int64_t row = (int64_t)p.item0 + blockIdx.x, t = row / p.a.Hq, R = p.q.T * p.a.Hq;
   const int hq = (int)(row - t * p.a.Hq);
-  // the row's sequence, and the reach of the tile that it was part of
-  int64_t b = t, n = 1, at = 0;
-  if (p.q.off) {
-    int64_t lo = 0, hi = p.q.B;
-    while (lo < hi) {
-      const int64_t mid = (lo + hi) >> 1;
-      if (p.q.off[mid + 1] > t) hi = mid;
-      else lo = mid + 1;
-    }
-    b = lo;
-    if (b >= p.q.B || p.q.off[b] > t) return;
-    n = min(p.q.off[b + 1], p.q.T) - max(p.q.off[b], (int64_t)0);
-    at = t - max(p.q.off[b], (int64_t)0);
-  }
-  const int len = max(p.q.lens[b], 0), first = (int)(at / p.tpt) * p.tpt, pos0 = len - (int)n + first;
-  const Reach reach = reach_of(p, len, pos0, pos0 + min(p.tpt, (int)n - first) - 1);
-  const int live = min(live_pieces(reach, p.chunk), p.splits);
-  const float* const ml = p.part + (int64_t)p.splits * R * D;
-  float top = neg_inf();
-  for (int s = tid; s < live; s += 256) top = fmaxf(top, ml[((int64_t)s * R + row) * 2]);
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
-  if (lane == 0) top_of[tid >> 6] = top;
-  __syncthreads();
-  top = fmaxf(fmaxf(top_of[0], top_of[1]), fmaxf(top_of[2], top_of[3]));
-  const float ref = top == neg_inf() ? 0.0f : top;
-  const int e = tid % L, part = tid / L;
   f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
-  float l = 0.0f;
-#pragma unroll 4
-  for (int s = part; s < live; s += P) {
-    const int64_t r = (int64_t)s * R + row;
-    const f32x2_t w = *reinterpret_cast<const f32x2_t*>(ml + r * 2);
-    const f32x4_t v = *reinterpret_cast<const f32x4_t*>(p.part + r * D + 4 * e);
-    const float f = __builtin_amdgcn_exp2f(w[0] - ref);
-    l += f * w[1];
-    acc += f * v;
+  float top = neg_inf(), l = 0.0f;
+  constexpr int U = 4;                                  // pieces whose loads are in flight together
+  for (int s0 = part; s0 < p.splits; s0 += U * P) {
+    f32x2_t w[U];
+    f32x4_t v[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int s = min(s0 + i * P, p.splits - 1);      // (past the last: the last again, which does not count)
+      w[i] = row_sums(p, s, row, D);
+      v[i] = *reinterpret_cast<const f32x4_t*>(p.part + (s * R + row) * D + 4 * e);
+      if (s0 + i * P >= p.splits) w[i][0] = neg_inf();
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (w[i][0] == neg_inf()) continue;               // (a piece without tokens holds no outputs)
+      const float now = fmaxf(top, w[i][0]), down = __builtin_amdgcn_exp2f(top - now), f = __builtin_amdgcn_exp2f(w[i][0] - now);
+      l = l * down + f * w[i][1];
+      acc = acc * down + f * v[i];
+      top = now;
+    }
   }
+  if (p.q.off && t >= p.q.off[p.q.B]) return;           // a row of nobody: nothing was written for it
   sum[part][e] = acc;
-  if (e == 0) l_of[part] = l;
+  if (e == 0) {
+    top_of[part] = top;
+    l_of[part] = l;
+  }
   __syncthreads();
   if (tid >= L) return;
-  acc = sum[0][tid];
-  l = l_of[0];
 #pragma unroll
-  for (int i = 1; i < P; ++i) {
-    acc += sum[i][tid];
-    l += l_of[i];
+  for (int i = 0; i < P; ++i) top = fmaxf(top, top_of[i]);
+  const float ref = top == neg_inf() ? 0.0f : top;
+  acc = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+  l = 0.0f;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const float f = __builtin_amdgcn_exp2f(top_of[i] - ref);
+    acc += f * sum[i][tid];
+    l += f * l_of[i];
   }
   const float f = l == 0.0f ? 0.0f : (FMT == QF_FMT_NVFP4 ? p.c.S[1][hq / p.G] : 0x1p-6f) / l;
   uint32_t w[4];
