@@ -872,7 +872,7 @@ typedef struct {
  *   ws     qf_lora_rows_workspace_size bytes, 256-byte aligned.
  * Rows of an adapter may lie anywhere; they cost least side by side.  FP32 sums in a fixed order; X A^T is
  * taken into the second product as the sum of two bf16 halves (2^-17 relative), Y rounded once.
- * Limits: M < 2^24, N and K < 2^30, n < 2^30.
+ * Limits: M < 2^24, N < 2^24, K < 2^30, n < 2^30.
  */
 QF_API qf_status qf_lora_rows_workspace_size(const qf_adapters* a, int64_t M, size_t* bytes);
 QF_API qf_status qf_lora_rows(const qf_adapters* a, const int32_t* ids, int64_t M, const uint16_t* X,

@@ -1,10 +1,14 @@
 // Low-rank adapters of many requests beside a shared projection: Y[m] = base[m] + s_a (x_m A_a^T) B_a^T
 // with a = ids[m] (QATFactory Eq. qad-lora's factors, served without merging them).
 //
-// Two launches on v_mfma_f32_16x16x32_bf16: down, z = x A^T (FP32, in slices of K), and up, which adds the
-// slices in order, splits s z into two bf16 halves and adds z B^T to base.  A workgroup takes 16 rows and one
-// of the adapters that occur among them: rows of other adapters ride along in the products and are not
-// stored, so rows may lie in any order, and an adapter is read once per 16 rows that use it.
+// Two products on v_mfma_f32_16x16x32_bf16: down, z = x A^T, and up, which adds s z B^T to base with s z as two bf16
+// halves.  Few rows leave z in FP32 slices of K, which up adds in order; with more rows there are workgroups enough
+// without slices, and down leaves the halves themselves.  A workgroup takes one adapter's rows, 16 at a time:
+//   up to 64 rows   the z-th adapter among them and the rows that have it (ballots, no memory but the ids);
+//   more            16 RB places in the order of the rows' adapters, which a launch of one workgroup makes (a
+//                   counting sort in LDS; the places of equal ones do not matter to any result).  Rows of other
+//                   adapters among them ride along in the products and are not stored.
+// More rows or adapters than the sort takes (2^16, 2^13) are taken as they come.
 // Bound by memory: the factors of the adapters in use (few rows), base and Y (many).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -21,8 +25,11 @@ namespace {
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
-constexpr int kWaves = 4, kRankTiles = 4;    // 64 ranks a workgroup of the first product
+constexpr int kRankTiles = 4;                // 64 ranks a workgroup of the first product
+constexpr int kDownWaves = 8, kUpWaves = 4;
 constexpr int kCols = 64;                    // columns of Y a wave takes at a time
+constexpr int kFew = 64;                     // rows without an order
+constexpr int kSortRows = 1 << 16, kSortAdapters = 1 << 13;
 
 struct RowsArgs {
   AdapterSet s;
@@ -34,10 +41,12 @@ struct RowsArgs {
   int64_t ldb;
   void* Y;
   int64_t ldy;
-  float* z;                                  // [slices, M, r]
+  float* z;                                  // FP32 [slices, M, r], or bf16 [M, 2, r]: the halves of s z
+  int2* order;                               // [M]: row and adapter (-1: none) of each place, or null
   int slices, kc;                            // slices of K, their size
-  int abreast;                               // adapters of 16 rows that workgroups take side by side
-  int block0;                                // the launch's first 16 rows
+  int abreast;                               // adapters of a group of rows that workgroups take side by side
+  int cols;                                  // workgroups of the second product that share a row
+  int group0;                                // the launch's first group
 };
 
 __device__ __forceinline__ f32x4_t mfma(uint4 a, uint4 b, f32x4_t c) {
@@ -48,80 +57,208 @@ __device__ __forceinline__ f32x4_t mfma(uint4 a, uint4 b, f32x4_t c) {
 #endif
 }
 
-// The adapters among 16 rows, by the rows' order: `id` of lane % 16's row (-1: none), bit i of `firsts`: row i
-// is the first of its adapter.
-struct Group {
-  int id;
-  uint32_t firsts, with;
-};
-__device__ __forceinline__ Group group_of(const RowsArgs& p, int block) {
-  const int row = block * 16 + (threadIdx.x & 15);
-  Group g;
-  g.id = row < p.M ? p.ids[row] : -1;
-  if (g.id < 0 || g.id >= p.s.n) g.id = -1;
-  uint32_t same = 0;
-#pragma unroll
-  for (int i = 15; i >= 0; --i)
-    if (__builtin_amdgcn_readlane(g.id, i) == g.id) same = i;
-  g.with = (uint32_t)__ballot(g.id >= 0) & 0xFFFFu;
-  g.firsts = (uint32_t)__ballot(g.id >= 0 && same == (threadIdx.x & 15)) & 0xFFFFu;
-  return g;
-}
-__device__ __forceinline__ int drop_firsts(uint32_t firsts, int n) {   // without the n lowest bits
-  while (n-- > 0) firsts &= firsts - 1;
-  return (int)firsts;
+__device__ __forceinline__ int adapter_of(const RowsArgs& p, int row) {
+  const int id = p.ids[row];
+  return id >= 0 && id < p.s.n ? id : -1;
 }
 __device__ __forceinline__ int rank_of(const AdapterSet& s, int a) {
   return s.ranks ? min(max(s.ranks[a], 0), s.r) : s.r;
 }
 
-// z[slice][row][j] of the rows of adapter after adapter.  Grid: (16 rows, adapter, slice, 64 ranks).
-__global__ __launch_bounds__(64 * kWaves) void down_kernel(RowsArgs p) {
-  __shared__ f32x4_t part[kWaves][kRankTiles][64];
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, l16 = lane & 15, g = lane >> 4;
-  const int block = p.block0 + blockIdx.x / p.abreast, slice = blockIdx.y, j0 = blockIdx.z * 16 * kRankTiles;
-  const Group grp = group_of(p, block);
-  const int row = min(block * 16 + l16, p.M - 1);
-  // a wave's quarter of the slice, in steps of 32
-  const int K = (int)p.s.K, k_lo = slice * p.kc, k_hi = min(k_lo + p.kc, K);
-  const int per = (p.kc / kWaves + 31) / 32 * 32, w_lo = k_lo + wv * per, w_hi = min(w_lo + per, k_hi);
-  const uint16_t* const x = p.X + row * p.ldx;
-  for (uint32_t left = drop_firsts(grp.firsts, blockIdx.x % p.abreast); left; left = drop_firsts(left, p.abreast)) {
-    const int a = __builtin_amdgcn_readlane(grp.id, __builtin_ctz(left));
-    const int rank = rank_of(p.s, a), tiles = min((rank - j0 + 15) / 16, kRankTiles);
-    const uint16_t* f[kRankTiles];
+// Adds one to the bin of every lane's adapter; returns the bin's count before that lane.  A wave of one adapter (rows
+// side by side, as prompts are) adds once: 64 additions to one address come one after the other.
+__device__ __forceinline__ int take_place(int* bins, int bin) {
+  const int first = __builtin_amdgcn_readfirstlane(bin);
+  const uint64_t active = __ballot(true);
+  if (__all(bin == first)) {
+    const int before = __popcll(active & ((1ull << (threadIdx.x & 63)) - 1));
+    int base = 0;
+    if (before == 0) base = atomicAdd(&bins[first], __popcll(active));
+    return __builtin_amdgcn_readfirstlane(base) + before;
+  }
+  return atomicAdd(&bins[bin], 1);
+}
+
+// The rows in the order of their adapters, those without one last.  One workgroup: counts of the adapters in LDS,
+// their prefix sums, then every row takes the next place of its adapter.
+__global__ __launch_bounds__(1024) void order_kernel(RowsArgs p) {
+  extern __shared__ int count[];             // [n + 1]
+  __shared__ int sums[16];
+  const int tid = threadIdx.x, lane = tid & 63, n = (int)p.s.n;
+  for (int i = tid; i <= n; i += 1024) count[i] = 0;
+  __syncthreads();
+  for (int m = tid; m < p.M; m += 1024) {
+    const int a = adapter_of(p, m);
+    take_place(count, a < 0 ? n : a);
+  }
+  __syncthreads();
+  // thread t owns bins t per .. t per + per - 1
+  const int per = n / 1024 + 1;
+  int mine = 0;
+  for (int i = 0; i < per; ++i)
+    if (tid * per + i <= n) mine += count[tid * per + i];
+  int inc = mine;
 #pragma unroll
-    for (int t = 0; t < kRankTiles; ++t) f[t] = p.s.A + ((int64_t)a * p.s.r + min(j0 + 16 * t + l16, p.s.r - 1)) * K;
-    f32x4_t acc[kRankTiles];
+  for (int d = 1; d < 64; d *= 2) {
+    const int o = __shfl_up(inc, d, 64);
+    if (lane >= d) inc += o;
+  }
+  if (lane == 63) sums[tid >> 6] = inc;
+  __syncthreads();
+  int at = inc - mine;
+  for (int w = 0; w < tid >> 6; ++w) at += sums[w];
+  for (int i = 0; i < per; ++i)
+    if (tid * per + i <= n) {
+      const int c = count[tid * per + i];
+      count[tid * per + i] = at;
+      at += c;
+    }
+  __syncthreads();
+  for (int m = tid; m < p.M; m += 1024) {
+    const int a = adapter_of(p, m);
+    p.order[take_place(count, a < 0 ? n : a)] = make_int2(m, a);
+  }
+}
+
+// Row and adapter (-1: none) of lane % 16 among 16; no row: -1, -1.
+struct Group {
+  int row, id;
+};
+__device__ __forceinline__ Group group_at(const RowsArgs& p, int place) {
+  const int at = place + (threadIdx.x & 15);
+  if (at >= p.M) return {-1, -1};
+  if (p.order == nullptr) return {at, adapter_of(p, at)};
+  const int2 o = p.order[at];
+  return {o.x, o.y};
+}
+// Bit i: row i of 16 is the first of its adapter.
+__device__ __forceinline__ uint32_t firsts_of(const Group& g) {
+  uint32_t left = (uint32_t)__ballot(g.id >= 0) & 0xFFFFu, firsts = 0;
+  while (left) {
+    const int i = __builtin_ctz(left);
+    firsts |= 1u << i;
+    left &= ~(uint32_t)__ballot(g.id == __builtin_amdgcn_readlane(g.id, i));
+  }
+  return firsts;
+}
+
+// The adapters and rows of up to 64 rows: the z-th adapter, and the rows that have it.
+struct Few {
+  int id;                                    // of row `lane`
+  uint64_t rows;                             // of adapter a
+  int a;                                     // -1: there is no z-th adapter
+  __device__ __forceinline__ Few(const RowsArgs& p, int z) {
+    const int lane = threadIdx.x & 63;
+    id = lane < p.M ? adapter_of(p, lane) : -1;
+    uint64_t left = __ballot(id >= 0);
+    a = -1;
+    rows = 0;
+    for (int i = 0; left != 0 && i <= z; ++i) {
+      const int b = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+      const uint64_t with = __ballot(id == b);
+      left &= ~with;
+      if (i == z) {
+        a = b;
+        rows = with;
+      }
+    }
+  }
+  // the first 16 rows of those left, which it takes away
+  __device__ __forceinline__ Group next() {
+    const int lane = threadIdx.x & 63, before = __popcll(rows & ((1ull << lane) - 1)), n = min(__popcll(rows), 16);
+    const bool has = (rows >> lane) & 1;
+    // row `lane` to lane `before`; the others to lanes behind, which nobody looks at
+    const int to = has ? before : 63 - (lane - before);
+    const int row = __shfl(__builtin_amdgcn_ds_permute(4 * to, lane), lane & 15, 64);
+    const Group g{(lane & 15) < n ? row : -1, (lane & 15) < n ? a : -1};
+    for (int i = 0; i < n; ++i) rows &= rows - 1;
+    return g;
+  }
+};
+
+// z of adapter a's rows among 16; each wave a part of the slice, U steps of 32 at once.
+template <int TILES, bool HALVES>
+__device__ __forceinline__ void down_rows(const RowsArgs& p, f32x4_t (*part)[kDownWaves][64], const Group& grp, int a, int slice, int j0) {
+  constexpr int U = 4;
+  const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4;
+  const int K = (int)p.s.K, k_hi = min((slice + 1) * p.kc, K), per = (p.kc / kDownWaves + 31) / 32 * 32;
+  const int w_lo = slice * p.kc + wv * per, w_hi = min(w_lo + per, k_hi), rank = rank_of(p.s, a);
+  const uint16_t* const x = p.X + max(grp.row, 0) * p.ldx;
+  const uint16_t* f[TILES];
 #pragma unroll
-    for (int t = 0; t < kRankTiles; ++t) acc[t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int k0 = w_lo; k0 < w_hi; k0 += 32) {
-      const int k = k0 + 8 * g;
-      uint4 xv = make_uint4(0, 0, 0, 0);
-      if (k < w_hi) xv = *reinterpret_cast<const uint4*>(x + k);
+  for (int t = 0; t < TILES; ++t) f[t] = p.s.A + ((int64_t)a * p.s.r + min(j0 + 16 * t + l16, p.s.r - 1)) * K;
+  f32x4_t acc[TILES];
 #pragma unroll
-      for (int t = 0; t < kRankTiles; ++t)
-        if (t < tiles) {
-          uint4 av = make_uint4(0, 0, 0, 0);
-          if (k < w_hi) av = *reinterpret_cast<const uint4*>(f[t] + k);
-          acc[t] = mfma(xv, av, acc[t]);
-        }
+  for (int t = 0; t < TILES; ++t) acc[t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+  int k0 = w_lo;
+  for (; k0 + 32 * U <= w_hi; k0 += 32 * U) {
+    uint4 xv[U], av[U][TILES];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + 32 * u + 8 * g;
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) av[u][t] = *reinterpret_cast<const uint4*>(f[t] + k);
+      xv[u] = *reinterpret_cast<const uint4*>(x + k);
     }
 #pragma unroll
-    for (int t = 0; t < kRankTiles; ++t) part[wv][t][lane] = acc[t];
-    __syncthreads();
-    if (wv < tiles) {                        // wave t finishes tile t: rows 4 g + i, rank l16
-      const uint32_t mine = (uint32_t)__ballot(grp.id == a);
-      f32x4_t v = part[0][wv][lane];
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) v += part[w][wv][lane];
-      const int j = j0 + 16 * wv + l16;
+      for (int t = 0; t < TILES; ++t) acc[t] = mfma(xv[u], av[u][t], acc[t]);
+  }
+#pragma unroll 1
+  for (; k0 < w_hi; k0 += 32) {              // the rest of the wave's part
+    const int k = k0 + 8 * g;
+    const uint4 xv = k < w_hi ? *reinterpret_cast<const uint4*>(x + k) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (j < rank && ((mine >> (4 * g + i)) & 1u))
-          p.z[((int64_t)slice * p.M + block * 16 + 4 * g + i) * p.s.r + j] = v[i];
+    for (int t = 0; t < TILES; ++t) {
+      const uint4 av = k < w_hi ? *reinterpret_cast<const uint4*>(f[t] + k) : make_uint4(0, 0, 0, 0);
+      acc[t] = mfma(xv, av, acc[t]);
     }
-    __syncthreads();
+  }
+#pragma unroll
+  for (int t = 0; t < TILES; ++t) part[t][wv][lane] = acc[t];
+  __syncthreads();
+  if (wv < TILES) {                          // tile wv: rows 4 g + k of 16, rank l16
+    f32x4_t v = part[wv][0][lane];
+#pragma unroll
+    for (int w = 1; w < kDownWaves; ++w) v += part[wv][w][lane];
+    const int j = j0 + 16 * wv + l16;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int row = __shfl(grp.row, 4 * g + k, 64), id = __shfl(grp.id, 4 * g + k, 64);
+      if (id != a) continue;
+      if constexpr (HALVES) {
+        if (j >= p.s.r) continue;
+        const float f = j < rank ? p.s.scale[a] * v[k] : 0.0f;
+        const uint32_t hi = codec::bf16_rne(f);
+        uint16_t* const to = reinterpret_cast<uint16_t*>(p.z) + (int64_t)row * 2 * p.s.r + j;
+        to[0] = (uint16_t)hi;
+        to[p.s.r] = __builtin_isfinite(f) ? (uint16_t)codec::bf16_rne(f - codec::as_f32(hi << 16)) : (uint16_t)0;
+      } else {
+        if (j < rank) p.z[((int64_t)slice * p.M + row) * p.s.r + j] = v[k];
+      }
+    }
+  }
+  __syncthreads();
+}
+
+// Grid: (16 places and adapter, slice, 64 ranks); FEW: up to 64 rows.
+template <int TILES, bool FEW>
+__global__ __launch_bounds__(64 * kDownWaves) void down_kernel(RowsArgs p) {
+  __shared__ f32x4_t part[TILES][kDownWaves][64];
+  const int slice = blockIdx.y, j0 = blockIdx.z * 16 * kRankTiles;
+  if constexpr (FEW) {
+    Few few(p, blockIdx.x);
+    while (few.rows) {
+      const Group g = few.next();
+      down_rows<TILES, false>(p, part, g, few.a, slice, j0);
+    }
+  } else {
+    const int z0 = blockIdx.x % p.abreast;
+    const Group g = group_at(p, (p.group0 + (int)(blockIdx.x / p.abreast)) * 16);
+    int i = 0;
+    for (uint32_t left = firsts_of(g); left; left &= left - 1, ++i)
+      if (i % p.abreast == z0) down_rows<TILES, true>(p, part, g, __builtin_amdgcn_readlane(g.id, __builtin_ctz(left)), slice, j0);
   }
 }
 
@@ -137,193 +274,312 @@ __device__ __forceinline__ uint4 keep_ranks(uint4 v, int j, int rank) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Y's columns 8 by 8: loads and stores of 8 elements at column n (fewer at the end).
+// Y's (base's) columns 8 by 8: 8 elements at `at`, of which `left` exist.
 template <bool F32>
-__device__ __forceinline__ void load8(const void* p, int64_t at, int left, float v[8]) {
-  if (F32) {
-    const float* const s = static_cast<const float*>(p) + at;
-    if (left >= 8) {
-      const float4 a = *reinterpret_cast<const float4*>(s), b = *reinterpret_cast<const float4*>(s + 4);
-      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-      v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    } else {
+struct Eight {
+  uint4 w[F32 ? 2 : 1];
+  __device__ __forceinline__ void zero() {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = i < left ? s[i] : 0.0f;
-    }
-  } else {
-    const uint16_t* const s = static_cast<const uint16_t*>(p) + at;
-    uint32_t h[8];
-    if (left >= 8) {
-      codec::unpack8(*reinterpret_cast<const uint4*>(s), h);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) h[i] = i < left ? s[i] : 0u;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = codec::as_f32(h[i] << 16);
+    for (int i = 0; i < (F32 ? 2 : 1); ++i) w[i] = make_uint4(0, 0, 0, 0);
   }
-}
-template <bool F32>
-__device__ __forceinline__ void store8(void* p, int64_t at, int left, const float v[8]) {
-  if (F32) {
-    float* const d = static_cast<float*>(p) + at;
-    if (left >= 8) {
-      *reinterpret_cast<float4*>(d) = make_float4(v[0], v[1], v[2], v[3]);
-      *reinterpret_cast<float4*>(d + 4) = make_float4(v[4], v[5], v[6], v[7]);
+  __device__ __forceinline__ void load(const void* p, int64_t at, int left) {
+    if (F32) {
+      const float* const s = static_cast<const float*>(p) + at;
+      if (left >= 8) {
+        w[0] = *reinterpret_cast<const uint4*>(s);
+        w[F32 ? 1 : 0] = *reinterpret_cast<const uint4*>(s + 4);
+      } else {
+        uint32_t h[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] = i < left ? codec::as_u32(s[i]) : 0u;
+        w[0] = make_uint4(h[0], h[1], h[2], h[3]);
+        w[F32 ? 1 : 0] = make_uint4(h[4], h[5], h[6], h[7]);
+      }
     } else {
+      const uint16_t* const s = static_cast<const uint16_t*>(p) + at;
+      if (left >= 8) {
+        w[0] = *reinterpret_cast<const uint4*>(s);
+      } else {
+        uint32_t h[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i < left) d[i] = v[i];
-    }
-  } else {
-    uint16_t* const d = static_cast<uint16_t*>(p) + at;
-    uint32_t h[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) h[i] = codec::bf16_rne(v[i]);
-    if (left >= 8) {
-      *reinterpret_cast<uint4*>(d) = codec::pack8(h);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i < left) d[i] = (uint16_t)h[i];
+        for (int i = 0; i < 8; ++i) h[i] = i < left ? s[i] : 0u;
+        w[0] = codec::pack8(h);
+      }
     }
   }
-}
+  __device__ __forceinline__ float get(int i) const {
+    const uint4 v = w[F32 ? i / 4 : 0];
+    const int k = F32 ? i % 4 : i / 2;
+    const uint32_t u = k == 0 ? v.x : k == 1 ? v.y : k == 2 ? v.z : v.w;
+    return F32 ? codec::as_f32(u) : codec::as_f32(i % 2 ? u & 0xFFFF0000u : u << 16);
+  }
+  __device__ __forceinline__ void store(void* p, int64_t at, int left, const float v[8]) const {
+    if (F32) {
+      float* const d = static_cast<float*>(p) + at;
+      if (left >= 8) {
+        *reinterpret_cast<float4*>(d) = make_float4(v[0], v[1], v[2], v[3]);
+        *reinterpret_cast<float4*>(d + 4) = make_float4(v[4], v[5], v[6], v[7]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < left) d[i] = v[i];
+      }
+    } else {
+      uint16_t* const d = static_cast<uint16_t*>(p) + at;
+      // (a NaN keeps its sign and leading bits)
+      const uint4 h = make_uint4(codec::bf16x2_rne_nonnan(v[0], v[1]), codec::bf16x2_rne_nonnan(v[2], v[3]),
+                                 codec::bf16x2_rne_nonnan(v[4], v[5]), codec::bf16x2_rne_nonnan(v[6], v[7]));
+      if (left >= 8) {
+        *reinterpret_cast<uint4*>(d) = h;
+      } else {
+        uint32_t e[8];
+        codec::unpack8(h, e);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < left) d[i] = (uint16_t)e[i];
+      }
+    }
+  }
+};
 
-// Grid: (16 rows and adapter, 256 columns).  The products are taken transposed, the factor's rows n against
-// the 16 rows of z, and tile t of a pair holds n = 8 (i / 4) + 4 t + i % 4 in its row i, so that a lane ends
-// up with 8 neighbouring columns of its row.
-template <bool F32, int STEPS>
-__global__ __launch_bounds__(64 * kWaves) void up_kernel(RowsArgs p) {
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, l16 = lane & 15, g = lane >> 4;
-  const int block = p.block0 + blockIdx.x / p.abreast, z0 = blockIdx.x % p.abreast;
-  const Group grp = group_of(p, block);
-  const int n0 = ((int)blockIdx.y * kWaves + wv) * kCols, N = (int)p.s.N, r = p.s.r;
-  if (n0 >= N) return;
-  const int row = block * 16 + l16;
-  if (z0 == 0 && grp.id < 0 && row < p.M && p.base != p.Y) {          // rows without an adapter
+// 64 columns from n0 on of adapter a's rows among 16 RB.  The products are taken transposed, the factor's rows n
+// against the 16 rows of z, and tile t of a pair holds n = 8 (i / 4) + 4 t + i % 4 in its row i, so that a lane ends up
+// with 8 neighbouring columns of its row.
+template <bool F32, int STEPS, int RB, bool HALVES>
+__device__ __forceinline__ void up_rows(const RowsArgs& p, const Group* grp, int a, int n0) {
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, N = (int)p.s.N, r = p.s.r;
+  const int rank = rank_of(p.s, a);
+  const uint16_t* const B = p.s.B + (int64_t)a * N * r;
+  Eight<F32> v[RB][2];
+  f32x4_t acc[RB][4];
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       const int n = n0 + 32 * c + 8 * g;
-      if (n >= N) break;
-      float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-      if (p.base) load8<F32>(p.base, row * p.ldb + n, N - n, v);
-      store8<F32>(p.Y, row * p.ldy + n, N - n, v);
+      v[b][c].zero();
+      if (p.base && grp[b].id == a && n < N) v[b][c].load(p.base, grp[b].row * p.ldb + n, N - n);
     }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) acc[b][t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
   }
-  for (uint32_t left = drop_firsts(grp.firsts, z0); left; left = drop_firsts(left, p.abreast)) {
-    const int a = __builtin_amdgcn_readlane(grp.id, __builtin_ctz(left));
-    const int rank = rank_of(p.s, a);
-    const float s = p.s.scale[a];
-    const bool mine = grp.id == a;
-    float v[2][8];
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
+  for (int st = 0; st < STEPS; ++st) {
+    if (32 * st >= rank) break;
+    const int j = 32 * st + 8 * g;
+    uint4 f[4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[c][i] = 0.0f;
-      const int n = n0 + 32 * c + 8 * g;
-      if (p.base && mine && n < N) load8<F32>(p.base, row * p.ldb + n, N - n, v[c]);
+    for (int t = 0; t < 4; ++t) {
+      const int n = n0 + 32 * (t >> 1) + 8 * (l16 >> 2) + 4 * (t & 1) + (l16 & 3);
+      f[t] = make_uint4(0, 0, 0, 0);
+      if (j < rank) f[t] = *reinterpret_cast<const uint4*>(B + (int64_t)min(n, N - 1) * r + j);
     }
-    f32x4_t acc[4];
+    uint4 zh[RB], zl[RB];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) acc[t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int st = 0; st < STEPS; ++st) {
-      const int j = 32 * st + 8 * g;
-      if (32 * st >= rank) break;
-      float z[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-      if (mine && j < rank) {
+    for (int b = 0; b < RB; ++b) {
+      zh[b] = zl[b] = make_uint4(0, 0, 0, 0);
+      if (!(grp[b].id == a && j < rank)) continue;
+      if constexpr (HALVES) {
+        const uint16_t* const src = reinterpret_cast<const uint16_t*>(p.z) + (int64_t)grp[b].row * 2 * r + j;
+        zh[b] = *reinterpret_cast<const uint4*>(src);
+        zl[b] = *reinterpret_cast<const uint4*>(src + r);
+      } else {
+        const float s = p.s.scale[a];
+        const float* src = p.z + (int64_t)grp[b].row * r + j;
+        float z[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll 4
         for (int sl = 0; sl < p.slices; ++sl) {
-          const float* const src = p.z + ((int64_t)sl * p.M + row) * r + j;
           const float4 lo = *reinterpret_cast<const float4*>(src), hi = *reinterpret_cast<const float4*>(src + 4);
+          src += (int64_t)p.M * r;
           z[0] += lo.x; z[1] += lo.y; z[2] += lo.z; z[3] += lo.w;
           z[4] += hi.x; z[5] += hi.y; z[6] += hi.z; z[7] += hi.w;
         }
-      }
-      uint32_t hi[8], lo[8];
+        uint32_t hi[8], lo[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {          // (ranks past the last hold what lay there: not used)
-        const float f = j + i < rank ? s * z[i] : 0.0f;
-        hi[i] = codec::bf16_rne(f);
-        const float rest = f - codec::as_f32(hi[i] << 16);
-        lo[i] = __builtin_isfinite(f) ? codec::bf16_rne(rest) : 0u;
-      }
-      const uint4 zh = codec::pack8(hi), zl = codec::pack8(lo);
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int n = n0 + 32 * (t >> 1) + 8 * (l16 >> 2) + 4 * (t & 1) + (l16 & 3);
-        uint4 b = make_uint4(0, 0, 0, 0);
-        if (j < rank) b = keep_ranks(*reinterpret_cast<const uint4*>(p.s.B + ((int64_t)a * N + min(n, N - 1)) * r + j), j, rank);
-        acc[t] = mfma(b, zh, acc[t]);
-        acc[t] = mfma(b, zl, acc[t]);
+        for (int i = 0; i < 8; ++i) {        // (ranks past the last hold what lay there: not used)
+          const float x = j + i < rank ? s * z[i] : 0.0f;
+          hi[i] = codec::bf16_rne(x);
+          lo[i] = __builtin_isfinite(x) ? codec::bf16_rne(x - codec::as_f32(hi[i] << 16)) : 0u;
+        }
+        zh[b] = codec::pack8(hi);
+        zl[b] = codec::pack8(lo);
       }
     }
-    if (mine) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const uint4 fr = keep_ranks(f[t], j, rank);
+#pragma unroll
+      for (int b = 0; b < RB; ++b) {
+        acc[b][t] = mfma(fr, zh[b], acc[b][t]);
+        acc[b][t] = mfma(fr, zl[b], acc[b][t]);
+      }
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < RB; ++b)
+    if (grp[b].id == a) {
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const int n = n0 + 32 * c + 8 * g;
         if (n >= N) break;
+        float y[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[c][i] += acc[2 * c + (i >> 2)][i & 3];
-        store8<F32>(p.Y, row * p.ldy + n, N - n, v[c]);
+        for (int i = 0; i < 8; ++i) y[i] = v[b][c].get(i) + acc[b][2 * c + (i >> 2)][i & 3];
+        v[b][c].store(p.Y, grp[b].row * p.ldy + n, N - n, y);
       }
+    }
+}
+
+// Rows without an adapter.
+template <bool F32>
+__device__ __forceinline__ void copy_row(const RowsArgs& p, int row, int n0) {
+  if (row < 0 || p.base == p.Y) return;
+  const int g = (threadIdx.x & 63) >> 4, N = (int)p.s.N;
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const int n = n0 + 32 * c + 8 * g;
+    if (n >= N) break;
+    Eight<F32> v;
+    v.zero();
+    if (p.base) v.load(p.base, row * p.ldb + n, N - n);
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = v.get(i);
+    v.store(p.Y, row * p.ldy + n, N - n, y);
+  }
+}
+
+// Workgroups: (16 RB places and adapter, 256 columns), columns first (rows first, the workgroups at work at one
+// time write to the same columns of many rows, and 4099 x 24576 took 155 us in all for 143); RB 0: up to 64 rows,
+// the workgroups past their adapters the rows without one.
+template <bool F32, int STEPS, int RB>
+__global__ __launch_bounds__(64 * kUpWaves) void up_kernel(RowsArgs p) {
+  const uint32_t bx = blockIdx.x / (uint32_t)p.cols;
+  const int n0 = ((int)(blockIdx.x % (uint32_t)p.cols) * kUpWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * kCols;
+  if (n0 >= p.s.N) return;
+  if constexpr (RB == 0) {
+    const int z0 = (int)bx;
+    Few few(p, z0 < p.abreast ? z0 : 0);
+    if (z0 < p.abreast) {
+      while (few.rows) {
+        const Group g = few.next();
+        up_rows<F32, STEPS, 1, false>(p, &g, few.a, n0);
+      }
+    } else {                                 // (the rows without an adapter as if they had one)
+      few.rows = __ballot((int)(threadIdx.x & 63) < p.M && few.id < 0);
+      while (few.rows) copy_row<F32>(p, few.next().row, n0);
+    }
+  } else {
+    const int place = (p.group0 + (int)bx / p.abreast) * 16 * RB, z0 = (int)bx % p.abreast;
+    Group grp[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) grp[b] = group_at(p, place + 16 * b);
+    if constexpr (RB > 1) {
+      const int a = __builtin_amdgcn_readfirstlane(grp[0].id);
+      bool one = a >= 0;
+#pragma unroll
+      for (int b = 0; b < RB; ++b) one = one && (grp[b].id == a || grp[b].row < 0);
+      if (__all(one)) {
+        up_rows<F32, STEPS, RB, true>(p, grp, a, n0);
+        return;
+      }
+    }
+#pragma unroll 1
+    for (int b = 0; b < RB; ++b) {
+      const Group g = RB == 1 ? grp[0] : group_at(p, place + 16 * b);
+      if (z0 == 0) copy_row<F32>(p, g.id < 0 ? g.row : -1, n0);
+      int i = 0;
+      for (uint32_t left = firsts_of(g); left; left &= left - 1, ++i)
+        if (i % p.abreast == z0) up_rows<F32, STEPS, 1, true>(p, &g, __builtin_amdgcn_readlane(g.id, __builtin_ctz(left)), n0);
     }
   }
 }
 
 // ------------------------------------------------------------------------------ the launch rules
 struct Plan {
-  int slices, kc, abreast;
+  int rb;                                    // 16 rows a workgroup takes at once; 0: up to 64 rows
+  int64_t groups;
+  int abreast, slices, kc;
+  bool sorted;
 };
 Plan plan_of(const AdapterSet& s, int64_t M) {
   Plan p;
-  const int64_t blocks = (M + 15) / 16;
-  // few rows: an adapter a workgroup; many: one after the other, where a block's rows mostly share one
-  p.abreast = M <= 256 ? (int)std::min<int64_t>(16, std::max<int64_t>(1, std::min(M, s.n))) : 1;
-  const int64_t want = (2 * compute_units() + blocks * p.abreast - 1) / std::max<int64_t>(1, blocks * p.abreast);
-  const int64_t most = std::max<int64_t>(1, (s.K + 511) / 512);
-  const int64_t slices = std::min(std::max<int64_t>(want, 1), std::min<int64_t>(most, 16));
-  p.kc = (int)((std::max<int64_t>(s.K, 1) + slices - 1) / slices + 127) / 128 * 128;
+  const int64_t n = std::max<int64_t>(1, std::min(M, s.n)), cus = compute_units();
+  p.sorted = M > kFew && M <= kSortRows && s.n <= kSortAdapters;
+  p.rb = M <= kFew ? 0 : M / n >= 64 ? 2 : 1;
+  p.groups = p.rb == 0 ? 1 : (M + 16 * p.rb - 1) / (16 * p.rb);
+  // adapters among 16 sorted rows: about one more than adapters a group
+  p.abreast = p.rb == 0 ? (int)n : p.rb == 2 ? 1 : (int)std::min<int64_t>({16, n, 1 + 16 * n / M});
+  const int64_t each = p.groups * p.abreast, want = (2 * cus + each - 1) / each;
+  const int64_t slices = p.rb ? 1 : std::min(want, std::min<int64_t>(std::max<int64_t>(1, s.K / 1024), 4));
+  p.kc = (int)((std::max<int64_t>(s.K, 1) + slices - 1) / slices + 255) / 256 * 256;
   p.slices = (int)std::max<int64_t>(1, (s.K + p.kc - 1) / p.kc);
   return p;
 }
 
+size_t z_bytes(const AdapterSet& s, int64_t M, const Plan& p) { return ((size_t)p.slices * M * s.r * 4 + 255) / 256 * 256; }
+
+template <int TILES>
+void launch_down(const RowsArgs& a, int rb, dim3 grid, hipStream_t s) {
+  const dim3 block(64 * kDownWaves);
+  if (rb == 0) hipLaunchKernelGGL((down_kernel<TILES, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((down_kernel<TILES, false>), grid, block, 0, s, a);
+}
+template <bool F32, int STEPS>
+void launch_up(const RowsArgs& a, int rb, dim3 grid, hipStream_t s) {
+  const dim3 block(64 * kUpWaves);
+  if (rb == 0) hipLaunchKernelGGL((up_kernel<F32, STEPS, 0>), grid, block, 0, s, a);
+  else if (rb == 1) hipLaunchKernelGGL((up_kernel<F32, STEPS, 1>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((up_kernel<F32, STEPS, 2>), grid, block, 0, s, a);
+}
 template <bool F32>
-void launch_up(const RowsArgs& a, dim3 grid, hipStream_t s) {
+void launch_up(const RowsArgs& a, int rb, dim3 grid, hipStream_t s) {
   const int steps = (a.s.r + 31) / 32;
-  if (steps <= 1) hipLaunchKernelGGL((up_kernel<F32, 1>), grid, dim3(64 * kWaves), 0, s, a);
-  else if (steps <= 2) hipLaunchKernelGGL((up_kernel<F32, 2>), grid, dim3(64 * kWaves), 0, s, a);
-  else if (steps <= 4) hipLaunchKernelGGL((up_kernel<F32, 4>), grid, dim3(64 * kWaves), 0, s, a);
-  else hipLaunchKernelGGL((up_kernel<F32, 8>), grid, dim3(64 * kWaves), 0, s, a);
+  if (steps <= 1) launch_up<F32, 1>(a, rb, grid, s);
+  else if (steps <= 2) launch_up<F32, 2>(a, rb, grid, s);
+  else if (steps <= 4) launch_up<F32, 4>(a, rb, grid, s);
+  else launch_up<F32, 8>(a, rb, grid, s);
 }
 
 }  // namespace
 
 size_t lora_rows_ws_bytes(const AdapterSet& s, int64_t M) {
-  return (size_t)plan_of(s, M).slices * M * s.r * 4;
+  const Plan p = plan_of(s, M);
+  return z_bytes(s, M, p) + (p.sorted ? (size_t)M * 8 : 0);
 }
 
 hipError_t launch_lora_rows(const AdapterSet& s, const int32_t* ids, int64_t M, const uint16_t* X, int64_t ldx,
                             const void* base, int64_t ldb, void* Y, int64_t ldy, int y_f32, float* ws,
                             hipStream_t stream) {
   const Plan p = plan_of(s, M);
+  const int64_t cols = (s.N + kUpWaves * kCols - 1) / (kUpWaves * kCols);
+  int2* const order = p.sorted ? reinterpret_cast<int2*>(reinterpret_cast<char*>(ws) + z_bytes(s, M, p)) : nullptr;
   // (no adapters, or nothing to sum: the products are zeros)
-  RowsArgs a{s, ids, (int)M, X, ldx, base, ldb, Y, ldy, ws, s.K > 0 ? p.slices : 0, p.kc, p.abreast, 0};
-  const int64_t blocks = (M + 15) / 16;
-  const unsigned cols = (unsigned)((s.N + kWaves * kCols - 1) / (kWaves * kCols));
+  RowsArgs a{s, ids, (int)M, X, ldx, base, ldb, Y, ldy, ws, order, s.K > 0 ? p.slices : 0, p.kc, p.abreast, (int)cols, 0};
+  if (order) {
+    hipLaunchKernelGGL(order_kernel, dim3(1), dim3(1024), (size_t)(s.n + 1) * 4, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
   const unsigned ranks = (unsigned)((s.r + 16 * kRankTiles - 1) / (16 * kRankTiles));
-  // a grid has fewer than 2^32 lanes, and at most 65535 workgroups along y
-  const int64_t fit = std::max<int64_t>(1, ((int64_t)1 << 23) / ((int64_t)std::max(std::min(cols, 65535u), p.slices * ranks) * p.abreast));
-  for (int64_t b = 0; b < blocks; b += fit) {
-    a.block0 = (int)b;
-    const unsigned x = (unsigned)(std::min(fit, blocks - b) * p.abreast);
-    if (s.n > 0 && s.K > 0) {
-      hipLaunchKernelGGL(down_kernel, dim3(x, (unsigned)p.slices, ranks), dim3(64 * kWaves), 0, stream, a);
+  // a grid has fewer than 2^32 lanes
+  const int64_t wide = std::max<int64_t>(cols, 2 * p.slices * ranks * std::max(p.rb, 1));
+  const int64_t fit = std::max<int64_t>(1, ((int64_t)1 << 22) / (wide * p.abreast));
+  for (int64_t g = 0; g < p.groups; g += fit) {
+    const unsigned x = (unsigned)(std::min(fit, p.groups - g) * p.abreast);
+    if (s.n > 0 && (s.K > 0 || p.rb > 0)) {  // (the halves of no sum are zeros)
+      a.group0 = (int)(g * std::max(p.rb, 1));
+      const dim3 grid(x * (unsigned)std::max(p.rb, 1), (unsigned)p.slices, ranks);
+      if (s.r <= 16) launch_down<1>(a, p.rb, grid, stream);
+      else if (s.r <= 32) launch_down<2>(a, p.rb, grid, stream);
+      else launch_down<4>(a, p.rb, grid, stream);
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
-    if (y_f32) launch_up<true>(a, dim3(x, cols), stream);
-    else launch_up<false>(a, dim3(x, cols), stream);
+    a.group0 = (int)g;
+    const dim3 grid((unsigned)((p.rb == 0 ? x + 1 : x) * cols));
+    if (y_f32) launch_up<true>(a, p.rb, grid, stream);
+    else launch_up<false>(a, p.rb, grid, stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

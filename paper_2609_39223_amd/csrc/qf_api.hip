@@ -1999,7 +1999,8 @@ qf_status check_adapters(const char* fn, const qf_adapters* a, int64_t M) {
   if (a->r < 8 || a->r > 256 || a->r % 8) return fail(QF_ENOTSUP, "%s: rank %lld, not a multiple of 8 up to 256", fn, (long long)a->r);
   if (a->K % 8) return fail(QF_ESHAPE, "%s: K=%lld is not a multiple of 8", fn, (long long)a->K);
   if (M >= 1 << 24) return fail(QF_ENOTSUP, "%s: 2^24 rows or more", fn);
-  if (a->N >= 1 << 30 || a->K >= 1 << 30 || a->n >= 1 << 30) return fail(QF_ENOTSUP, "%s: N, K or n of 2^30 or more", fn);
+  if (a->N >= 1 << 24) return fail(QF_ENOTSUP, "%s: 2^24 columns or more", fn);
+  if (a->K >= 1 << 30 || a->n >= 1 << 30) return fail(QF_ENOTSUP, "%s: K or n of 2^30 or more", fn);
   return QF_OK;
 }
 

@@ -24,11 +24,6 @@ struct KvSeqs {
   int64_t cols, B, T;
 };
 
-// A page's first byte of head h in an array of `row` bytes a token.
-__device__ __forceinline__ int64_t kv_page_at(const KvCache& c, int64_t page, int h, int row) {
-  return ((page * c.H + h) << c.page_log) * row;
-}
-
 hipError_t launch_kv_write(const KvCache& c, const KvSeqs& q, const uint16_t* K, int64_t ldk,
                            const uint16_t* V, int64_t ldv, hipStream_t s);
 hipError_t launch_kv_read(const KvCache& c, const KvSeqs& q, uint16_t* K, int64_t ldk, uint16_t* V,

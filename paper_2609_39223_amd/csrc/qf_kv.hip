@@ -2,9 +2,11 @@
 // new tokens' rows quantized into their sequences' pages, and rows read back.
 //
 // Both are the quantizers' per-chunk codecs (qf_codecs.h) with the row's address taken from the table of
-// pages: a lane owns 8 consecutive elements of a token's keys or values (a block is 2 or 4 lanes), finds
-// its token's sequence by binary search in the offsets, and the page.  NVFP4's tensor scale S is given
-// per head, so one pass suffices.  Bound by memory: 2 bytes an element one way, 0.53 or 0.56 the other.
+// pages: a lane owns 8 consecutive elements of a token's keys or values (a block is 2 or 4 lanes).  A workgroup
+// first finds the places of its tokens, one a thread (binary search in the offsets, length, page: four trips to
+// memory one after the other), and leaves them in LDS; rows to be written are loaded meanwhile.  NVFP4's tensor
+// scale S is given per head, so one pass suffices.  Bound by memory: 2 bytes an element one way, 0.53 or 0.56
+// the other; few tokens by the trips.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -20,8 +22,6 @@ namespace {
 
 using namespace codec;
 
-constexpr int kTok = 4;                  // tokens a lane takes, their loads all in flight
-
 struct KvRows {
   KvCache c;
   KvSeqs q;
@@ -31,10 +31,9 @@ struct KvRows {
   int64_t group0;                        // the launch's first group of tokens
 };
 
-// The place of token t in the cache: first byte of a page counted in tokens (page 2^log + offset, H
-// heads apart), -1 if it has none.
-__device__ __forceinline__ int64_t kv_place(const KvCache& c, const KvSeqs& q, int64_t t, int& offset) {
-  if (t >= q.T) return -1;
+// The place of token t in the cache: page << page_log | offset; -1 if it has none, -2 if it is nobody's.
+__device__ __forceinline__ int64_t kv_place(const KvCache& c, const KvSeqs& q, int64_t t) {
+  if (t >= q.T) return -2;
   int64_t b = t, behind = 1;             // tokens of the sequence from t on
   if (q.off) {
     int64_t lo = 0, hi = q.B;            // the first b with off[b + 1] > t
@@ -44,85 +43,129 @@ __device__ __forceinline__ int64_t kv_place(const KvCache& c, const KvSeqs& q, i
       else lo = mid + 1;
     }
     b = lo;
-    if (b >= q.B || q.off[b] > t) return -1;
+    if (b >= q.B || q.off[b] > t) return -2;
     behind = q.off[b + 1] - t;
   }
   const int64_t pos = q.lens[b] - behind;
   if (pos < 0 || (pos >> c.page_log) >= q.cols) return -1;
   const int64_t page = q.table[b * q.cols + (pos >> c.page_log)];
-  offset = (int)(pos & ((1 << c.page_log) - 1));
-  return page < c.pages ? page : -1;     // (a negative entry is none either)
+  if (page < 0 || page >= c.pages) return -1;
+  return (page << c.page_log) | (pos & ((1 << c.page_log) - 1));
 }
 
-template <int FMT, bool READ>
+// A block's (D, 1 / D) where it is known already.
+struct Nvfp4Known {
+  f32x2_t dr;
+  __device__ __forceinline__ f32x2_t operator()(uint32_t) const { return dr; }
+};
+
+// Codes and scale bytes of N chunks.  NVFP4: the two lanes of a block share the scales' work, the even one takes
+// chunks 0, 2 .., the odd one chunks 1, 3 .., and each hands the other its results (two divisions a block instead of
+// a lane; 13600 tokens x 2048: 34 -> 32 us).
+template <int FMT, int N>
+__device__ __forceinline__ void encode(const uint4 in[N], float S, uint32_t cw[N], uint32_t sc[N]) {
+  uint32_t h[8], xh[8];
+  if constexpr (FMT == QF_FMT_NVFP4 && N % 2 == 0) {
+    const float six_s = 6.0f * S;
+    const bool odd = threadIdx.x & 1;
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      uint32_t h1[8];
+      unpack8(in[i], h);
+      unpack8(in[i + 1], h1);
+      const uint32_t ab0 = nvfp4_block_max(h), ab1 = nvfp4_block_max(h1);
+      const uint32_t own = nvfp4_scale_code(odd ? ab1 : ab0, S, six_s);
+      const f32x2_t dr = nvfp4_scale_pair(S, own), other = {xor1_f(dr.x), xor1_f(dr.y)};
+      const uint32_t so = xor1_u32(own);
+      sc[i] = odd ? so : own;
+      sc[i + 1] = odd ? own : so;
+      nvfp4_encode(h, ab0, sc[i], Nvfp4Known{{odd ? other.x : dr.x, odd ? other.y : dr.y}}, cw[i], xh);
+      nvfp4_encode(h1, ab1, sc[i + 1], Nvfp4Known{{odd ? dr.x : other.x, odd ? dr.y : other.y}}, cw[i + 1], xh);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      unpack8(in[i], h);
+      if (FMT == QF_FMT_NVFP4) nvfp4_chunk(h, S, 6.0f * S, cw[i], sc[i], xh);
+      else mxfp4_chunk(h, cw[i], sc[i], xh);
+    }
+  }
+}
+
+// N tokens a lane, one after the other of a group's 256 >> log_lanes N.
+template <int FMT, bool READ, int N>
 __global__ __launch_bounds__(256) void kv_rows_kernel(KvRows p) {
   constexpr int BLOCK = FMT == QF_FMT_NVFP4 ? 16 : 32;
-  const int H = p.c.H, D = p.c.D, chunks = H * D / 8;
-  const int lanes = 1 << p.log_lanes;
+  __shared__ int64_t places[16 * N];
+  const int H = p.c.H, D = p.c.D, chunks = H * D / 8, log = p.c.page_log;
+  const int lanes = 1 << p.log_lanes, abreast = 256 >> p.log_lanes, mine = threadIdx.x >> p.log_lanes;
+  const int64_t t0 = (p.group0 + blockIdx.x) * abreast * N;
   int col = (int)blockIdx.y * lanes + (threadIdx.x & (lanes - 1));
-  if (col >= 2 * chunks) return;         // (whole groups of 8 lanes: 2 H D / 8 is a multiple of 16)
   const int v = col >= chunks;
   uint16_t* const x = p.x[v];
-  if (x == nullptr) return;
+  const bool has = col < 2 * chunks && x != nullptr;   // (whole groups of 8 lanes: H D / 8 is a multiple of 8)
   col -= v * chunks;
-  const int h = col / (D / 8), d = col % (D / 8);
-  const int64_t t0 = ((p.group0 + blockIdx.x) * (256 >> p.log_lanes) + (threadIdx.x >> p.log_lanes)) * kTok;
-  int64_t page[kTok];
-  int at[kTok];
+  const int h = has ? col / (D / 8) : 0, d = col % (D / 8);
+  uint16_t* const row = x + (t0 + mine) * p.ld[v] + (int64_t)col * 8;
+  const int64_t step = abreast * p.ld[v];
+  uint4 in[N];
+  auto load = [&]() {
 #pragma unroll
-  for (int i = 0; i < kTok; ++i) {
-    at[i] = 0;
-    page[i] = kv_place(p.c, p.q, t0 + i, at[i]);
-  }
+    for (int i = 0; i < N; ++i) {
+      in[i] = make_uint4(0, 0, 0, 0);
+      if (has && t0 + mine + i * abreast < p.q.T) in[i] = *reinterpret_cast<const uint4*>(row + i * step);
+    }
+  };
+  // (several rows behind the places: in front of them each trip waited for the rows, 13600 tokens took 32 us for 27)
+  if (!READ && N == 1) load();
+  if ((int)threadIdx.x < abreast * N) places[threadIdx.x] = kv_place(p.c, p.q, t0 + threadIdx.x);
   const float S = FMT == QF_FMT_NVFP4 ? p.c.S[v][h] : 1.0f;
-  uint16_t* const row = x + t0 * p.ld[v] + (int64_t)col * 8;
-  if constexpr (READ) {
-    uint32_t cw[kTok], sc[kTok];
+  __syncthreads();
+  if (!has) return;
+  if (!READ && N > 1) load();
+  // the page's first token of head h, then the token: bytes of codes and scales follow from it
+  int64_t at[N];
 #pragma unroll
-    for (int i = 0; i < kTok; ++i) {
+  for (int i = 0; i < N; ++i) {
+    const int64_t w = places[mine + i * abreast];
+    at[i] = w < 0 ? w : ((((w >> log) * H + h) << log) | (w & ((1 << log) - 1)));
+  }
+  if constexpr (READ) {
+    uint32_t cw[N], sc[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
       cw[i] = sc[i] = 0;
-      if (page[i] < 0) continue;
-      cw[i] = *reinterpret_cast<const uint32_t*>(p.c.codes[v] + kv_page_at(p.c, page[i], h, D / 2) +
-                                                 (int64_t)at[i] * (D / 2) + 4 * d);
-      sc[i] = p.c.scales[v][kv_page_at(p.c, page[i], h, D / BLOCK) + (int64_t)at[i] * (D / BLOCK) + d * 8 / BLOCK];
+      if (at[i] < 0) continue;
+      cw[i] = *reinterpret_cast<const uint32_t*>(p.c.codes[v] + at[i] * (D / 2) + 4 * d);
+      sc[i] = p.c.scales[v][at[i] * (D / BLOCK) + d * 8 / BLOCK];
     }
 #pragma unroll
-    for (int i = 0; i < kTok; ++i) {
-      // a token of a sequence that has no place reads as zeros; rows of no sequence are left alone
-      if (t0 + i >= p.q.T || (p.q.off && t0 + i >= p.q.off[p.q.B])) continue;
+    for (int i = 0; i < N; ++i) {
+      if (at[i] == -2) continue;         // (a token without a place reads as zeros)
       uint32_t w[4] = {0, 0, 0, 0};
-      if (page[i] >= 0) {
+      if (at[i] >= 0) {
         if (FMT == QF_FMT_NVFP4) nvfp4_decode8(cw[i], S * __builtin_amdgcn_cvt_f32_fp8((int)sc[i], 0), w);
         else mxfp4_decode8(cw[i], sc[i], w);
       }
-      *reinterpret_cast<uint4*>(row + i * p.ld[v]) = make_uint4(w[0], w[1], w[2], w[3]);
+      *reinterpret_cast<uint4*>(row + i * step) = make_uint4(w[0], w[1], w[2], w[3]);
     }
   } else {
-    uint4 in[kTok];
+    uint32_t cw[N], sc[N];
+    encode<FMT, N>(in, S, cw, sc);
 #pragma unroll
-    for (int i = 0; i < kTok; ++i) {
-      in[i] = make_uint4(0, 0, 0, 0);
-      if (page[i] >= 0) in[i] = *reinterpret_cast<const uint4*>(row + i * p.ld[v]);
-    }
-    const float six_s = 6.0f * S;
-#pragma unroll
-    for (int i = 0; i < kTok; ++i) {
-      uint32_t hh[8], cw, sc, xh[8];
-      unpack8(in[i], hh);
-      if (FMT == QF_FMT_NVFP4) nvfp4_chunk(hh, S, six_s, cw, sc, xh);
-      else mxfp4_chunk(hh, cw, sc, xh);
+    for (int i = 0; i < N; ++i) {
       // the scale bytes of 8 lanes (64 elements: four NVFP4 blocks or two MXFP4 ones) in one store
       uint32_t s8;
       if (FMT == QF_FMT_NVFP4) {
-        s8 = sc | (xor2_u32(sc) << 8);
+        s8 = sc[i] | (xor2_u32(sc[i]) << 8);
         s8 |= xor_swz_u32<4>(s8) << 16;
       } else {
-        s8 = sc | (xor_swz_u32<4>(sc) << 8);
+        s8 = sc[i] | (xor_swz_u32<4>(sc[i]) << 8);
       }
-      if (page[i] < 0) continue;
-      *reinterpret_cast<uint32_t*>(p.c.codes[v] + kv_page_at(p.c, page[i], h, D / 2) + (int64_t)at[i] * (D / 2) + 4 * d) = cw;
+      if (at[i] < 0) continue;
+      *reinterpret_cast<uint32_t*>(p.c.codes[v] + at[i] * (D / 2) + 4 * d) = cw[i];
       if ((d & 7) == 0) {
-        uint8_t* const to = p.c.scales[v] + kv_page_at(p.c, page[i], h, D / BLOCK) + (int64_t)at[i] * (D / BLOCK) + d * 8 / BLOCK;
+        uint8_t* const to = p.c.scales[v] + at[i] * (D / BLOCK) + d * 8 / BLOCK;
         if (FMT == QF_FMT_NVFP4) *reinterpret_cast<uint32_t*>(to) = s8;
         else *reinterpret_cast<uint16_t*>(to) = (uint16_t)s8;
       }
@@ -130,21 +173,28 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(KvRows p) {
   }
 }
 
-template <int FMT, bool READ>
-hipError_t launch_rows(KvRows p, hipStream_t s) {
+template <int FMT, bool READ, int N>
+hipError_t launch_n(KvRows p, hipStream_t s) {
   const int cols = 2 * p.c.H * p.c.D / 8;
   p.log_lanes = 4;                       // 16 chunks at least
   while (p.log_lanes < 8 && (1 << p.log_lanes) < cols) ++p.log_lanes;
-  const int64_t per = (int64_t)(256 >> p.log_lanes) * kTok, groups = (p.q.T + per - 1) / per;
+  const int64_t per = (int64_t)(256 >> p.log_lanes) * N, groups = (p.q.T + per - 1) / per;
   const unsigned wide = (unsigned)((cols + (1 << p.log_lanes) - 1) >> p.log_lanes);
   const int64_t most = ((int64_t)1 << 23) / wide;     // a grid has fewer than 2^32 lanes
   for (int64_t g = 0; g < groups; g += most) {
     p.group0 = g;
-    hipLaunchKernelGGL((kv_rows_kernel<FMT, READ>), dim3((unsigned)std::min(most, groups - g), wide), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((kv_rows_kernel<FMT, READ, N>), dim3((unsigned)std::min(most, groups - g), wide), dim3(256), 0, s, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
+}
+
+// Tokens a lane takes: as many as leave every compute unit a workgroup of 256 lanes or two.
+template <int FMT, bool READ>
+hipError_t launch_rows(const KvRows& p, hipStream_t s) {
+  const int64_t lanes = p.q.T * (2 * p.c.H * p.c.D / 8), unit = 512 * compute_units();
+  return lanes >= 8 * unit ? launch_n<FMT, READ, 8>(p, s) : lanes >= 2 * unit ? launch_n<FMT, READ, 2>(p, s) : launch_n<FMT, READ, 1>(p, s);
 }
 
 }  // namespace
