@@ -27,188 +27,11 @@
 
 #include <algorithm>
 
-#include "qf.h"
-#include "qf_codecs.h"
-#include "qf_internal.h"
-#include "qf_kv.h"
-
-#define QF_LDS(T, p) ((__attribute__((address_space(3))) T*)(p))
+#include "qf_attend.h"
 
 namespace qf {
+namespace attend {
 namespace {
-
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
-typedef int v2i_t __attribute__((ext_vector_type(2)));
-
-constexpr int kWaves = 4, kTile = 64;
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
-constexpr float kUp = 14.0f;                 // probabilities are held 2^14 times as large
-
-struct AttendArgs {
-  KvCache c;
-  KvSeqs q;
-  AttendCall a;
-  int G, Gg, groups;                         // queries' heads to a cache head, of them in a row tile
-  int tpt;                                   // tokens in a row tile
-  int splits, chunk;                         // pieces a row tile's tokens may have, their size
-  int most, window;                          // positions from `most` on are not looked at
-  int item0;
-  float* part;                               // [splits, T Hq, D], then (m, l) [splits, T Hq, 2]
-};
-
-__device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
-
-// The sequence of row tile `item` and the tile's index in it: tiles of sequence b are those from
-// off[b] / tpt + b on, which leaves one too many at most.  Every wave finds it by itself, 64 steps at a
-// time.  False if the tile does not exist.
-__device__ __forceinline__ bool find_tile(const KvSeqs& q, int tpt, int item, int& b, int& tok0, int& first, int& n) {
-  if (q.off == nullptr) {
-    b = tok0 = item;
-    first = 0;
-    n = 1;
-    return item < q.B;
-  }
-  const int lane = threadIdx.x & 63;
-  auto off = [&](int i) { return (int)min(max(q.off[i], (int64_t)0), q.T); };
-  int lo = 0, hi = (int)q.B;
-  while (hi - lo > 1) {
-    const int step = (hi - lo + 63) / 64, i = lo + lane * step;
-    const bool below = i < hi && off(i) / tpt + i <= item;
-    const int k = __popcll(__ballot(below));
-    if (k == 0) return false;
-    lo += (k - 1) * step;
-    hi = min(lo + step, hi);
-  }
-  b = __builtin_amdgcn_readfirstlane(lo);
-  const int o = __builtin_amdgcn_readfirstlane(off(b));
-  n = __builtin_amdgcn_readfirstlane(off(b + 1)) - o;
-  first = (item - (o / tpt + b)) * tpt;
-  tok0 = o + first;
-  return b < q.B && first >= 0 && first < n;
-}
-
-// The positions [lo, hi) that any row of a tile sees; lo is a multiple of 16.
-struct Reach {
-  int lo, hi;
-};
-__device__ __forceinline__ Reach reach_of(const AttendArgs& p, int len, int pos0, int pos1) {
-  Reach r;
-  r.hi = min(min(pos1 + 1, len), p.most);
-  r.lo = p.window > 0 ? max(pos0 - p.window + 1, 0) & ~15 : 0;
-  return r;
-}
-__device__ __forceinline__ int live_pieces(const Reach& r, int chunk) {
-  return r.hi > r.lo ? (r.hi - r.lo - 1) / chunk + 1 : 0;
-}
-
-// The maximum and sum of a row's piece in the workspace, behind the pieces' outputs.
-__device__ __forceinline__ f32x2_t& row_sums(const AttendArgs& p, int split, int64_t row, int D) {
-  const int64_t R = p.q.T * p.a.Hq;
-  return *reinterpret_cast<f32x2_t*>(p.part + p.splits * R * D + (split * R + row) * 2);
-}
-
-template <int FMT>
-__device__ __forceinline__ f32x4_t mfma_z(uint4 a, uint4 b, f32x4_t c) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  if constexpr (FMT == QF_FMT_NVFP4)
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
-  else
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
-#else
-  return c;
-#endif
-}
-__device__ __forceinline__ f32x4_t mfma_o(uint4 a, uint4 b, f32x4_t c) {
-  return mfma_z<QF_FMT_NVFP4>(a, b, c);
-}
-
-// Eight codes as FP16, pairs times the scale pairs s[0..3].
-__device__ __forceinline__ uint4 decode_f16(uint32_t cw, const f16x2_t s[4]) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  const f16x2_t v0 = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(cw, 1.0f, 0)) * s[0];
-  const f16x2_t v1 = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(cw, 1.0f, 1)) * s[1];
-  const f16x2_t v2 = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(cw, 1.0f, 2)) * s[2];
-  const f16x2_t v3 = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(cw, 1.0f, 3)) * s[3];
-  return make_uint4(__builtin_bit_cast(uint32_t, v0), __builtin_bit_cast(uint32_t, v1), __builtin_bit_cast(uint32_t, v2),
-                    __builtin_bit_cast(uint32_t, v3));
-#else
-  return make_uint4(0, 0, 0, 0);
-#endif
-}
-// The E4M3 values of the low two bytes of w.
-__device__ __forceinline__ f16x2_t e4m3_f16(uint32_t w) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  return __builtin_bit_cast(f16x2_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, false));
-#else
-  return f16x2_t{};
-#endif
-}
-__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
-  const f32x2_t v = {a, b};
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2_t));
-}
-
-// Scale codes of V that the products do not take.
-template <int FMT>
-__device__ __forceinline__ bool is_special(uint32_t e) {
-  return FMT == QF_FMT_NVFP4 ? (e & 0x7Fu) == 0x7Fu : e != 0u && (e < 107u || e > 134u);
-}
-
-// What one lane holds of 64 tokens on their way in: a quarter of the bytes of 4 x 16 tokens.
-template <int FMT, int D>
-struct Tile {
-  static constexpr int W = D / 32;           // words of codes of a token's quarter
-  static constexpr int KS = FMT == QF_FMT_NVFP4 ? D / 64 : D == 256 ? 2 : 1;     // scale bytes of it
-  static constexpr int VS = FMT == QF_FMT_NVFP4 ? D / 16 : D / 32;               // scale bytes of a token
-  uint32_t k[4][W], ks[4], vs[4];
-};
-
-// A wave's address p and a lane's offset, left apart: the load takes one from scalar and the other from vector
-// registers (as one 64-bit address a lane they cost additions and twice the registers).
-typedef const __attribute__((address_space(1))) uint8_t global_byte;
-__device__ __forceinline__ global_byte* lane_at(const uint8_t* p, uint32_t offset) {
-  global_byte* g = (global_byte*)p;
-#if defined(__HIP_DEVICE_COMPILE__)
-  asm volatile("" : "+s"(g), "+v"(offset));
-#endif
-  return g + offset;
-}
-template <class U>
-__device__ __forceinline__ U load_as(global_byte* p) {
-  return *(const __attribute__((address_space(1))) U*)p;
-}
-
-template <int W>
-__device__ __forceinline__ void load_words(global_byte* p, uint32_t* w) {
-  typedef uint32_t words __attribute__((ext_vector_type(W < 4 ? W : 4)));
-#pragma unroll
-  for (int i = 0; i < W; i += 4) {
-    const words x = load_as<words>(p + 4 * i);
-#pragma unroll
-    for (int k = 0; k < (W < 4 ? W : 4); ++k) w[i + k] = x[k];
-  }
-}
-
-// V's codes in LDS: row r (16 u + 4 g + i) of D / 2 bytes, its 16-byte chunk c at c ^ v_swap(r).  A transposed
-// read takes 8 bytes of 16 rows, four consecutive ones of each u: with the chunks exchanged by u (and, where
-// four rows pass 256 bytes, by i) they lie on different banks (D = 64: on half as many as there are).
-template <int D>
-__device__ __forceinline__ int v_swap(int r) {
-  const int u = r >> 4;
-  return D == 64 ? u & 1 : D == 128 ? u : u ^ ((r & 2) << 1);
-}
-
-// A copy from memory to LDS: lane i's 16 bytes at g go to l + 16 i.
-__device__ __forceinline__ void copy16(global_byte* g, char* l) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)g,
-                                   (__attribute__((address_space(3))) void*)l, 16, 0, 0);
-#endif
-}
 
 template <int FMT, int D, int NQ>
 __global__ __launch_bounds__(64 * kWaves, NQ == 2 && D == 256 ? 1 : NQ == 2 || D == 256 ? 2 : 3) void attend_kernel(AttendArgs p) {
@@ -335,43 +158,16 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 && D == 256 ? 1 : NQ == 2 || D
     load_v(0);
   }
 
-  float cz[NQ];                                         // times this scores are in units of log 2; positive
+  float cz[NQ];                                         // times this scores are in units of log 2
   const float S_k = FMT == QF_FMT_NVFP4 ? c.S[0][h] : 1.0f;
-  const uint32_t flip = p.a.scale * S_k < 0.0f ? 0x80008000u : 0u;
 #pragma unroll
   for (int j = 0; j < NQ; ++j) {
-    const int t = row_at[j] / (int)p.a.Hq, hq = row_at[j] - t * (int)p.a.Hq;
-    const uint16_t* const src = p.a.Q + t * p.a.ldq + (int64_t)hq * D + g * (D / 4);
-    uint4 qf[CS];
-    uint32_t top = 0;
+    uint4 q[CS];
+    cz[j] = load_query<FMT, D>(p, row_at[j], g, S_k, q);
 #pragma unroll
-    for (int s = 0; s < CS; ++s) {
-      qf[s] = *reinterpret_cast<const uint4*>(src + 8 * s);
-      uint32_t w[8];
-      codec::unpack8(qf[s], w);
-      top = max(top, codec::max_abs_bits8(w));
-      qf[s] = make_uint4(qf[s].x ^ flip, qf[s].y ^ flip, qf[s].z ^ flip, qf[s].w ^ flip);
-    }
-    top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
-    float f = __builtin_fabsf(p.a.scale * S_k) * kLog2e;
-    const int e = (int)(top >> 7) - 127 - 14;           // (zeros and subnormals: any factor will do)
-#pragma unroll
-    for (int s = 0; s < CS; ++s) {
-      const uint32_t w[4] = {qf[s].x, qf[s].y, qf[s].z, qf[s].w};
-      uint32_t o[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float lo = __builtin_ldexpf(codec::as_f32(w[k] << 16), -e), hi = __builtin_ldexpf(codec::as_f32(w[k] & 0xFFFF0000u), -e);
-        o[k] = FMT == QF_FMT_NVFP4 ? pack_f16(lo, hi) : codec::bf16x2_rne_nonnan(lo, hi);
-      }
-      if (s % kWaves == wv) queries[j][s][lane] = make_uint4(o[0], o[1], o[2], o[3]);
-    }
-    f = __builtin_ldexpf(f, e);
-    // a query with an infinity or NaN: NaN; never zero, so that hidden scores stay -inf
-    cz[j] = top >= 0x7F80u ? __builtin_nanf("") : f < 0x1p-126f ? 0x1p-126f : f;
+    for (int s = 0; s < CS; ++s)
+      if (s % kWaves == wv) queries[j][s][lane] = q[s];
   }
-
   __syncthreads();
 
   float m[NQ], l[NQ];
@@ -400,16 +196,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 && D == 256 ? 1 : NQ == 2 || D
         for (int j = 0; j < NQ; ++j) q[j] = queries[j][s][lane];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          uint4 a;
-          if constexpr (FMT == QF_FMT_NVFP4) {
-            const f16x2_t v = e4m3_f16(x.ks[u] >> (8 * (s >> 2 << 1)));   // scales of 32 elements
-            const f16x2_t q2 = (s >> 1) & 1 ? f16x2_t{v[1], v[1]} : f16x2_t{v[0], v[0]}, q4[4] = {q2, q2, q2, q2};
-            a = decode_f16(x.k[u][s], q4);
-          } else {
-            uint32_t w[4];
-            codec::fp4_decode8(x.k[u][s], codec::e8m0_scale((x.ks[u] >> (8 * (s >> 2))) & 0xFFu), w);
-            a = make_uint4(w[0], w[1], w[2], w[3]);
-          }
+          const uint4 a = decode_key<FMT>(x.k[u][s], x.ks[u], s);
 #pragma unroll
           for (int j = 0; j < NQ; ++j) zz[j][u] = mfma_z<FMT>(a, q[j], zz[j][u]);
         }
@@ -417,12 +204,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 && D == 256 ? 1 : NQ == 2 || D
       float z[NQ][16];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        uint32_t nan_rows = 0;                          // MXFP4: tokens with a NaN scale
-        if constexpr (FMT == QF_FMT_MXFP4) {
-          const bool bad = (x.ks[u] & 0xFFu) == 0xFFu || (T::KS == 2 && (x.ks[u] >> 8) == 0xFFu);
-          const uint64_t all = __ballot(bad);
-          nan_rows = (uint32_t)(all | (all >> 16) | (all >> 32) | (all >> 48)) & 0xFFFFu;
-        }
+        const uint32_t nan_rows = nan_keys<FMT, T::KS>(x.ks[u]);
 #pragma unroll
         for (int j = 0; j < NQ; ++j)
 #pragma unroll
@@ -437,27 +219,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 && D == 256 ? 1 : NQ == 2 || D
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const bool seen = t0 + 16 * u + (lane >> 2) < todo && !((bad_now >> u) & 1u);
-        uint32_t sv = seen ? x.vs[u] : 0u;
-#pragma unroll
-        for (int k = 0; k < T::KS; ++k)
-          if (is_special<FMT>((sv >> (8 * k)) & 0xFFu)) {
-            sv &= ~(0xFFu << (8 * k));
-            special |= 1u << u;
-          }
-        // token 16 u + 4 gg + i % 4 lies at i = 4 u + i % 4 of the lanes of group gg
-        _Float16* const to = vscale + (quarter(lane & 3) * 4 + (lane >> 4)) * 16 + 4 * u + ((lane >> 2) & 3);
-#pragma unroll
-        for (int k = 0; k < T::KS; k += 2) {
-          uint32_t w;
-          if constexpr (FMT == QF_FMT_NVFP4) {
-            w = __builtin_bit_cast(uint32_t, e4m3_f16(sv >> (8 * k)));
-          } else {                                      // 2^(e - 127 + 6): exponent field e - 106
-            const uint32_t lo = (sv >> (8 * k)) & 0xFFu, hi = (sv >> (8 * k + 8)) & 0xFFu;
-            w = (lo ? (lo - 106u) << 10 : 0u) | (hi ? (hi - 106u) << 26 : 0u);
-          }
-          to[k * 64] = __builtin_bit_cast(f16x2_t, w)[0];
-          if (k + 1 < T::KS) to[k * 64 + 64] = __builtin_bit_cast(f16x2_t, w)[1];
-        }
+        if (store_scales<FMT, T::KS>(seen ? x.vs[u] : 0u, quarter(lane & 3), u, lane, vscale)) special |= 1u << u;
       }
       // ---- which positions a row sees, its maximum, its probabilities
       const int base = w0 + t0;
@@ -465,38 +227,8 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 && D == 256 ? 1 : NQ == 2 || D
       uint32_t pw[NQ][8];
 #pragma unroll
       for (int j = 0; j < NQ; ++j) {
-        // this lane's tokens are 16 u + 4 g + i; it sees them from `from` to below `to`
-        const int to = min(row_pos[j] + 1 - base, todo - t0);
-        const int from = p.window > 0 ? row_pos[j] - p.window + 1 - base : 0;
-        if (!(whole && __all(to >= kTile && from <= 0))) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int t = 16 * (i >> 2) + 4 * g + (i & 3);
-            if (t < from || t >= to || ((bad_now >> (i >> 2)) & 1u)) z[j][i] = neg_inf();
-          }
-        }
-        float top = z[j][0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, z[j][i]);
-        top = fmaxf(top, __shfl_xor(top, 16, 64));
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        // the reference is a whole number, so that adding it to 14 and powers of two of it are exact
-        top = fmaxf(__builtin_ceilf(top * cz[j]), m[j]);
-        if (__any(top > m[j])) {
-          const float down = __builtin_amdgcn_exp2f(m[j] - (top == neg_inf() ? 0.0f : top));
-          l[j] *= down;
-#pragma unroll
-          for (int d = 0; d < DT; ++d) acc[j][d] *= down;
-          m[j] = top;
-        }
-        const float up = top == neg_inf() ? 0.0f : kUp - top;   // (nothing seen yet: probabilities of zero)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          z[j][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][i], cz[j], up));
-          l[j] += z[j][i];
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) pw[j][i] = pack_f16(z[j][2 * i], z[j][2 * i + 1]);
+        softmax_step<DT>(z[j], cz[j], p.window > 0 ? row_pos[j] - p.window + 1 - base : 0, min(row_pos[j] + 1 - base, todo - t0),
+                         whole, bad_now, g, m[j], l[j], acc[j], pw[j]);
       }
       // ---- outputs
       asm volatile("" ::: "memory");
@@ -505,21 +237,8 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 && D == 256 ? 1 : NQ == 2 || D
       if (t0 + kTile < todo) load_k(t0 + kTile);
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
-        const int rr = 16 * (l16 >> 2) + 4 * g + (l16 & 3);
-        const char* const from = mine + rr * (D / 2) + 8 * (d ^ (v_swap<D>(rr) << 1));
-#if defined(__HIP_DEVICE_COMPILE__)
-        const v2i_t cw = __builtin_amdgcn_ds_read_tr4_b64_v2i32(QF_LDS(v2i_t, const_cast<char*>(from)));
-#else
-        const v2i_t cw = {};
-        (void)from;
-#endif
-        const uint4* const sp = reinterpret_cast<const uint4*>(vscale + ((FMT == QF_FMT_NVFP4 ? d : d >> 1) * 4 + g) * 16);
-        const uint4 sa = sp[0], sb = sp[1];
-        const f16x2_t s0[4] = {__builtin_bit_cast(f16x2_t, sa.x), __builtin_bit_cast(f16x2_t, sa.y),
-                               __builtin_bit_cast(f16x2_t, sa.z), __builtin_bit_cast(f16x2_t, sa.w)};
-        const f16x2_t s1[4] = {__builtin_bit_cast(f16x2_t, sb.x), __builtin_bit_cast(f16x2_t, sb.y),
-                               __builtin_bit_cast(f16x2_t, sb.z), __builtin_bit_cast(f16x2_t, sb.w)};
-        const uint4 v0 = decode_f16((uint32_t)cw[0], s0), v1 = decode_f16((uint32_t)cw[1], s1);
+        uint4 v0, v1;
+        decode_values<FMT, D>(mine, vscale, d, lane, v0, v1);
 #pragma unroll
         for (int j = 0; j < NQ; ++j) {
           acc[j][d] = mfma_o(v0, make_uint4(pw[j][0], pw[j][1], pw[j][2], pw[j][3]), acc[j][d]);
@@ -538,35 +257,9 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 && D == 256 ? 1 : NQ == 2 || D
             const int id = table[pos >> page_log];      // (a good page: it was seen)
             const uint8_t* const sp = c.scales[1] + ((((int64_t)id * c.H + h) << page_log) + (pos & ((1 << page_log) - 1))) * SB;
             const char* const codes = mine + t * (D / 2) + 2 * g;
-            const int i = 4 * u + (r & 3);              // its place among the probabilities of group r / 4
-            float pr[NQ];
-            bool sees[NQ];
-#pragma unroll
-            for (int j = 0; j < NQ; ++j) {
-              uint32_t w = pw[j][0];
-#pragma unroll
-              for (int k = 1; k < 8; ++k) w = i >> 1 == k ? pw[j][k] : w;
-              w = (uint32_t)__shfl((int)w, 16 * (r >> 2) + l16, 64);
-              pr[j] = (float)__builtin_bit_cast(f16x2_t, w >> (16 * (i & 1)))[0];
-              sees[j] = pos <= row_pos[j] && (p.window <= 0 || pos > row_pos[j] - p.window);
-            }
-#pragma unroll
-            for (int d = 0; d < DT; ++d) {
-              const uint32_t sc = sp[FMT == QF_FMT_NVFP4 ? d : d >> 1];
-              if (!is_special<FMT>(sc)) continue;
-              const uint32_t four = *reinterpret_cast<const uint16_t*>(codes + 8 * (d ^ (v_swap<D>(t) << 1)));
-              float f;
-              if constexpr (FMT == QF_FMT_NVFP4) f = __builtin_nanf("");
-              else f = sc == 0xFFu ? __builtin_nanf("") : __builtin_ldexpf(1.0f, (int)sc - 127 + 6);
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const uint32_t code = (four >> (4 * k)) & 15u;
-                const float v = codec::e2m1_value(code & 7u) * f;
-#pragma unroll
-                for (int j = 0; j < NQ; ++j)
-                  if (sees[j]) acc[j][d][k] = __builtin_fmaf(pr[j], code & 8u ? -v : v, acc[j][d][k]);
-              }
-            }
+            add_special<FMT, D, NQ>(p, sp, [&](int d) -> uint32_t {
+              return *reinterpret_cast<const uint16_t*>(codes + 8 * (d ^ (v_swap<D>(t) << 1)));
+            }, u, r, pos, l16, pw, row_pos, acc);
           }
         }
       }
@@ -628,26 +321,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 && D == 256 ? 1 : NQ == 2 || D
 
 #pragma unroll
   for (int j = 0; j < NQ; ++j) {
-    if (!row_ok[j]) continue;
-    if (p.splits > 1) {
-      const int64_t at = (int64_t)split * (p.q.T * p.a.Hq) + row_at[j];
-      float* const to = p.part + at * D + 4 * g;
-#pragma unroll
-      for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4_t*>(to + 16 * d) = acc[j][d];
-      if (g == 0) row_sums(p, split, row_at[j], D) = f32x2_t{mt[j], lt[j]};
-    } else {
-      const float f = lt[j] == 0.0f ? 0.0f : (FMT == QF_FMT_NVFP4 ? c.S[1][h] : 0x1p-6f) / lt[j];
-      const int t = row_at[j] / (int)p.a.Hq;
-      uint16_t* const to = p.a.O + t * p.a.ldo + (int64_t)(row_at[j] - t * (int)p.a.Hq) * D + 4 * g;
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        uint32_t w[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = codec::bf16_rne(lt[j] == 0.0f ? 0.0f : acc[j][d][k] * f);
-        *reinterpret_cast<uint2*>(to + 16 * d) = make_uint2(w[0] | (w[1] << 16), w[2] | (w[3] << 16));
-      }
-      if (p.a.lse && g == 0) p.a.lse[row_at[j]] = lt[j] == 0.0f ? neg_inf() : (mt[j] + (__builtin_log2f(lt[j]) - kUp)) * kLn2;
-    }
+    if (row_ok[j]) emit_row<FMT, D>(p, split, row_at[j], h, g, acc[j], mt[j], lt[j]);
   }
 }
 
@@ -712,7 +386,7 @@ __global__ __launch_bounds__(256) void merge_kernel(AttendArgs p) {
 
 // ------------------------------------------------------------------------------ the launch rules
 struct Plan {
-  int nq, G, Gg, groups, tpt, splits, chunk, most;
+  int nq, G, Gg, groups, tpt, splits, chunk, most;      // nq: 16 rows a wave takes; 0: qf_attend_rows.hip
   int64_t items;
 };
 
@@ -721,9 +395,11 @@ Plan plan_of(const KvCache& c, const KvSeqs& q, const AttendCall& a) {
   p.G = (int)(a.Hq / c.H);
   p.groups = (p.G + 15) / 16;
   p.Gg = (p.G + p.groups - 1) / p.groups;
-  // 32 rows a wave where a sequence has them: keys and values are decoded once for both halves
-  p.nq = q.off && q.T / std::max<int64_t>(q.B, 1) * p.Gg > 16 ? 2 : 1;
-  p.tpt = 16 * p.nq / p.Gg;
+  // rows a sequence has on average: from 17 on 32 a wave, so that keys and values are decoded once for both
+  // halves; from 128 on the kernel that shares the decoded ones between waves (heads of 256 do not fit it)
+  const int64_t rows = q.off ? q.T / std::max<int64_t>(q.B, 1) * p.Gg : 1;
+  p.nq = rows <= 16 ? 1 : rows < kManyRows || c.D == 256 ? 2 : 0;
+  p.tpt = (p.nq ? 16 * p.nq : kManyRows) / p.Gg;
   p.items = q.off ? q.T / p.tpt + q.B : q.B;
   // pieces of the tokens: enough workgroups for the card, none of less than one tile a wave
   p.most = c.pages == 0 ? 0 : (int)std::min(a.max_len, q.cols << c.page_log);
@@ -736,16 +412,9 @@ Plan plan_of(const KvCache& c, const KvSeqs& q, const AttendCall& a) {
   return p;
 }
 
-template <int FMT, int D, int NQ>
-hipError_t launch(AttendArgs a, const Plan& p, hipStream_t s) {
-  const int64_t each = (int64_t)p.splits * p.groups * a.c.H, most = std::max<int64_t>(1, ((int64_t)1 << 23) / each);
-  for (int64_t i = 0; i < p.items; i += most) {
-    a.item0 = (int)i;
-    hipLaunchKernelGGL((attend_kernel<FMT, D, NQ>), dim3((unsigned)(std::min(most, p.items - i) * each)), dim3(64 * kWaves), 0, s, a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  if (p.splits == 1) return hipSuccess;
+template <int FMT, int D>
+hipError_t merge(AttendArgs a, hipStream_t s) {
+  if (a.splits == 1) return hipSuccess;
   const int64_t R = a.q.T * a.a.Hq, step = (int64_t)1 << 23;
   for (int64_t r = 0; r < R; r += step) {
     a.item0 = (int)r;
@@ -756,9 +425,22 @@ hipError_t launch(AttendArgs a, const Plan& p, hipStream_t s) {
   return hipSuccess;
 }
 
+template <int FMT, int D, int NQ>
+hipError_t launch(AttendArgs a, const Plan& p, hipStream_t s) {
+  const int64_t each = (int64_t)p.splits * p.groups * a.c.H, most = std::max<int64_t>(1, ((int64_t)1 << 23) / each);
+  for (int64_t i = 0; i < p.items; i += most) {
+    a.item0 = (int)i;
+    hipLaunchKernelGGL((attend_kernel<FMT, D, NQ>), dim3((unsigned)(std::min(most, p.items - i) * each)), dim3(64 * kWaves), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 template <int FMT, int D>
 hipError_t launch_nq(const AttendArgs& a, const Plan& p, hipStream_t s) {
-  return p.nq == 2 ? launch<FMT, D, 2>(a, p, s) : launch<FMT, D, 1>(a, p, s);
+  const hipError_t e = p.nq == 0 ? launch_rows(a, p.items, s) : p.nq == 2 ? launch<FMT, D, 2>(a, p, s) : launch<FMT, D, 1>(a, p, s);
+  return e == hipSuccess ? merge<FMT, D>(a, s) : e;
 }
 
 template <int FMT>
@@ -767,17 +449,18 @@ hipError_t launch_d(const AttendArgs& a, const Plan& p, hipStream_t s) {
 }
 
 }  // namespace
+}  // namespace attend
 
 size_t kv_attention_ws_bytes(const KvCache& c, const KvSeqs& q, const AttendCall& a) {
-  const Plan p = plan_of(c, q, a);
+  const attend::Plan p = attend::plan_of(c, q, a);
   return p.splits == 1 ? 0 : (size_t)p.splits * q.T * a.Hq * (c.D + 2) * 4;
 }
 
 hipError_t launch_kv_attention(const KvCache& c, const KvSeqs& q, const AttendCall& a, float* ws, hipStream_t s) {
-  const Plan p = plan_of(c, q, a);
-  const AttendArgs args{c, q, a, p.G, p.Gg, p.groups, p.tpt, p.splits, p.chunk, p.most,
+  const attend::Plan p = attend::plan_of(c, q, a);
+  const attend::AttendArgs args{c, q, a, p.G, p.Gg, p.groups, p.tpt, p.splits, p.chunk, p.most,
                         (int)std::min<int64_t>(a.window, INT32_MAX / 2), 0, ws};
-  return c.fmt == QF_FMT_NVFP4 ? launch_d<QF_FMT_NVFP4>(args, p, s) : launch_d<QF_FMT_MXFP4>(args, p, s);
+  return c.fmt == QF_FMT_NVFP4 ? attend::launch_d<QF_FMT_NVFP4>(args, p, s) : attend::launch_d<QF_FMT_MXFP4>(args, p, s);
 }
 
 }  // namespace qf

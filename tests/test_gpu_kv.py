@@ -230,6 +230,16 @@ def test_long(qf, fmt):
     _run(qf, fmt, [70001], None, 1, 2, 256, 1024, seed=4)
 
 
+@pytest.mark.parametrize("fmt,D,page", [("nvfp4", 64, 16), ("nvfp4", 128, 64), ("mxfp4", 64, 128), ("mxfp4", 128, 16), ("mxfp4", 256, 32)])
+@pytest.mark.parametrize("window", [0, 700])
+def test_pieces_of_prompts(qf, fmt, D, page, window):
+    """Many new tokens behind many cached ones: every wave's share, more than 64 tiles a piece, row tiles that
+    are not full, a sequence that is all new and one without new tokens."""
+    _run(qf, fmt, [700, 131, 64, 1500], [300, 131, 0, 257], 1, 4, D, page, window=window, seed=30, extra=3)
+    _run(qf, fmt, [5000], [70], 2, 3, D, page, window=window, seed=31)
+    _run(qf, fmt, [200, 333], [200, 333], 1, 16, D, page, window=window, seed=32)
+
+
 @pytest.mark.parametrize("fmt", ["nvfp4", "mxfp4"])
 @pytest.mark.parametrize("scale", [0.0, -0.3, 1.0, 1e-30, 6.0])
 def test_scales(qf, fmt, scale):
@@ -253,7 +263,7 @@ def test_many_sequences(qf, fmt):
 
 
 @pytest.mark.parametrize("fmt", ["nvfp4", "mxfp4"])
-@pytest.mark.parametrize("new", [None, [20, 1, 40]])
+@pytest.mark.parametrize("new", [None, [20, 1, 40], [100, 16, 150]])
 def test_bad_pages(qf, fmt, new):
     """Tokens of a page that is none are not seen."""
     def spoil(table, k, v):
@@ -266,7 +276,7 @@ def test_bad_pages(qf, fmt, new):
 
 
 @pytest.mark.parametrize("fmt", ["nvfp4", "mxfp4"])
-@pytest.mark.parametrize("new,window", [(None, 0), ([9, 30], 0), ([9, 30], 13), (None, 20)])
+@pytest.mark.parametrize("new,window", [(None, 0), ([9, 30], 0), ([9, 30], 13), (None, 20), ([60, 50], 0), ([60, 50], 13)])
 def test_nan_scales(qf, fmt, new, window):
     """Keys and values with NaN scales behind a sequence's end or outside the window are not seen; the ones
     that a row sees make it NaN (a value's block: those outputs alone), and no row before them."""
@@ -312,6 +322,8 @@ def test_values_of_any_scale(qf):
     _run(qf, "mxfp4", [150, 33, 64], None, 2, 2, 64, 16, seed=13, spoil=spoil)
     _run(qf, "mxfp4", [150, 33, 64], [20, 3, 64], 2, 3, 128, 16, seed=13, spoil=spoil)
     _run(qf, "mxfp4", [80], [7], 1, 2, 256, 16, seed=13, spoil=spoil)
+    _run(qf, "mxfp4", [150, 133], [120, 90], 2, 3, 128, 16, seed=13, spoil=spoil)
+    _run(qf, "mxfp4", [150, 133], [120, 90], 1, 5, 64, 32, seed=13, spoil=spoil)
 
     def tiny(table, k, v):
         v[1][:] = 20
