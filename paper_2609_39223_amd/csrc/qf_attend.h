@@ -150,6 +150,8 @@ typedef const __attribute__((address_space(1))) uint8_t global_byte;
 __device__ __forceinline__ global_byte* lane_at(const uint8_t* p, uint32_t offset) {
   global_byte* g = (global_byte*)p;
 #if defined(__HIP_DEVICE_COMPILE__)
+  const uint64_t v = (uint64_t)p;
+  g = (global_byte*)((uint64_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
   asm volatile("" : "+s"(g), "+v"(offset));
 #endif
   return g + offset;
@@ -179,12 +181,24 @@ __device__ __forceinline__ int v_swap(int r) {
   return D == 64 ? u & 1 : D == 128 ? u : u ^ ((r & 2) << 1);
 }
 
-// A copy from memory to LDS: lane i's 16 bytes at g go to l + 16 i.
-__device__ __forceinline__ void copy16(global_byte* g, char* l) {
+// A copy from memory to LDS: the 16 bytes at p + offset of lane i go to l + 16 i (p, l and `bytes`, what may be read from p
+// on, are the wave's).  (The global form, without a resource, makes the compiler wait for it before any LDS access.)
+__device__ __forceinline__ void copy16(const uint8_t* p, uint32_t bytes, uint32_t offset, char* l) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)g,
-                                   (__attribute__((address_space(3))) void*)l, 16, 0, 0);
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, (int)bytes, 0x00020000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)l, 16, (int)offset, 0, 0, 0);
 #endif
+}
+// V's codes of the 16 tokens at p, tokens 16 u .. of a tile, to LDS: rows back to back, chunks exchanged.
+template <int D>
+__device__ __forceinline__ void copy_values(const uint8_t* p, int u, int lane, char* to) {
+  constexpr int C = D / 32, R = 64 / C;                 // chunks of a row, rows a copy
+#pragma unroll
+  for (int i = 0; i < (16 + R - 1) / R; ++i) {
+    const int r = i * R + lane / C;
+    if (R <= 16 || lane < 16 * C)
+      copy16(p, 16 * (D / 2), r * (D / 2) + 16 * ((lane % C) ^ v_swap<D>(16 * u + r)), to + (16 * u + i * R) * (D / 2));
+  }
 }
 
 // A row of Q as the products take it, lane group g's quarter of D, and the factor that brings its scores to units of

@@ -132,24 +132,8 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 && D == 256 ? 1 : NQ == 2 || D
       at[u] = place(t + 16 * u, bad);
       x.vs[u] = load_scales(lane_at(c.scales[1] + at[u] * SB, row_vs));
     }
-    if constexpr (D == 64) {                            // 32 rows a copy
 #pragma unroll
-      for (int u = 0; u < 4; u += 2) {
-        const int r = 16 * u + (lane >> 1);
-        copy16((global_byte*)c.codes[1] + (lane < 32 ? at[u] : at[u + 1]) * (D / 2) + (uint32_t)((r & 15) * (D / 2) + 16 * ((lane & 1) ^ v_swap<D>(r))),
-               mine + u * 512);
-      }
-    } else {
-      constexpr int C = D / 32, R = 64 / C;             // chunks of a row, rows a copy
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int k = 0; k < 16 / R; ++k) {
-          const int r = k * R + lane / C;
-          copy16(lane_at(c.codes[1] + at[u] * (D / 2), r * (D / 2) + 16 * ((lane % C) ^ v_swap<D>(16 * u + r))),
-                 mine + (16 * u + k * R) * (D / 2));
-        }
-    }
+    for (int u = 0; u < 4; ++u) copy_values<D>(c.codes[1] + at[u] * (D / 2), u, lane, mine);
   };
 
   if (todo > 0) {

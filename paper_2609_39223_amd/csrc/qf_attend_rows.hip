@@ -97,15 +97,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_rows_kernel(AttendArgs 
     at_v = place(tile, bad_vs);
     vs = load_scales(lane_at(c.scales[1] + at_v * SB, row_vs));
   };
-  auto copy_v = [&](int64_t at, char* to) {             // 16 tokens' codes, rows back to back, chunks exchanged
-    constexpr int C = D / 32, R = 64 / C;
-#pragma unroll
-    for (int i = 0; i < (16 + R - 1) / R; ++i) {
-      const int r = i * R + lane / C;
-      if (R <= 16 || lane < 16 * C)
-        copy16(lane_at(c.codes[1] + at * (D / 2), r * (D / 2) + 16 * ((lane % C) ^ v_swap<D>(16 * wv + r))), to + (16 * wv + i * R) * (D / 2));
-    }
-  };
+  auto copy_v = [&](int64_t at, char* to) { copy_values<D>(c.codes[1] + at * (D / 2), wv, lane, to); };
   auto put_scales = [&](int tile) {
     const bool seen = tile * kTile + 16 * wv + (lane >> 2) < todo && !bad_vs;
     const uint64_t special = __ballot(store_scales<FMT, T::KS>(seen ? vs : 0u, quarter(lane & 3), wv, lane, vscale[tile & 1]));
@@ -176,16 +168,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_rows_kernel(AttendArgs 
   }
 
   for (int k = 0; k < tiles; ++k) {
-    if (k + 2 < tiles) copy_v(at_next, raw[k & 1]);     // (V's codes of tile k were decoded a step ago)
-    const int64_t at_keys = at_next;
     if (k + 2 < tiles) put_scales(k + 2);
-    if (k + 1 < tiles) put_keys(k + 1);
-    if (k + 2 < tiles) load_k(at_keys);
+    if (k + 1 < tiles) {
+      put_keys(k + 1);
+      put_values(k + 1);
+    }
+    if (k + 2 < tiles) {                                // (after the use of what was loaded a step ago, or that would wait for these)
+      copy_v(at_next, raw[k & 1]);                      // (V's codes of tile k were decoded a step ago)
+      load_k(at_next);
+    }
     if (k + 3 < tiles) {
       load_vs(k + 3);
       at_next = at_v;
     }
-    if (k + 1 < tiles) put_values(k + 1);
 
     const int t0 = k * kTile, base = a0 + t0;
     if (base < wave_end) {
