@@ -305,40 +305,73 @@ __device__ __forceinline__ void decode_values(const char* codes, const _Float16*
   v1 = decode_f16((uint32_t)cw[1], s1);
 }
 
-// One step of a row's running softmax over the tile's 64 tokens, of which the lane holds scores z of 16 u + 4 g + i: it
-// sees those from `from` to below `to` that have a page (whole: no lane has to look).  Probabilities go to pw in FP16.
-template <int DT>
-__device__ __forceinline__ void softmax_step(float (&z)[16], float cz, int from, int to, bool whole, uint32_t bad, int g, float& m,
-                                             float& l, f32x4_t (&acc)[DT], uint32_t (&pw)[8]) {
-  if (!(whole && __all(to >= kTile && from <= 0))) {
+// The largest of the four lanes that hold one row: 16 and 32 lanes apart, exchanged without LDS.
+__device__ __forceinline__ float row_max(float x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const uint32_t v = __builtin_bit_cast(uint32_t, x);
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  x = fmaxf(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1]));
+  const uint32_t w = __builtin_bit_cast(uint32_t, x);
+  const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+  x = fmaxf(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
+#endif
+  return x;
+}
+
+// One step of the rows' running softmax over the tile's 64 tokens, of which the lane holds scores z of 16 u + 4 g + i: a
+// row sees those from `from` to below `to` that have a page (whole: no lane has to look).  Probabilities go to pw in FP16.
+// (All rows' maxima first, then one branch: taken one row after the other each waits for its own exchanges.)
+template <int DT, int NQ>
+__device__ __forceinline__ void softmax_step(float (&z)[NQ][16], const float (&cz)[NQ], const int (&from)[NQ], const int (&to)[NQ],
+                                             bool whole, uint32_t bad, int g, float (&m)[NQ], float (&l)[NQ], f32x4_t (&acc)[NQ][DT],
+                                             uint32_t (&pw)[NQ][8]) {
+  bool all = whole;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int t = 16 * (i >> 2) + 4 * g + (i & 3);
-      if (t < from || t >= to || ((bad >> (i >> 2)) & 1u)) z[i] = neg_inf();
+  for (int j = 0; j < NQ; ++j) all = all && to[j] >= kTile && from[j] <= 0;
+  if (!__all(all)) {
+#pragma unroll
+    for (int j = 0; j < NQ; ++j)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int t = 16 * (i >> 2) + 4 * g + (i & 3);
+        if (t < from[j] || t >= to[j] || ((bad >> (i >> 2)) & 1u)) z[j][i] = neg_inf();
+      }
+  }
+  float top[NQ];
+  bool grows = false;
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    top[j] = z[j][0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top[j] = fmaxf(top[j], z[j][i]);
+    // the reference is a whole number, so that adding it to 14 and powers of two of it are exact
+    top[j] = fmaxf(__builtin_ceilf(row_max(top[j]) * cz[j]), m[j]);
+    grows = grows || top[j] > m[j];
+  }
+  if (__any(grows)) {
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+      const float down = __builtin_amdgcn_exp2f(m[j] - (top[j] == neg_inf() ? 0.0f : top[j]));
+      l[j] *= down;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) acc[j][d] *= down;
+      m[j] = top[j];
     }
   }
-  float top = z[0];
 #pragma unroll
-  for (int i = 1; i < 16; ++i) top = fmaxf(top, z[i]);
-  top = fmaxf(top, __shfl_xor(top, 16, 64));
-  top = fmaxf(top, __shfl_xor(top, 32, 64));
-  // the reference is a whole number, so that adding it to 14 and powers of two of it are exact
-  top = fmaxf(__builtin_ceilf(top * cz), m);
-  if (__any(top > m)) {
-    const float down = __builtin_amdgcn_exp2f(m - (top == neg_inf() ? 0.0f : top));
-    l *= down;
+  for (int j = 0; j < NQ; ++j) {
+    const float up = top[j] == neg_inf() ? 0.0f : kUp - top[j];   // (nothing seen yet: probabilities of zero)
+    float sum[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int d = 0; d < DT; ++d) acc[d] *= down;
-    m = top;
+    for (int i = 0; i < 16; i += 2) {
+      const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][i], cz[j], up));
+      const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][i + 1], cz[j], up));
+      sum[0] += a;
+      sum[1] += b;
+      pw[j][i / 2] = pack_f16(a, b);
+    }
+    l[j] += sum[0] + sum[1];
   }
-  const float up = top == neg_inf() ? 0.0f : kUp - top;   // (nothing seen yet: probabilities of zero)
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    z[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[i], cz, up));
-    l += z[i];
-  }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) pw[i] = pack_f16(z[2 * i], z[2 * i + 1]);
 }
 
 // The special blocks of token r of the tile's 16 u .. added in FP32: scales sp and codes of the token, this lane's two

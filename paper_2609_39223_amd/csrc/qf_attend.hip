@@ -209,11 +209,13 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 && D == 256 ? 1 : NQ == 2 || D
       const int base = w0 + t0;
       const bool whole = t0 + kTile <= todo && bad_now == 0;
       uint32_t pw[NQ][8];
+      int from[NQ], to[NQ];
 #pragma unroll
       for (int j = 0; j < NQ; ++j) {
-        softmax_step<DT>(z[j], cz[j], p.window > 0 ? row_pos[j] - p.window + 1 - base : 0, min(row_pos[j] + 1 - base, todo - t0),
-                         whole, bad_now, g, m[j], l[j], acc[j], pw[j]);
+        from[j] = p.window > 0 ? row_pos[j] - p.window + 1 - base : 0;
+        to[j] = min(row_pos[j] + 1 - base, todo - t0);
       }
+      softmax_step<DT>(z, cz, from, to, whole, bad_now, g, m, l, acc, pw);
       // ---- outputs
       asm volatile("" ::: "memory");
       __builtin_amdgcn_s_waitcnt(0x0F70);               // vmcnt(0): this wave's copies of V are in its region

@@ -219,10 +219,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_rows_kernel(AttendArgs 
       }
       const bool whole = t0 + kTile <= todo && bad == 0;
       uint32_t pw[NQ][8];
+      int from[NQ], to[NQ];
 #pragma unroll
-      for (int j = 0; j < NQ; ++j)
-        softmax_step<DT>(z[j], cz[j], p.window > 0 ? row_pos[j] - p.window + 1 - base : 0, min(row_pos[j] + 1 - base, todo - t0), whole,
-                         bad, g, m[j], l[j], acc[j], pw[j]);
+      for (int j = 0; j < NQ; ++j) {
+        from[j] = p.window > 0 ? row_pos[j] - p.window + 1 - base : 0;
+        to[j] = min(row_pos[j] + 1 - base, todo - t0);
+      }
+      softmax_step<DT>(z, cz, from, to, whole, bad, g, m, l, acc, pw);
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         const uint4 v0 = values[k & 1][2 * d][lane], v1 = values[k & 1][2 * d + 1][lane];
