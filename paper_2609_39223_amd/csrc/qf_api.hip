@@ -1876,6 +1876,8 @@ qf_status qf_packed_matvec_grouped(const qf_packed* w, const int64_t* group_offs
 namespace {
 
 bool aligned_to(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+// A window that no sequence can fill is as good as any larger one.
+int64_t window_of(int64_t window) { return std::min<int64_t>(window, 1 << 30); }
 
 qf_status check_cache(const char* fn, const qf_kv_cache* c) {
   if (!c) return fail(QF_EINVAL, "%s: null cache", fn);
@@ -1968,7 +1970,7 @@ qf_status qf_kv_attention_workspace_size(const qf_kv_cache* c, const qf_kv_seqs*
   if (!bytes) return fail(QF_EINVAL, "%s: null output", fn);
   *bytes = 0;
   if (T > 0 && Hq > 0 && q->B > 0)
-    *bytes = up(qf::kv_attention_ws_bytes(cache_of(c), seqs_of(q, T), {nullptr, 0, nullptr, 0, nullptr, Hq, q->max_len, window, 0.0f}));
+    *bytes = up(qf::kv_attention_ws_bytes(cache_of(c), seqs_of(q, T), {nullptr, 0, nullptr, 0, nullptr, Hq, q->max_len, window_of(window), 0.0f}));
   return ok();
 }
 
@@ -1984,7 +1986,7 @@ qf_status qf_kv_attention(const qf_kv_cache* c, const qf_kv_seqs* q, int64_t T, 
   QF_TRY(check_kv_call(fn, c, q));
   const qf::KvCache kc = cache_of(c);
   const qf::KvSeqs ks = seqs_of(q, T);
-  const qf::AttendCall call{Q, ldq, O, ldo, lse, Hq, q->max_len, window, scale};
+  const qf::AttendCall call{Q, ldq, O, ldo, lse, Hq, q->max_len, window_of(window), scale};
   const size_t need = qf::kv_attention_ws_bytes(kc, ks, call);
   if (need > 0) QF_TRY(check_ws(fn, need, ws, ws_bytes));
   QF_TRY(dev(qf::launch_kv_attention(kc, ks, call, static_cast<float*>(ws), S(stream)), fn));

@@ -445,7 +445,7 @@ size_t kv_attention_ws_bytes(const KvCache& c, const KvSeqs& q, const AttendCall
 hipError_t launch_kv_attention(const KvCache& c, const KvSeqs& q, const AttendCall& a, float* ws, hipStream_t s) {
   const attend::Plan p = attend::plan_of(c, q, a);
   const attend::AttendArgs args{c, q, a, p.G, p.Gg, p.groups, p.tpt, p.splits, p.chunk, p.most,
-                        (int)std::min<int64_t>(a.window, INT32_MAX / 2), 0, ws};
+                        (int)a.window, 0, ws};
   return c.fmt == QF_FMT_NVFP4 ? attend::launch_d<QF_FMT_NVFP4>(args, p, s) : attend::launch_d<QF_FMT_MXFP4>(args, p, s);
 }
 

@@ -109,6 +109,8 @@ def test_attention_operands(L):
     assert size(ctypes.byref(c), ctypes.byref(q), I(6), I(8), I(300), ctypes.byref(n)) == QF_OK and n.value < long
     assert size(ctypes.byref(c), ctypes.byref(q), I(6), I(8), I(0), None) == QF_EINVAL
     assert size(ctypes.byref(c), ctypes.byref(q), I(6), I(9), I(0), ctypes.byref(n)) == QF_ESHAPE
+    for w in ((1 << 30) - 1, 1 << 40, (1 << 63) - 1):               # windows longer than any sequence are none
+        assert size(ctypes.byref(c), ctypes.byref(q), I(6), I(8), I(w), ctypes.byref(n)) == QF_OK and n.value == long
     q = seqs(max_len=200, cols=10000)                               # short sequences need none
     assert size(ctypes.byref(c), ctypes.byref(q), I(6), I(8), I(0), ctypes.byref(n)) == QF_OK and n.value == 0
     assert size(ctypes.byref(c), ctypes.byref(q), I(0), I(8), I(0), ctypes.byref(n)) == QF_OK and n.value == 0

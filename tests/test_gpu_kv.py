@@ -221,6 +221,14 @@ def test_windows(qf, fmt, window):
     _run(qf, fmt, [333, 64, 90], None, 2, 2, 64, 32, window=window, seed=window)
 
 
+def test_window_of_any_size(qf):
+    """Windows longer than any sequence equal none, to the largest that the type holds."""
+    want = _run(qf, "nvfp4", [3000, 90], None, 1, 2, 64, 32, seed=3)
+    for window in (3000, 1 << 31, (1 << 63) - 1):
+        got = _run(qf, "nvfp4", [3000, 90], None, 1, 2, 64, 32, window=window, seed=3)
+        assert window == 3000 or all(np.array_equal(a, b) for a, b in zip(want, got))
+
+
 @pytest.mark.parametrize("fmt", ["nvfp4", "mxfp4"])
 def test_long(qf, fmt):
     """Pieces that meet in the merge, pages of 16 (more than 64 a wave), an odd end, a sequence far shorter."""
