@@ -176,6 +176,16 @@ struct Few {
   }
 };
 
+// f as the sum of two bf16 halves: 2^-17 relative; an infinity or NaN in the first.  (Next to the largest float the
+// first would round up to an infinity, and the second with it.)
+__device__ __forceinline__ void split_halves(float f, uint32_t& hi, uint32_t& lo) {
+  hi = codec::bf16_rne(f);
+  lo = 0;
+  if (!__builtin_isfinite(f)) return;
+  if ((hi & 0x7FFFu) == 0x7F80u) --hi;
+  lo = codec::bf16_rne(f - codec::as_f32(hi << 16));
+}
+
 // z of adapter a's rows among 16; each wave a part of the slice, U steps of 32 at once.
 template <int TILES, bool HALVES>
 __device__ __forceinline__ void down_rows(const RowsArgs& p, f32x4_t (*part)[kDownWaves][64], const Group& grp, int a, int slice, int j0) {
@@ -230,10 +240,11 @@ __device__ __forceinline__ void down_rows(const RowsArgs& p, f32x4_t (*part)[kDo
       if constexpr (HALVES) {
         if (j >= p.s.r) continue;
         const float f = j < rank ? p.s.scale[a] * v[k] : 0.0f;
-        const uint32_t hi = codec::bf16_rne(f);
+        uint32_t hi, lo;
+        split_halves(f, hi, lo);
         uint16_t* const to = reinterpret_cast<uint16_t*>(p.z) + (int64_t)row * 2 * p.s.r + j;
         to[0] = (uint16_t)hi;
-        to[p.s.r] = __builtin_isfinite(f) ? (uint16_t)codec::bf16_rne(f - codec::as_f32(hi << 16)) : (uint16_t)0;
+        to[p.s.r] = (uint16_t)lo;
       } else {
         if (j < rank) p.z[((int64_t)slice * p.M + row) * p.s.r + j] = v[k];
       }
@@ -396,11 +407,8 @@ __device__ __forceinline__ void up_rows(const RowsArgs& p, const Group* grp, int
         }
         uint32_t hi[8], lo[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {        // (ranks past the last hold what lay there: not used)
-          const float x = j + i < rank ? s * z[i] : 0.0f;
-          hi[i] = codec::bf16_rne(x);
-          lo[i] = __builtin_isfinite(x) ? codec::bf16_rne(x - codec::as_f32(hi[i] << 16)) : 0u;
-        }
+        for (int i = 0; i < 8; ++i)          // (ranks past the last hold what lay there: not used)
+          split_halves(j + i < rank ? s * z[i] : 0.0f, hi[i], lo[i]);
         zh[b] = codec::pack8(hi);
         zl[b] = codec::pack8(lo);
       }

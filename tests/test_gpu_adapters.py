@@ -140,6 +140,20 @@ def test_non_finite_rows_and_adapters(qf):
     assert np.array_equal(np.isnan(got), bad) and np.array_equal(got[~bad], clean[~bad])
 
 
+@pytest.mark.parametrize("M", [5, 80])
+def test_sums_next_to_the_largest_float(qf, M):
+    """s z between the largest bf16 and the largest FP32 value, of either sign, is still finite times a small B."""
+    c = _case(np.random.default_rng(9), M, 1, 8, 8, 24, np.zeros(M))
+    bf = lambda v: int(np.float32(v).view(np.uint32)) >> 16  # noqa: E731
+    c["X"][:], c["A"][:], c["base"][:], c["scale"][:] = 0, 0, 0, 1
+    c["X"][:, 0], c["X"][:, 1], c["A"][:, 0, :2] = bf(2.0 ** 127 * (2 - 2.0 ** -7)), bf(1.5 * 2.0 ** 119), bf(1)
+    c["X"][1::2, :2] |= 0x8000
+    c["B"][:] = bf(2.0 ** -20)
+    got, ref = _run(qf, c), _ref(c)
+    assert np.abs(ref[0]).min() > 2.0 ** 107
+    _check(got, *ref, 8, 8, False)
+
+
 def test_no_adapters_and_no_columns(qf):
     c = _case(np.random.default_rng(7), 20, 3, 8, 64, 40, np.full(20, 2))
     bf = lambda a: to_dev(a).view(torch.bfloat16)  # noqa: E731
