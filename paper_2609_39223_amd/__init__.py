@@ -738,6 +738,8 @@ def kv_sequences(lens, table, offsets=None, max_len=None) -> KvSeqs:
     (None: what the table's rows hold, known when a cache is).  Holds references to the tensors, whose values
     may change between calls."""
     B, cols = table.shape
+    if max_len is not None and max_len < 0:
+        raise ValueError("max_len is negative")
     q = KvSeqs(B, _typed(offsets, torch.int64, "offsets", (B + 1,)), _dense(lens, torch.int32, "lens", (B,)),
                _dense(table, torch.int32, "table"), cols, -1 if max_len is None else max_len)
     q._tensors = (offsets, lens, table)

@@ -498,6 +498,8 @@ def test_python_refusals(qf):
         qf.kv_sequences(lens.long(), table)
     with pytest.raises(ValueError):
         qf.kv_sequences(lens[:1], table)
+    with pytest.raises(ValueError):
+        qf.kv_sequences(lens, table, max_len=-3)
     seqs = qf.kv_sequences(lens, table)
     x = torch.zeros(2, 64, dtype=torch.bfloat16, device="cuda")
     with pytest.raises(ValueError):
