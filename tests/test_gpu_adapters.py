@@ -154,6 +154,30 @@ def test_sums_next_to_the_largest_float(qf, M):
     _check(got, *ref, 8, 8, False)
 
 
+@pytest.mark.parametrize("M,n,r,K,N", [(100, 9000, 8, 8, 8), (70000, 3, 8, 8, 8), (200, 2, 256, 72, 40), (129, 1, 24, 40, 300)])
+def test_many_rows_or_adapters(qf, M, n, r, K, N):
+    """More adapters or rows than are put in order first, the widest rank, two and three groups of rows of one adapter."""
+    c = _case(np.random.default_rng(M + n), M, n, r, K, N)
+    _check(_run(qf, c), *_ref(c), r, K, False)
+    _check(_run(qf, c, f32=True, inplace=True), *_ref(c), r, K, True)
+
+
+@pytest.mark.parametrize("M", [3, 90])
+def test_nothing_to_sum(qf, M):
+    """K = 0, or no adapters at all: base alone."""
+    rng = np.random.default_rng(10)
+    bf = lambda a: to_dev(a).view(torch.bfloat16)  # noqa: E731
+    base, ids = workloads.normal_bf16(rng, (M, 40)), to_dev(rng.integers(-1, 3, M).astype(np.int32))
+    for n, K in ((2, 0), (0, 64), (0, 0)):
+        e = lambda *s: torch.empty(s, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+        a = qf.adapters(e(n, 8, K), e(n, 40, 8).fill_(1), torch.ones(n, device="cuda"))
+        ws = qf.lora_rows_workspace(a, M)
+        ws.fill_(0xFF)
+        Y = e(M, 40).fill_(7)
+        qf.lora_rows(a, ids, e(M, K), Y, ws, base=bf(base))
+        assert torch.equal(Y, bf(base))
+
+
 def test_no_adapters_and_no_columns(qf):
     c = _case(np.random.default_rng(7), 20, 3, 8, 64, 40, np.full(20, 2))
     bf = lambda a: to_dev(a).view(torch.bfloat16)  # noqa: E731
