@@ -6,7 +6,8 @@
 // first finds the places of its tokens, one a thread (binary search in the offsets, length, page: four trips to
 // memory one after the other), and leaves them in LDS; rows to be written are loaded meanwhile.  NVFP4's tensor
 // scale S is given per head, so one pass suffices.  Bound by memory: 2 bytes an element one way, 0.53 or 0.56
-// the other; few tokens by the trips.
+// the other; few tokens by the trips.  32768 tokens x 1024 of K and of V read back (MXFP4): 41 us, 4.1 TB/s;
+// 13600 x 1024 written (NVFP4): 27 us, 2.6 TB/s, the vector units nearly as busy (maxima, a division, 16 codes).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -190,11 +191,14 @@ hipError_t launch_n(KvRows p, hipStream_t s) {
   return hipSuccess;
 }
 
-// Tokens a lane takes: as many as leave every compute unit a workgroup of 256 lanes or two.
+// Tokens a lane takes, by lanes of one token each in units of two workgroups a compute unit (8 heads of 128; us,
+// writing / reading NVFP4):  4 units (2048 tokens)  1: 12.2 / 5.9   2: 11.5 / 5.6
+//   8 (4096)  1: 18.9 / 8.7   2: 14.6 / 6.7   8: 16.3 / 7.4     16 (8192)  2: 23.6 / 11.6   8: 22.7 / 10.2
+// (4 a lane at 13600 tokens: 49.0 us for both directions, 16: 50.1, 8: 48.1.)
 template <int FMT, bool READ>
 hipError_t launch_rows(const KvRows& p, hipStream_t s) {
   const int64_t lanes = p.q.T * (2 * p.c.H * p.c.D / 8), unit = 512 * compute_units();
-  return lanes >= 8 * unit ? launch_n<FMT, READ, 8>(p, s) : lanes >= 2 * unit ? launch_n<FMT, READ, 2>(p, s) : launch_n<FMT, READ, 1>(p, s);
+  return lanes >= 10 * unit ? launch_n<FMT, READ, 8>(p, s) : lanes >= 2 * unit ? launch_n<FMT, READ, 2>(p, s) : launch_n<FMT, READ, 1>(p, s);
 }
 
 }  // namespace
