@@ -9,7 +9,11 @@
 //                   counting sort in LDS; the places of equal ones do not matter to any result).  Rows of other
 //                   adapters among them ride along in the products and are not stored.
 // More rows or adapters than the sort takes (2^16, 2^13) are taken as they come.
-// Bound by memory: the factors of the adapters in use (few rows), base and Y (many).
+// Bound by memory: base and Y of many rows (4099 of 6 adapters, rank 32, 4096 x 24576, bf16: 143 us, of them 110 up at
+// 3.7 TB/s, 28 down, 7 the order; factors read again by every 32 rows from L2), the factors in use of few (61 of
+// 24, rank 64, 4096 x 4096: 16 us, two launches of 8), and launches (16 of 16, rank 16, 4096 x 6144: 9.7 us).  What did not
+// pay: a wave that goes over columns with the next ones on their way (186 us for 143), base and Y past the caches
+// (149, 150, both 156), 16 rows a workgroup for 32 (155).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -516,8 +520,10 @@ Plan plan_of(const AdapterSet& s, int64_t M) {
   p.sorted = M > kFew && M <= kSortRows && s.n <= kSortAdapters;
   p.rb = M <= kFew ? 0 : M / n >= 64 ? 2 : 1;
   p.groups = p.rb == 0 ? 1 : (M + 16 * p.rb - 1) / (16 * p.rb);
-  // adapters among 16 sorted rows: about one more than adapters a group
-  p.abreast = p.rb == 0 ? (int)n : p.rb == 2 ? 1 : (int)std::min<int64_t>({16, n, 1 + 16 * n / M});
+  // adapters among 16 sorted rows, one more than there would be if every group began with a new one, side by side
+  // (100 rows of 10 adapters, 4096 x 8192: 25.5 -> 17.1 us, 2048 of 100: 43.6 -> 38.1), unless there are workgroups
+  // enough without the last, which few groups need (4099 of 6, 24576 wide: 143 us, with it 150)
+  p.abreast = p.rb == 0 ? (int)n : (int)std::min<int64_t>({16, n, 1 + (16 * n + (M < 12 * cus ? M - 1 : 0)) / M});
   const int64_t each = p.groups * p.abreast, want = (2 * cus + each - 1) / each;
   const int64_t slices = p.rb ? 1 : std::min(want, std::min<int64_t>(std::max<int64_t>(1, s.K / 1024), 4));
   p.kc = (int)((std::max<int64_t>(s.K, 1) + slices - 1) / slices + 255) / 256 * 256;
@@ -574,7 +580,8 @@ hipError_t launch_lora_rows(const AdapterSet& s, const int32_t* ids, int64_t M, 
   const int64_t wide = std::max<int64_t>(cols, 2 * p.slices * ranks * std::max(p.rb, 1));
   const int64_t fit = std::max<int64_t>(1, ((int64_t)1 << 22) / (wide * p.abreast));
   for (int64_t g = 0; g < p.groups; g += fit) {
-    const unsigned x = (unsigned)(std::min(fit, p.groups - g) * p.abreast);
+    const unsigned groups = (unsigned)std::min(fit, p.groups - g), x = groups * (unsigned)p.abreast;
+    a.abreast = p.abreast;
     if (s.n > 0 && (s.K > 0 || p.rb > 0)) {  // (the halves of no sum are zeros)
       a.group0 = (int)(g * std::max(p.rb, 1));
       const dim3 grid(x * (unsigned)std::max(p.rb, 1), (unsigned)p.slices, ranks);
@@ -585,7 +592,8 @@ hipError_t launch_lora_rows(const AdapterSet& s, const int32_t* ids, int64_t M, 
       if (e != hipSuccess) return e;
     }
     a.group0 = (int)g;
-    const dim3 grid((unsigned)((p.rb == 0 ? x + 1 : x) * cols));
+    if (p.rb == 2) a.abreast = 1;            // (groups of one adapter nearly all)
+    const dim3 grid((unsigned)((p.rb == 0 ? x + 1 : groups * (unsigned)a.abreast) * cols));
     if (y_f32) launch_up<true>(a, p.rb, grid, stream);
     else launch_up<false>(a, p.rb, grid, stream);
     const hipError_t e = hipGetLastError();
