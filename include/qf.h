@@ -830,7 +830,7 @@ QF_API qf_status qf_kv_read(const qf_kv_cache* c, const qf_kv_seqs* q, int64_t T
  * A row that sees nothing (no tokens, positions below zero, pages that are none) gets zeros and -inf.
  * Tokens without a page are not seen, positions from max_len on neither; rows that belong to nobody are
  * left alone.  K and V count as their codes decode (not rounded to bf16); sums, maxima and normalizers are
- * FP32, probabilities are rounded to FP16 relative to the row's largest (2^-12 each, 2^-39 absolute).
+ * FP32, probabilities are rounded to FP16 relative to the row's largest (2^-11 each, 2^-38 absolute).
  * A NaN or infinity in q makes its row NaN; NaN scales reach the rows that see their tokens, and no others.
  * MXFP4 values of 2^100 or more may come out infinite; blocks of V with scale code 0 count as zeros.
  *   ws     qf_kv_attention_workspace_size bytes of the same cache sizes, sequences' sizes (B, cols, max_len,

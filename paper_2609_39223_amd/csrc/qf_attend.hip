@@ -19,9 +19,16 @@
 // -20 <= p <= 7; blocks with any other scale (but 0, the code of a block of zeros), and under both
 // formats blocks with NaN scales, are "special" and added one by one in FP32, which also keeps an
 // infinity or NaN away from the rows that do not see it.
-// Probabilities are rounded to FP16 as 2^14 exp(z - max): relative 2^-12 down to 2^-28 of the row's
-// largest and absolute 2^-39 of it below, so that many small ones still sum.  The sum of
+// Probabilities are rounded to FP16 as 2^14 exp(z - max): relative 2^-11 down to 2^-28 of the row's
+// largest and absolute 2^-38 of it below, so that many small ones still sum.  The sum of
 // probabilities is of the unrounded ones, in FP32.
+// Bound by memory where the batch fills the card: 64 sequences x 8192 tokens x 8 heads of 128 (NVFP4, 4 rows a
+// head) 115 us, 5.3 TB/s; its loads alone take 103.  One sequence of 131072: 39 us, 3.9 TB/s, loads alone 33.  With
+// several rows a head (5 drafted tokens) by the softmax, 16 exponents a lane, row and 64 tokens, and by what
+// decoding costs each wave; short sequences by trips to memory one after the other (row, length, page, codes), 7 us.
+// What did not pay: four or two workgroups a compute unit for three (registers spilled at 128: 127 us for 117),
+// waves taking every fourth tile of the piece instead of a quarter of it (129), workgroups of 8 or 16 waves
+// (129 - 144), 64 rows a wave.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -311,15 +318,17 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 && D == 256 ? 1 : NQ == 2 || D
   }
 }
 
-// One workgroup a row: its pieces' sums, brought to the largest maximum.  A lane takes 4 of the row's elements of
-// every (256 / (D / 4))-th piece with a running maximum of its own, so no load waits for another.
-template <int FMT, int D>
+// A row's pieces' sums, brought to the largest maximum.  A lane takes 4 of the row's elements of every P-th piece with
+// a running maximum of its own, so no load waits for another; D / 4 P lanes have a row, all of a workgroup
+// (P = 256 / (D / 4), its parts meet in LDS) or, for few pieces, a wave or less (P = 1).
+template <int FMT, int D, int P>
 __global__ __launch_bounds__(256) void merge_kernel(AttendArgs p) {
-  constexpr int L = D / 4, P = 256 / L;
+  constexpr int L = D / 4, ROWS = 256 / (L * P);
   __shared__ f32x4_t sum[P][L];
   __shared__ float top_of[P], l_of[P];
-  const int tid = threadIdx.x, e = tid % L, part = tid / L;
-  const int64_t row = (int64_t)p.item0 + blockIdx.x, t = row / p.a.Hq, R = p.q.T * p.a.Hq;
+  const int tid = threadIdx.x, e = tid % L, part = P == 1 ? 0 : tid / L;
+  const int64_t R = p.q.T * p.a.Hq, row = (int64_t)p.item0 + (int64_t)blockIdx.x * ROWS + (P == 1 ? tid / L : 0), t = row / p.a.Hq;
+  if (P == 1 && row >= R) return;
   const int hq = (int)(row - t * p.a.Hq);
   f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
   float top = neg_inf(), l = 0.0f;
@@ -344,30 +353,32 @@ __global__ __launch_bounds__(256) void merge_kernel(AttendArgs p) {
     }
   }
   if (p.q.off && t >= p.q.off[p.q.B]) return;           // a row of nobody: nothing was written for it
-  sum[part][e] = acc;
-  if (e == 0) {
-    top_of[part] = top;
-    l_of[part] = l;
-  }
-  __syncthreads();
-  if (tid >= L) return;
+  if constexpr (P > 1) {
+    sum[part][e] = acc;
+    if (e == 0) {
+      top_of[part] = top;
+      l_of[part] = l;
+    }
+    __syncthreads();
+    if (tid >= L) return;
 #pragma unroll
-  for (int i = 0; i < P; ++i) top = fmaxf(top, top_of[i]);
-  const float ref = top == neg_inf() ? 0.0f : top;
-  acc = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-  l = 0.0f;
+    for (int i = 0; i < P; ++i) top = fmaxf(top, top_of[i]);
+    const float ref = top == neg_inf() ? 0.0f : top;
+    acc = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    l = 0.0f;
 #pragma unroll
-  for (int i = 0; i < P; ++i) {
-    const float f = __builtin_amdgcn_exp2f(top_of[i] - ref);
-    acc += f * sum[i][tid];
-    l += f * l_of[i];
+    for (int i = 0; i < P; ++i) {
+      const float f = __builtin_amdgcn_exp2f(top_of[i] - ref);
+      acc += f * sum[i][tid];
+      l += f * l_of[i];
+    }
   }
   const float f = l == 0.0f ? 0.0f : (FMT == QF_FMT_NVFP4 ? p.c.S[1][hq / p.G] : 0x1p-6f) / l;
   uint32_t w[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) w[k] = codec::bf16_rne(l == 0.0f ? 0.0f : acc[k] * f);
-  *reinterpret_cast<uint2*>(p.a.O + t * p.a.ldo + (int64_t)hq * D + 4 * tid) = make_uint2(w[0] | (w[1] << 16), w[2] | (w[3] << 16));
-  if (p.a.lse && tid == 0) p.a.lse[row] = l == 0.0f ? neg_inf() : (top + (__builtin_log2f(l) - kUp)) * kLn2;
+  *reinterpret_cast<uint2*>(p.a.O + t * p.a.ldo + (int64_t)hq * D + 4 * e) = make_uint2(w[0] | (w[1] << 16), w[2] | (w[3] << 16));
+  if (p.a.lse && e == 0) p.a.lse[row] = l == 0.0f ? neg_inf() : (top + (__builtin_log2f(l) - kUp)) * kLn2;
 }
 
 // ------------------------------------------------------------------------------ the launch rules
@@ -382,15 +393,26 @@ Plan plan_of(const KvCache& c, const KvSeqs& q, const AttendCall& a) {
   p.groups = (p.G + 15) / 16;
   p.Gg = (p.G + p.groups - 1) / p.groups;
   // rows a sequence has on average: from 17 on 32 a wave, so that keys and values are decoded once for both
-  // halves; from 128 on the kernel that shares the decoded ones between waves (heads of 256 do not fit it)
+  // halves; from 128 on the kernel that shares the decoded ones between waves (heads of 256 do not fit it).  16
+  // sequences x 4096 tokens x 8 heads of 128, us with 16 a wave / 32 a wave / shared:  16 rows 27 / 29 / 53,
+  // 20 rows 40 / 30 / 53, 64 rows 65 / 45 / 59, 128 rows 87 / 69 / 66, 512 rows 295 / 243 / 178
   const int64_t rows = q.off ? q.T / std::max<int64_t>(q.B, 1) * p.Gg : 1;
   p.nq = rows <= 16 ? 1 : rows < kManyRows || c.D == 256 ? 2 : 0;
   p.tpt = (p.nq ? 16 * p.nq : kManyRows) / p.Gg;
   p.items = q.off ? q.T / p.tpt + q.B : q.B;
-  // pieces of the tokens: enough workgroups for the card, none of less than one tile a wave
+  // pieces of the tokens: two workgroups a compute unit (one sequence of 131072: one 48 us, two 38, three 38, four
+  // 42, eight 47; 20 of 8192: 59, 47, 47, 50, 51), none of less than one tile a wave (4 of 2048: pieces of 256
+  // 10.2 us, of 512 11.9)
   p.most = c.pages == 0 ? 0 : (int)std::min(a.max_len, q.cols << c.page_log);
   const int64_t longest = std::max<int64_t>(1, a.window > 0 ? std::min<int64_t>(p.most, a.window + p.tpt + 15) : p.most);
-  const int64_t tiles = std::max<int64_t>(1, p.items * p.groups * c.H), want = (2 * compute_units() + tiles - 1) / tiles;
+  // (the row tiles of sequences with as many rows each: p.items, the most that there can be, has up to twice as
+  // many, and 16 sequences of 8 new tokens took 45 us for 32)
+  const int64_t each = q.off ? (q.T + q.B * p.tpt - 1) / (q.B * p.tpt) : 1;
+  const int64_t tiles = std::max<int64_t>(1, q.B * each * p.groups * c.H), goal = 2 * compute_units();
+  int64_t want = (goal + tiles - 1) / tiles;
+  if (want > 1 && tiles * want > (p.nq == 1 ? 3 : 2) * compute_units()) --want;
+  // (no more than run at one time: 16 sequences of 24 new tokens in 768 workgroups, 512 of them at a time, took 86
+  // us, in 384 69)
   const int64_t least = kWaves * kTile;
   const int64_t chunk = (longest + want - 1) / want;
   p.chunk = (int)((chunk + least - 1) / least * least);
@@ -398,13 +420,13 @@ Plan plan_of(const KvCache& c, const KvSeqs& q, const AttendCall& a) {
   return p;
 }
 
-template <int FMT, int D>
+template <int FMT, int D, int P>
 hipError_t merge(AttendArgs a, hipStream_t s) {
-  if (a.splits == 1) return hipSuccess;
-  const int64_t R = a.q.T * a.a.Hq, step = (int64_t)1 << 23;
+  constexpr int64_t rows = 256 / (D / 4 * P);
+  const int64_t R = a.q.T * a.a.Hq, step = rows << 23;
   for (int64_t r = 0; r < R; r += step) {
     a.item0 = (int)r;
-    hipLaunchKernelGGL((merge_kernel<FMT, D>), dim3((unsigned)std::min(step, R - r)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((merge_kernel<FMT, D, P>), dim3((unsigned)((std::min(step, R - r) + rows - 1) / rows)), dim3(256), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -426,7 +448,9 @@ hipError_t launch(AttendArgs a, const Plan& p, hipStream_t s) {
 template <int FMT, int D>
 hipError_t launch_nq(const AttendArgs& a, const Plan& p, hipStream_t s) {
   const hipError_t e = p.nq == 0 ? launch_rows(a, p.items, s) : p.nq == 2 ? launch<FMT, D, 2>(a, p, s) : launch<FMT, D, 1>(a, p, s);
-  return e == hipSuccess ? merge<FMT, D>(a, s) : e;
+  if (e != hipSuccess || a.splits == 1) return e;
+  // (a whole workgroup for 32 rows of 64 pieces: 37 us of attention, less 50; for 9600 rows of 6 pieces: 86, less 82)
+  return a.splits <= (a.q.T * a.a.Hq < 4096 ? 4 : 8) ? merge<FMT, D, 1>(a, s) : merge<FMT, D, 1024 / D>(a, s);
 }
 
 template <int FMT>

@@ -9,8 +9,11 @@
 // codes are on their way are three different ones, so there is one barrier a tile:
 //   step k   copies of V's codes of tile k + 2 to LDS, its scales to FP16 in LDS; K's codes of k + 1 (loaded in
 //            step k - 1) and V's (in LDS since then) decoded; tile k multiplied.
-// Bound by the vector units (per 64 x 32 scores 16 exponents, a maximum, a sum and a quarter of the decode) and by
-// LDS (32 KB of operands a wave and tile, as long as its 64 MFMAs take).
+// 2048 new tokens behind 8192, 32 heads over 8, 128 wide (NVFP4): 405 us, 0.76 PFLOP/s; 32 rows a wave that each decode
+// for themselves took 502, 16 rows 601, 64 rows 608.  Bound by what the two waves of a SIMD do one after the other:
+// vector units busy half of the time (per row and token an exponent, a maximum, a sum, conversions; the decode),
+// matrix units 30 %, LDS 30 % (32 KB of operands a wave and tile).  Scores of the next tile between the
+// exponents of this one need more registers than there are (spilled, 487 us).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
