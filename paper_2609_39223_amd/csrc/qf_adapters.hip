@@ -525,7 +525,9 @@ Plan plan_of(const AdapterSet& s, int64_t M) {
   // enough without the last, which few groups need (4099 of 6, 24576 wide: 143 us, with it 150)
   p.abreast = p.rb == 0 ? (int)n : (int)std::min<int64_t>({16, n, 1 + (16 * n + (M < 12 * cus ? M - 1 : 0)) / M});
   const int64_t each = p.groups * p.abreast, want = (2 * cus + each - 1) / each;
-  const int64_t slices = p.rb ? 1 : std::min(want, std::min<int64_t>(std::max<int64_t>(1, s.K / 1024), 4));
+  // slices of K for few rows, 1024 each (61 rows, K 4096, us by slices of 4096 / 2048 / 1024 / 512 / 256: 26.6 / 20.0 /
+  // 16.3 / 17.2 / 20.8), 16 at most (one row, K 16384, 1 / 2 / 4 / 8 / 16: 69 / 40 / 26 / 20 / 19)
+  const int64_t slices = p.rb ? 1 : std::min(want, std::min<int64_t>(std::max<int64_t>(1, s.K / 1024), 16));
   p.kc = (int)((std::max<int64_t>(s.K, 1) + slices - 1) / slices + 255) / 256 * 256;
   p.slices = (int)std::max<int64_t>(1, (s.K + p.kc - 1) / p.kc);
   return p;

@@ -449,8 +449,9 @@ template <int FMT, int D>
 hipError_t launch_nq(const AttendArgs& a, const Plan& p, hipStream_t s) {
   const hipError_t e = p.nq == 0 ? launch_rows(a, p.items, s) : p.nq == 2 ? launch<FMT, D, 2>(a, p, s) : launch<FMT, D, 1>(a, p, s);
   if (e != hipSuccess || a.splits == 1) return e;
-  // (a whole workgroup for 32 rows of 64 pieces: 37 us of attention, less 50; for 9600 rows of 6 pieces: 86, less 82)
-  return a.splits <= (a.q.T * a.a.Hq < 4096 ? 4 : 8) ? merge<FMT, D, 1>(a, s) : merge<FMT, D, 1024 / D>(a, s);
+  // (a whole workgroup for 32 rows of 64 pieces: 37 us of attention, less 50; for 9600 rows of
+  // 6 pieces 86, less 82; for 2560 rows of 5 17.7, less 17.2; for 64 rows of 8 10.1, less 11.0)
+  return a.splits <= (a.q.T * a.a.Hq < 2048 ? 4 : 8) ? merge<FMT, D, 1>(a, s) : merge<FMT, D, 1024 / D>(a, s);
 }
 
 template <int FMT>
