@@ -270,6 +270,17 @@ def test_many_sequences(qf, fmt):
     _run(qf, fmt, [int(v) for v in rng.integers(0, 40, 150)], None, 1, 2, 64, 16, seed=9)
 
 
+@pytest.mark.parametrize("B", [1, 2, 62, 63, 64, 65, 128])
+@pytest.mark.parametrize("many", [4, 60])
+def test_numbers_of_sequences(qf, B, many):
+    """Around one wave of sequences, the first and last without new tokens or with the most."""
+    for ends in (0, many):
+        rng = np.random.default_rng(B + ends)
+        new = [int(v) for v in rng.integers(0, many, B)]
+        new[0], new[-1] = ends, many - ends
+        _run(qf, "nvfp4", [n + int(rng.integers(0, 30)) for n in new], new, 1, 4, 64, 16, seed=B, extra=1)
+
+
 @pytest.mark.parametrize("fmt", ["nvfp4", "mxfp4"])
 @pytest.mark.parametrize("new", [None, [20, 1, 40], [100, 16, 150]])
 def test_bad_pages(qf, fmt, new):
