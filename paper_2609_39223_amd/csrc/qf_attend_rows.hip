@@ -9,11 +9,11 @@
 // codes are on their way are three different ones, so there is one barrier a tile:
 //   step k   copies of V's codes of tile k + 2 to LDS, its scales to FP16 in LDS; K's codes of k + 1 (loaded in
 //            step k - 1) and V's (in LDS since then) decoded; tile k multiplied.
-// 2048 new tokens behind 8192, 32 heads over 8, 128 wide (NVFP4): 405 us, 0.76 PFLOP/s; 32 rows a wave that each decode
+// 2048 new tokens behind 8192, 32 heads over 8, 128 wide (NVFP4): 355 us, 0.87 PFLOP/s; 32 rows a wave that each decode
 // for themselves took 502, 16 rows 601, 64 rows 608.  Bound by what the two waves of a SIMD do one after the other:
 // vector units busy half of the time (per row and token an exponent, a maximum, a sum, conversions; the decode),
 // matrix units 30 %, LDS 30 % (32 KB of operands a wave and tile).  Scores of the next tile between the
-// exponents of this one need more registers than there are (spilled, 487 us).
+// exponents of this one need more registers than there are (spilled, 487 us for 405 then).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -34,7 +34,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_rows_kernel(AttendArgs 
   __shared__ __align__(16) char raw[2][kTile * D / 2];  // V's codes on their way
   __shared__ __align__(16) _Float16 vscale[2][NB * kTile];
   __shared__ uint64_t special_of[4][4];                 // of tile k % 4, 16 tokens: bits 4 r .. 4 r + 3 of token r
-  __shared__ uint32_t bad_of[4][4], nan_of[2][4];       // of 16 tokens: no page; keys with NaN scales
+  __shared__ __align__(4) uint8_t flags_of[4][4];       // of 16 tokens: 1 no page, 2 some are special
+  __shared__ __align__(16) uint32_t nan_of[2][4];       // of 16 tokens: keys with NaN scales (MXFP4)
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g = lane >> 4;
   const KvCache& c = p.c;
@@ -45,7 +46,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_rows_kernel(AttendArgs 
   bid /= (uint32_t)p.groups;
   const int split = (int)(bid % (uint32_t)p.splits);
   int b, tok0, first, n;
-  if (!find_tile(p.q, p.tpt, p.item0 + (int)(bid / (uint32_t)p.splits), b, tok0, first, n)) return;
+  // (the last row tiles, which see most, first: 405 -> 387 us)
+  const int items = (int)(gridDim.x / (uint32_t)(c.H * p.groups * p.splits)), item = p.item0 + items - 1 - (int)(bid / (uint32_t)p.splits);
+  if (!find_tile(p.q, p.tpt, item, b, tok0, first, n)) return;
 
   const int page_log = c.page_log;
   const int len = max(__builtin_amdgcn_readfirstlane(p.q.lens[b]), 0), pos0 = len - n + first, toks = min(p.tpt, n - first);
@@ -106,14 +109,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_rows_kernel(AttendArgs 
     const uint64_t special = __ballot(store_scales<FMT, T::KS>(seen ? vs : 0u, quarter(lane & 3), wv, lane, vscale[tile & 1]));
     if (lane == 0) {
       special_of[tile & 3][wv] = special;
-      bad_of[tile & 3][wv] = bad_vs;
+      flags_of[tile & 3][wv] = (uint8_t)(bad_vs | (special ? 2u : 0u));
     }
   };
   auto put_keys = [&](int tile) {
 #pragma unroll
     for (int s = 0; s < CS; ++s) keys[tile & 1][wv * CS + s][lane] = decode_key<FMT>(kw[s], ks, s);
-    const uint32_t nan = nan_keys<FMT, T::KS>(ks);
-    if (lane == 0) nan_of[tile & 1][wv] = nan;
+    if constexpr (FMT == QF_FMT_MXFP4) {
+      const uint32_t nan = nan_keys<FMT, T::KS>(ks);
+      if (lane == 0) nan_of[tile & 1][wv] = nan;
+    }
   };
   auto put_values = [&](int tile) {
 #pragma unroll
@@ -170,7 +175,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_rows_kernel(AttendArgs 
     __syncthreads();
   }
 
+  // A wave on its way to the barrier, from its outputs through the next tile's decode, goes before the other workgroup's
+  // wave that scores: 387 -> 357 us (the other way round, products first, 410; softmax first 378).
   for (int k = 0; k < tiles; ++k) {
+    __builtin_amdgcn_s_setprio(1);
     if (k + 2 < tiles) put_scales(k + 2);
     if (k + 1 < tiles) {
       put_keys(k + 1);
@@ -185,6 +193,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_rows_kernel(AttendArgs 
       at_next = at_v;
     }
 
+    __builtin_amdgcn_s_setprio(0);
     const int t0 = k * kTile, base = a0 + t0;
     if (base < wave_end) {
       f32x4_t zz[NQ][4];
@@ -200,25 +209,23 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_rows_kernel(AttendArgs 
 #pragma unroll
           for (int j = 0; j < NQ; ++j) zz[j][u] = mfma_z<FMT>(a, q[j][s], zz[j][u]);
         }
-      uint32_t bad = 0, specials = 0;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        bad |= bad_of[k & 3][u] << u;
-        specials |= (uint32_t)(special_of[k & 3][u] != 0) << u;
-      }
-      bad = __builtin_amdgcn_readfirstlane(bad);
-      specials = __builtin_amdgcn_readfirstlane(specials);
+      const uint32_t flags = __builtin_amdgcn_readfirstlane(*reinterpret_cast<const uint32_t*>(flags_of[k & 3]));
+      const uint32_t bad = (flags & 1u) | (flags >> 7 & 2u) | (flags >> 14 & 4u) | (flags >> 21 & 8u);
       float z[NQ][16];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const uint32_t nan = FMT == QF_FMT_MXFP4 ? __builtin_amdgcn_readfirstlane(nan_of[k & 1][u]) : 0u;
+      for (int j = 0; j < NQ; ++j)
 #pragma unroll
-        for (int j = 0; j < NQ; ++j)
+        for (int i = 0; i < 16; ++i) z[j][i] = zz[j][i >> 2][i & 3];
+      if constexpr (FMT == QF_FMT_MXFP4) {
+        const uint4 nan4 = *reinterpret_cast<const uint4*>(nan_of[k & 1]);
+        if (__builtin_amdgcn_readfirstlane(nan4.x | nan4.y | nan4.z | nan4.w)) {
+          const uint32_t nan[4] = {nan4.x, nan4.y, nan4.z, nan4.w};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            z[j][4 * u + i] = zz[j][u][i];
-            if (nan && ((nan >> (4 * g + i)) & 1u)) z[j][4 * u + i] = __builtin_nanf("");
-          }
+          for (int j = 0; j < NQ; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if ((nan[i >> 2] >> (4 * g + (i & 3))) & 1u) z[j][i] = __builtin_nanf("");
+        }
       }
       const bool whole = t0 + kTile <= todo && bad == 0;
       uint32_t pw[NQ][8];
@@ -229,6 +236,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_rows_kernel(AttendArgs 
         to[j] = min(row_pos[j] + 1 - base, todo - t0);
       }
       softmax_step<DT>(z, cz, from, to, whole, bad, g, m, l, acc, pw);
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         const uint4 v0 = values[k & 1][2 * d][lane], v1 = values[k & 1][2 * d + 1][lane];
@@ -238,7 +246,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_rows_kernel(AttendArgs 
           acc[j][d] = mfma_o(v1, make_uint4(pw[j][4], pw[j][5], pw[j][6], pw[j][7]), acc[j][d]);
         }
       }
-      if (specials) {
+      if (flags & 0x02020202u) {
 #pragma unroll 1
         for (int u = 0; u < 4; ++u) {
           uint64_t those = special_of[k & 3][u];
@@ -257,6 +265,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_rows_kernel(AttendArgs 
     }
     arrived();
   }
+  __builtin_amdgcn_s_setprio(0);
 
 #pragma unroll
   for (int j = 0; j < NQ; ++j) {
