@@ -9,10 +9,10 @@
 //                   counting sort in LDS; the places of equal ones do not matter to any result).  Rows of other
 //                   adapters among them ride along in the products and are not stored.
 // More rows or adapters than the sort takes (2^16, 2^13) are taken as they come.
-// Bound by memory: base and Y of many rows (4099 of 6 adapters, rank 32, 4096 x 24576, bf16: 143 us, of them 110 up at
-// 3.7 TB/s, 28 down, 7 the order; factors read again by every 32 rows from L2), the factors in use of few (61 of
+// Bound by memory: base and Y of many rows (4099 of 6 adapters, rank 32, 4096 x 24576, bf16: 126 us, of them 95 up at
+// 4.3 TB/s, 28 down, 7 the order; factors read again by every 32 rows from L2), the factors in use of few (61 of
 // 24, rank 64, 4096 x 4096: 16 us, two launches of 8), and launches (16 of 16, rank 16, 4096 x 6144: 9.7 us).  What did not
-// pay: a wave that goes over columns with the next ones on their way (186 us for 143), base and Y past the caches
+// pay: a wave that goes over columns with the next ones on their way (186 us for 143 then), base and Y past the caches
 // (149, 150, both 156), 16 rows a workgroup for 32 (155).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -357,13 +357,19 @@ struct Eight {
   }
 };
 
+// A lane's part of base and Y: 8 columns from 8 (lane % 8) on of rows lane / 8 and lane / 8 + 8, so that the eight lanes of
+// a row are neighbours.  (The products leave a row to lane % 16; loads and stores in that order, the same 64 bytes a
+// row in lanes 16 apart, took 111 us for 4099 x 24576, 95 now.)
+__device__ __forceinline__ int row_of(int lane, int half) { return (lane >> 3) + 8 * half; }
+constexpr int kRowWords = kCols + 4;         // a row of sums in LDS: four banks further than the one before
+
 // 64 columns from n0 on of adapter a's rows among 16 RB.  The products are taken transposed, the factor's rows n
 // against the 16 rows of z, and tile t of a pair holds n = 8 (i / 4) + 4 t + i % 4 in its row i, so that a lane ends up
-// with 8 neighbouring columns of its row.
+// with 8 neighbouring columns of its row; `sums`, the wave's, takes them to the lanes that store them.
 template <bool F32, int STEPS, int RB, bool HALVES>
-__device__ __forceinline__ void up_rows(const RowsArgs& p, const Group* grp, int a, int n0) {
+__device__ __forceinline__ void up_rows(const RowsArgs& p, float* sums, const Group* grp, int a, int n0) {
   const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, N = (int)p.s.N, r = p.s.r;
-  const int rank = rank_of(p.s, a);
+  const int rank = rank_of(p.s, a), n_mine = n0 + 8 * (lane & 7);
   const uint16_t* const B = p.s.B + (int64_t)a * N * r;
   Eight<F32> v[RB][2];
   f32x4_t acc[RB][4];
@@ -371,9 +377,9 @@ __device__ __forceinline__ void up_rows(const RowsArgs& p, const Group* grp, int
   for (int b = 0; b < RB; ++b) {
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      const int n = n0 + 32 * c + 8 * g;
+      const int row = __shfl(grp[b].row, row_of(lane, c), 64), id = __shfl(grp[b].id, row_of(lane, c), 64);
       v[b][c].zero();
-      if (p.base && grp[b].id == a && n < N) v[b][c].load(p.base, grp[b].row * p.ldb + n, N - n);
+      if (p.base && id == a && n_mine < N) v[b][c].load(p.base, row * p.ldb + n_mine, N - n_mine);
     }
 #pragma unroll
     for (int t = 0; t < 4; ++t) acc[b][t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
@@ -428,29 +434,33 @@ __device__ __forceinline__ void up_rows(const RowsArgs& p, const Group* grp, int
     }
   }
 #pragma unroll
-  for (int b = 0; b < RB; ++b)
-    if (grp[b].id == a) {
+  for (int b = 0; b < RB; ++b) {
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const int n = n0 + 32 * c + 8 * g;
-        if (n >= N) break;
-        float y[8];
+    for (int t = 0; t < 4; ++t)
+      *reinterpret_cast<f32x4_t*>(sums + l16 * kRowWords + 32 * (t >> 1) + 8 * g + 4 * (t & 1)) = acc[b][t];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = v[b][c].get(i) + acc[b][2 * c + (i >> 2)][i & 3];
-        v[b][c].store(p.Y, grp[b].row * p.ldy + n, N - n, y);
-      }
+    for (int c = 0; c < 2; ++c) {
+      const int row = __shfl(grp[b].row, row_of(lane, c), 64), id = __shfl(grp[b].id, row_of(lane, c), 64);
+      const float* const from = sums + row_of(lane, c) * kRowWords + 8 * (lane & 7);
+      const f32x4_t s0 = *reinterpret_cast<const f32x4_t*>(from), s1 = *reinterpret_cast<const f32x4_t*>(from + 4);
+      if (id != a || n_mine >= N) continue;
+      float y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = v[b][c].get(i) + (i < 4 ? s0[i & 3] : s1[i & 3]);
+      v[b][c].store(p.Y, row * p.ldy + n_mine, N - n_mine, y);
     }
+  }
 }
 
-// Rows without an adapter.
+// Rows without an adapter: row of lane % 16, -1: none.
 template <bool F32>
-__device__ __forceinline__ void copy_row(const RowsArgs& p, int row, int n0) {
-  if (row < 0 || p.base == p.Y) return;
-  const int g = (threadIdx.x & 63) >> 4, N = (int)p.s.N;
+__device__ __forceinline__ void copy_rows(const RowsArgs& p, int rows, int n0) {
+  if (p.base == p.Y) return;
+  const int lane = threadIdx.x & 63, N = (int)p.s.N, n = n0 + 8 * (lane & 7);
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
-    const int n = n0 + 32 * c + 8 * g;
-    if (n >= N) break;
+    const int row = __shfl(rows, row_of(lane, c), 64);
+    if (row < 0 || n >= N) continue;
     Eight<F32> v;
     v.zero();
     if (p.base) v.load(p.base, row * p.ldb + n, N - n);
@@ -468,6 +478,8 @@ template <bool F32, int STEPS, int RB>
 __global__ __launch_bounds__(64 * kUpWaves) void up_kernel(RowsArgs p) {
   const uint32_t bx = blockIdx.x / (uint32_t)p.cols;
   const int n0 = ((int)(blockIdx.x % (uint32_t)p.cols) * kUpWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * kCols;
+  __shared__ __align__(16) float all_sums[kUpWaves][16 * kRowWords];
+  float* const sums = all_sums[threadIdx.x >> 6];
   if (n0 >= p.s.N) return;
   if constexpr (RB == 0) {
     const int z0 = (int)bx;
@@ -475,11 +487,11 @@ __global__ __launch_bounds__(64 * kUpWaves) void up_kernel(RowsArgs p) {
     if (z0 < p.abreast) {
       while (few.rows) {
         const Group g = few.next();
-        up_rows<F32, STEPS, 1, false>(p, &g, few.a, n0);
+        up_rows<F32, STEPS, 1, false>(p, sums, &g, few.a, n0);
       }
     } else {                                 // (the rows without an adapter as if they had one)
       few.rows = __ballot((int)(threadIdx.x & 63) < p.M && few.id < 0);
-      while (few.rows) copy_row<F32>(p, few.next().row, n0);
+      while (few.rows) copy_rows<F32>(p, few.next().row, n0);
     }
   } else {
     const int place = (p.group0 + (int)bx / p.abreast) * 16 * RB, z0 = (int)bx % p.abreast;
@@ -492,17 +504,17 @@ __global__ __launch_bounds__(64 * kUpWaves) void up_kernel(RowsArgs p) {
 #pragma unroll
       for (int b = 0; b < RB; ++b) one = one && (grp[b].id == a || grp[b].row < 0);
       if (__all(one)) {
-        up_rows<F32, STEPS, RB, true>(p, grp, a, n0);
+        up_rows<F32, STEPS, RB, true>(p, sums, grp, a, n0);
         return;
       }
     }
 #pragma unroll 1
     for (int b = 0; b < RB; ++b) {
       const Group g = RB == 1 ? grp[0] : group_at(p, place + 16 * b);
-      if (z0 == 0) copy_row<F32>(p, g.id < 0 ? g.row : -1, n0);
+      if (z0 == 0) copy_rows<F32>(p, g.id < 0 ? g.row : -1, n0);
       int i = 0;
       for (uint32_t left = firsts_of(g); left; left &= left - 1, ++i)
-        if (i % p.abreast == z0) up_rows<F32, STEPS, 1, true>(p, &g, __builtin_amdgcn_readlane(g.id, __builtin_ctz(left)), n0);
+        if (i % p.abreast == z0) up_rows<F32, STEPS, 1, true>(p, sums, &g, __builtin_amdgcn_readlane(g.id, __builtin_ctz(left)), n0);
     }
   }
 }
@@ -522,7 +534,7 @@ Plan plan_of(const AdapterSet& s, int64_t M) {
   p.groups = p.rb == 0 ? 1 : (M + 16 * p.rb - 1) / (16 * p.rb);
   // adapters among 16 sorted rows, one more than there would be if every group began with a new one, side by side
   // (100 rows of 10 adapters, 4096 x 8192: 25.5 -> 17.1 us, 2048 of 100: 43.6 -> 38.1), unless there are workgroups
-  // enough without the last, which few groups need (4099 of 6, 24576 wide: 143 us, with it 150)
+  // enough without the last, which few groups need (4099 of 6, 24576 wide: down 28 us, with it 35)
   p.abreast = p.rb == 0 ? (int)n : (int)std::min<int64_t>({16, n, 1 + (16 * n + (M < 12 * cus ? M - 1 : 0)) / M});
   const int64_t each = p.groups * p.abreast, want = (2 * cus + each - 1) / each;
   // slices of K for few rows, 1024 each (61 rows, K 4096, us by slices of 4096 / 2048 / 1024 / 512 / 256: 26.6 / 20.0 /
