@@ -9,8 +9,8 @@
 //                   counting sort in LDS; the places of equal ones do not matter to any result).  Rows of other
 //                   adapters among them ride along in the products and are not stored.
 // More rows or adapters than the sort takes (2^16, 2^13) are taken as they come.
-// Bound by memory: base and Y of many rows (4099 of 6 adapters, rank 32, 4096 x 24576, bf16: 126 us, of them 95 up at
-// 4.3 TB/s, 28 down, 7 the order; factors read again by every 32 rows from L2), the factors in use of few (61 of
+// Bound by memory: base and Y of many rows (4099 of 6 adapters, rank 32, 4096 x 24576, bf16: 115 us, of them 95 up at
+// 4.3 TB/s, 19 down, 7 the order; factors read again by every 32 rows from L2), the factors in use of few (61 of
 // 24, rank 64, 4096 x 4096: 16 us, two launches of 8), and launches (16 of 16, rank 16, 4096 x 6144: 9.7 us).  What did not
 // pay: a wave that goes over columns with the next ones on their way (186 us for 143 then), base and Y past the caches
 // (149, 150, both 156), 16 rows a workgroup for 32 (155).
@@ -190,45 +190,110 @@ __device__ __forceinline__ void split_halves(float f, uint32_t& hi, uint32_t& lo
   lo = codec::bf16_rne(f - codec::as_f32(hi << 16));
 }
 
-// z of adapter a's rows among 16; each wave a part of the slice, U steps of 32 at once.
+// Where chunk c (16 bytes of 128) of row r of 16 lies in a wave's LDS: reads of 16 rows' chunks c meet different banks.
+__device__ __forceinline__ int chunk_at(int r, int c) { return r * 8 + (c ^ (r & 7)); }
 template <int TILES, bool HALVES>
-__device__ __forceinline__ void down_rows(const RowsArgs& p, f32x4_t (*part)[kDownWaves][64], const Group& grp, int a, int slice, int j0) {
-  constexpr int U = 4;
+constexpr bool kDownStaged = HALVES && TILES <= 2;
+// A workgroup's LDS: the waves' operands of 64 k (staged), afterwards their sums.
+template <int TILES, bool HALVES>
+constexpr int kDownLds = kDownWaves * (kDownStaged<TILES, HALVES> ? (TILES + 1) * 2048 : TILES * 1024);
+
+// z of adapter a's rows among 16; each wave a part of the slice, 128 k at once.  Of many rows and up to 32 ranks 128 bytes
+// a row are loaded, by eight lanes each, and go through LDS to the lanes that multiply them (staged; 4099 rows of 6
+// adapters, rank 32, K 4096: 18.7 us; loaded as they are multiplied, 64 bytes of 16 rows, every line is asked for
+// twice: 28.5).  With more ranks, or 128 k a wave in all, the way through LDS costs more than it saves (4000 rows of
+// 9, rank 256: 235 us in all for 185; 61 rows of 24, rank 64: 12.3 for 8.9).
+template <int TILES, bool HALVES>
+__device__ __forceinline__ void down_rows(const RowsArgs& p, char* smem, const Group& grp, int a, int slice, int j0) {
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4;
   const int K = (int)p.s.K, k_hi = min((slice + 1) * p.kc, K), per = (p.kc / kDownWaves + 31) / 32 * 32;
   const int w_lo = slice * p.kc + wv * per, w_hi = min(w_lo + per, k_hi), rank = rank_of(p.s, a);
-  const uint16_t* const x = p.X + max(grp.row, 0) * p.ldx;
-  const uint16_t* f[TILES];
-#pragma unroll
-  for (int t = 0; t < TILES; ++t) f[t] = p.s.A + ((int64_t)a * p.s.r + min(j0 + 16 * t + l16, p.s.r - 1)) * K;
+  const uint16_t* const A = p.s.A + (int64_t)a * p.s.r * K;
   f32x4_t acc[TILES];
 #pragma unroll
   for (int t = 0; t < TILES; ++t) acc[t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
   int k0 = w_lo;
-  for (; k0 + 32 * U <= w_hi; k0 += 32 * U) {
-    uint4 xv[U], av[U][TILES];
+  if constexpr (kDownStaged<TILES, HALVES>) {
+    constexpr int P = 2;
+    // operand 0: X's rows, 1 ..: A's; this lane's rows of 128 bytes are lane / 8 and lane / 8 + 8
+    const uint16_t* src[TILES + 1][2];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int k = k0 + 32 * u + 8 * g;
+    for (int h = 0; h < 2; ++h) {
+      const int r = (lane >> 3) + 8 * h;
+      src[0][h] = p.X + max(__shfl(grp.row, r, 64), 0) * p.ldx + 8 * (lane & 7);
 #pragma unroll
-      for (int t = 0; t < TILES; ++t) av[u][t] = *reinterpret_cast<const uint4*>(f[t] + k);
-      xv[u] = *reinterpret_cast<const uint4*>(x + k);
+      for (int t = 0; t < TILES; ++t) src[t + 1][h] = A + (int64_t)min(j0 + 16 * t + r, p.s.r - 1) * K + 8 * (lane & 7);
     }
+    uint4* const stage = reinterpret_cast<uint4*>(smem) + wv * (TILES + 1) * 128;
+    // 64 k that lie in LDS
+    auto multiply = [&]() {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+      for (int u = 0; u < 2; ++u) {
+        const uint4 xv = stage[chunk_at(l16, 4 * u + g)];
 #pragma unroll
-      for (int t = 0; t < TILES; ++t) acc[t] = mfma(xv[u], av[u][t], acc[t]);
-  }
+        for (int t = 0; t < TILES; ++t) acc[t] = mfma(xv, stage[(t + 1) * 128 + chunk_at(l16, 4 * u + g)], acc[t]);
+      }
+    };
+    for (; k0 + 64 * P <= w_hi; k0 += 64 * P) {
+      uint4 v[P][TILES + 1][2];
+#pragma unroll
+      for (int i = 0; i < P; ++i)
+#pragma unroll
+        for (int o = 0; o <= TILES; ++o)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) v[i][o][h] = *reinterpret_cast<const uint4*>(src[o][h] + k0 + 64 * i);
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+#pragma unroll
+        for (int o = 0; o <= TILES; ++o)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) stage[o * 128 + chunk_at((lane >> 3) + 8 * h, lane & 7)] = v[i][o][h];
+        multiply();
+      }
+    }
 #pragma unroll 1
-  for (; k0 < w_hi; k0 += 32) {              // the rest of the wave's part
-    const int k = k0 + 8 * g;
-    const uint4 xv = k < w_hi ? *reinterpret_cast<const uint4*>(x + k) : make_uint4(0, 0, 0, 0);
+    for (; k0 < w_hi; k0 += 64) {              // the rest of the wave's part, zeros behind it
 #pragma unroll
-    for (int t = 0; t < TILES; ++t) {
-      const uint4 av = k < w_hi ? *reinterpret_cast<const uint4*>(f[t] + k) : make_uint4(0, 0, 0, 0);
-      acc[t] = mfma(xv, av, acc[t]);
+      for (int o = 0; o <= TILES; ++o)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          stage[o * 128 + chunk_at((lane >> 3) + 8 * h, lane & 7)] =
+              k0 + 8 * (lane & 7) < w_hi ? *reinterpret_cast<const uint4*>(src[o][h] + k0) : make_uint4(0, 0, 0, 0);
+      multiply();
+    }
+    __syncthreads();
+  } else {
+    constexpr int U = 4;
+    const uint16_t* const x = p.X + max(grp.row, 0) * p.ldx;
+    const uint16_t* f[TILES];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) f[t] = A + (int64_t)min(j0 + 16 * t + l16, p.s.r - 1) * K;
+    for (; k0 + 32 * U <= w_hi; k0 += 32 * U) {
+      uint4 xv[U], av[U][TILES];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int k = k0 + 32 * u + 8 * g;
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) av[u][t] = *reinterpret_cast<const uint4*>(f[t] + k);
+        xv[u] = *reinterpret_cast<const uint4*>(x + k);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) acc[t] = mfma(xv[u], av[u][t], acc[t]);
+    }
+#pragma unroll 1
+    for (; k0 < w_hi; k0 += 32) {            // the rest of the wave's part
+      const int k = k0 + 8 * g;
+      const uint4 xv = k < w_hi ? *reinterpret_cast<const uint4*>(x + k) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int t = 0; t < TILES; ++t) {
+        const uint4 av = k < w_hi ? *reinterpret_cast<const uint4*>(f[t] + k) : make_uint4(0, 0, 0, 0);
+        acc[t] = mfma(xv, av, acc[t]);
+      }
     }
   }
+  f32x4_t(*const part)[kDownWaves][64] = reinterpret_cast<f32x4_t(*)[kDownWaves][64]>(smem);
 #pragma unroll
   for (int t = 0; t < TILES; ++t) part[t][wv][lane] = acc[t];
   __syncthreads();
@@ -260,20 +325,20 @@ __device__ __forceinline__ void down_rows(const RowsArgs& p, f32x4_t (*part)[kDo
 // Grid: (16 places and adapter, slice, 64 ranks); FEW: up to 64 rows.
 template <int TILES, bool FEW>
 __global__ __launch_bounds__(64 * kDownWaves) void down_kernel(RowsArgs p) {
-  __shared__ f32x4_t part[TILES][kDownWaves][64];
+  __shared__ __align__(16) char smem[kDownLds<TILES, !FEW>];
   const int slice = blockIdx.y, j0 = blockIdx.z * 16 * kRankTiles;
   if constexpr (FEW) {
     Few few(p, blockIdx.x);
     while (few.rows) {
       const Group g = few.next();
-      down_rows<TILES, false>(p, part, g, few.a, slice, j0);
+      down_rows<TILES, false>(p, smem, g, few.a, slice, j0);
     }
   } else {
     const int z0 = blockIdx.x % p.abreast;
     const Group g = group_at(p, (p.group0 + (int)(blockIdx.x / p.abreast)) * 16);
     int i = 0;
     for (uint32_t left = firsts_of(g); left; left &= left - 1, ++i)
-      if (i % p.abreast == z0) down_rows<TILES, true>(p, part, g, __builtin_amdgcn_readlane(g.id, __builtin_ctz(left)), slice, j0);
+      if (i % p.abreast == z0) down_rows<TILES, true>(p, smem, g, __builtin_amdgcn_readlane(g.id, __builtin_ctz(left)), slice, j0);
   }
 }
 
@@ -534,7 +599,7 @@ Plan plan_of(const AdapterSet& s, int64_t M) {
   p.groups = p.rb == 0 ? 1 : (M + 16 * p.rb - 1) / (16 * p.rb);
   // adapters among 16 sorted rows, one more than there would be if every group began with a new one, side by side
   // (100 rows of 10 adapters, 4096 x 8192: 25.5 -> 17.1 us, 2048 of 100: 43.6 -> 38.1), unless there are workgroups
-  // enough without the last, which few groups need (4099 of 6, 24576 wide: down 28 us, with it 35)
+  // enough without the last, which few groups need (4099 of 6, 24576 wide: down 28 us then, with it 35)
   p.abreast = p.rb == 0 ? (int)n : (int)std::min<int64_t>({16, n, 1 + (16 * n + (M < 12 * cus ? M - 1 : 0)) / M});
   const int64_t each = p.groups * p.abreast, want = (2 * cus + each - 1) / each;
   // slices of K for few rows, 1024 each (61 rows, K 4096, us by slices of 4096 / 2048 / 1024 / 512 / 256: 26.6 / 20.0 /
