@@ -9,8 +9,8 @@
 //                   counting sort in LDS; the places of equal ones do not matter to any result).  Rows of other
 //                   adapters among them ride along in the products and are not stored.
 // More rows or adapters than the sort takes (2^16, 2^13) are taken as they come.
-// Bound by memory: base and Y of many rows (4099 of 6 adapters, rank 32, 4096 x 24576, bf16: 115 us, of them 95 up at
-// 4.3 TB/s, 19 down, 7 the order; factors read again by every 32 rows from L2), the factors in use of few (61 of
+// Bound by memory: base and Y of many rows (4099 of 6 adapters, rank 32, 4096 x 24576, bf16: 118 us, of them 97 up at
+// 4.2 TB/s, 19 down, 7 the order; factors read again by every 32 rows from L2), the factors in use of few (61 of
 // 24, rank 64, 4096 x 4096: 16 us, two launches of 8), and launches (16 of 16, rank 16, 4096 x 6144: 9.7 us).  What did not
 // pay: a wave that goes over columns with the next ones on their way (186 us for 143 then), base and Y past the caches
 // (149, 150, both 156), 16 rows a workgroup for 32 (155).
@@ -193,16 +193,16 @@ __device__ __forceinline__ void split_halves(float f, uint32_t& hi, uint32_t& lo
 // Where chunk c (16 bytes of 128) of row r of 16 lies in a wave's LDS: reads of 16 rows' chunks c meet different banks.
 __device__ __forceinline__ int chunk_at(int r, int c) { return r * 8 + (c ^ (r & 7)); }
 template <int TILES, bool HALVES>
-constexpr bool kDownStaged = HALVES && TILES <= 2;
+constexpr bool kDownStaged = HALVES && TILES == 2;
 // A workgroup's LDS: the waves' operands of 64 k (staged), afterwards their sums.
 template <int TILES, bool HALVES>
 constexpr int kDownLds = kDownWaves * (kDownStaged<TILES, HALVES> ? (TILES + 1) * 2048 : TILES * 1024);
 
-// z of adapter a's rows among 16; each wave a part of the slice, 128 k at once.  Of many rows and up to 32 ranks 128 bytes
+// z of adapter a's rows among 16; each wave a part of the slice, 128 k at once.  Of many rows and 17 to 32 ranks 128 bytes
 // a row are loaded, by eight lanes each, and go through LDS to the lanes that multiply them (staged; 4099 rows of 6
 // adapters, rank 32, K 4096: 18.7 us; loaded as they are multiplied, 64 bytes of 16 rows, every line is asked for
-// twice: 28.5).  With more ranks, or 128 k a wave in all, the way through LDS costs more than it saves (4000 rows of
-// 9, rank 256: 235 us in all for 185; 61 rows of 24, rank 64: 12.3 for 8.9).
+// twice: 28.5).  Elsewhere the way through LDS costs more than it saves (in all, staged and not: 4000 rows of 200
+// adapters, rank 16, 80.5 and 70.9 us; of 9, rank 256, 235 and 185; 61 rows of 24, rank 64, 20.5 and 17.2).
 template <int TILES, bool HALVES>
 __device__ __forceinline__ void down_rows(const RowsArgs& p, char* smem, const Group& grp, int a, int slice, int j0) {
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4;
@@ -214,7 +214,7 @@ __device__ __forceinline__ void down_rows(const RowsArgs& p, char* smem, const G
   for (int t = 0; t < TILES; ++t) acc[t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
   int k0 = w_lo;
   if constexpr (kDownStaged<TILES, HALVES>) {
-    constexpr int P = 2;
+    constexpr int P = 2;                       // 64 k that are under way at a time
     // operand 0: X's rows, 1 ..: A's; this lane's rows of 128 bytes are lane / 8 and lane / 8 + 8
     const uint16_t* src[TILES + 1][2];
 #pragma unroll
@@ -422,29 +422,33 @@ struct Eight {
   }
 };
 
-// A lane's part of base and Y: 8 columns from 8 (lane % 8) on of rows lane / 8 and lane / 8 + 8, so that the eight lanes of
-// a row are neighbours.  (The products leave a row to lane % 16; loads and stores in that order, the same 64 bytes a
-// row in lanes 16 apart, took 111 us for 4099 x 24576, 95 now.)
+// A row of 16 by neighbouring lanes, 8 columns each: lane's rows are lane / 8 and lane / 8 + 8.
 __device__ __forceinline__ int row_of(int lane, int half) { return (lane >> 3) + 8 * half; }
 constexpr int kRowWords = kCols + 4;         // a row of sums in LDS: four banks further than the one before
 
 // 64 columns from n0 on of adapter a's rows among 16 RB.  The products are taken transposed, the factor's rows n
 // against the 16 rows of z, and tile t of a pair holds n = 8 (i / 4) + 4 t + i % 4 in its row i, so that a lane ends up
-// with 8 neighbouring columns of its row; `sums`, the wave's, takes them to the lanes that store them.
+// with 8 neighbouring columns of row lane % 16.  Of many rows base and Y go by whole lines, 128 bytes a row, and the sums to
+// their lanes through LDS (`sums`, the wave's): 4099 x 24576 95 us, 111 with 64 bytes of 16 rows at a time; of few rows
+// (HALVES false) that way costs more (61 of 24 adapters 17.1 us for 16.5).
 template <bool F32, int STEPS, int RB, bool HALVES>
 __device__ __forceinline__ void up_rows(const RowsArgs& p, float* sums, const Group* grp, int a, int n0) {
   const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, N = (int)p.s.N, r = p.s.r;
-  const int rank = rank_of(p.s, a), n_mine = n0 + 8 * (lane & 7);
+  const int rank = rank_of(p.s, a);
   const uint16_t* const B = p.s.B + (int64_t)a * N * r;
+  constexpr bool LINES = HALVES;
   Eight<F32> v[RB][2];
   f32x4_t acc[RB][4];
+  auto row_mine = [&](int b, int c) { return LINES ? __shfl(grp[b].row, row_of(lane, c), 64) : grp[b].row; };
+  auto id_mine = [&](int b, int c) { return LINES ? __shfl(grp[b].id, row_of(lane, c), 64) : grp[b].id; };
+  auto n_mine = [&](int c) { return n0 + (LINES ? 8 * (lane & 7) : 32 * c + 8 * g); };
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      const int row = __shfl(grp[b].row, row_of(lane, c), 64), id = __shfl(grp[b].id, row_of(lane, c), 64);
+      const int row = row_mine(b, c), id = id_mine(b, c), n = n_mine(c);
       v[b][c].zero();
-      if (p.base && id == a && n_mine < N) v[b][c].load(p.base, row * p.ldb + n_mine, N - n_mine);
+      if (p.base && id == a && n < N) v[b][c].load(p.base, row * p.ldb + n, N - n);
     }
 #pragma unroll
     for (int t = 0; t < 4; ++t) acc[b][t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
@@ -500,19 +504,25 @@ __device__ __forceinline__ void up_rows(const RowsArgs& p, float* sums, const Gr
   }
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
+    if constexpr (LINES) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-      *reinterpret_cast<f32x4_t*>(sums + l16 * kRowWords + 32 * (t >> 1) + 8 * g + 4 * (t & 1)) = acc[b][t];
+      for (int t = 0; t < 4; ++t)
+        *reinterpret_cast<f32x4_t*>(sums + l16 * kRowWords + 32 * (t >> 1) + 8 * g + 4 * (t & 1)) = acc[b][t];
+    }
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      const int row = __shfl(grp[b].row, row_of(lane, c), 64), id = __shfl(grp[b].id, row_of(lane, c), 64);
-      const float* const from = sums + row_of(lane, c) * kRowWords + 8 * (lane & 7);
-      const f32x4_t s0 = *reinterpret_cast<const f32x4_t*>(from), s1 = *reinterpret_cast<const f32x4_t*>(from + 4);
-      if (id != a || n_mine >= N) continue;
+      const int row = row_mine(b, c), id = id_mine(b, c), n = n_mine(c);
+      f32x4_t s0 = acc[b][2 * c], s1 = acc[b][2 * c + 1];
+      if constexpr (LINES) {
+        const float* const from = sums + row_of(lane, c) * kRowWords + 8 * (lane & 7);
+        s0 = *reinterpret_cast<const f32x4_t*>(from);
+        s1 = *reinterpret_cast<const f32x4_t*>(from + 4);
+      }
+      if (id != a || n >= N) continue;
       float y[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) y[i] = v[b][c].get(i) + (i < 4 ? s0[i & 3] : s1[i & 3]);
-      v[b][c].store(p.Y, row * p.ldy + n_mine, N - n_mine, y);
+      v[b][c].store(p.Y, row * p.ldy + n, N - n, y);
     }
   }
 }
@@ -543,8 +553,8 @@ template <bool F32, int STEPS, int RB>
 __global__ __launch_bounds__(64 * kUpWaves) void up_kernel(RowsArgs p) {
   const uint32_t bx = blockIdx.x / (uint32_t)p.cols;
   const int n0 = ((int)(blockIdx.x % (uint32_t)p.cols) * kUpWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * kCols;
-  __shared__ __align__(16) float all_sums[kUpWaves][16 * kRowWords];
-  float* const sums = all_sums[threadIdx.x >> 6];
+  __shared__ __align__(16) float all_sums[RB > 0 ? kUpWaves : 1][RB > 0 ? 16 * kRowWords : 4];
+  float* const sums = all_sums[RB > 0 ? threadIdx.x >> 6 : 0];
   if (n0 >= p.s.N) return;
   if constexpr (RB == 0) {
     const int z0 = (int)bx;
