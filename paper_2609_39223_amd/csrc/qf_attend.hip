@@ -395,7 +395,7 @@ Plan plan_of(const KvCache& c, const KvSeqs& q, const AttendCall& a) {
   // rows a sequence has on average: from 17 on 32 a wave, so that keys and values are decoded once for both
   // halves; from 128 on the kernel that shares the decoded ones between waves (heads of 256 do not fit it).  16
   // sequences x 4096 tokens x 8 heads of 128, us with 16 a wave / 32 a wave / shared:  16 rows 27 / 29 / 53,
-  // 20 rows 40 / 30 / 53, 64 rows 65 / 45 / 59, 128 rows 87 / 69 / 66, 512 rows 295 / 243 / 178
+  // 20 rows 40 / 30 / 53, 64 rows 65 / 45 / 59, 128 rows 87 / 69 / 62, 512 rows 295 / 243 / 156
   const int64_t rows = q.off ? q.T / std::max<int64_t>(q.B, 1) * p.Gg : 1;
   p.nq = rows <= 16 ? 1 : rows < kManyRows || c.D == 256 ? 2 : 0;
   p.tpt = (p.nq ? 16 * p.nq : kManyRows) / p.Gg;

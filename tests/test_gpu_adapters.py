@@ -154,9 +154,11 @@ def test_sums_next_to_the_largest_float(qf, M):
     _check(got, *ref, 8, 8, False)
 
 
-@pytest.mark.parametrize("M,n,r,K,N", [(100, 9000, 8, 8, 8), (70000, 3, 8, 8, 8), (200, 2, 256, 72, 40), (129, 1, 24, 40, 300)])
+@pytest.mark.parametrize("M,n,r,K,N", [(100, 9000, 8, 8, 8), (70000, 3, 8, 8, 8), (200, 2, 256, 72, 40), (129, 1, 24, 40, 300),
+                                       (200, 3, 24, 2056, 40), (150, 2, 32, 4168, 264), (90, 20, 32, 1024, 64), (130, 4, 16, 2312, 72)])
 def test_many_rows_or_adapters(qf, M, n, r, K, N):
-    """More adapters or rows than are put in order first, the widest rank, two and three groups of rows of one adapter."""
+    """More adapters or rows than are put in order first, the widest rank, two and three groups of rows of one adapter,
+    sums long enough for every loop, with odd ends."""
     c = _case(np.random.default_rng(M + n), M, n, r, K, N)
     _check(_run(qf, c), *_ref(c), r, K, False)
     _check(_run(qf, c, f32=True, inplace=True), *_ref(c), r, K, True)
