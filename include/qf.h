@@ -768,7 +768,7 @@ QF_API qf_status qf_packed_matvec_grouped(const qf_packed* w, const int64_t* gro
  *   k_codes, v_codes    [pages, H, page, D/2] bytes, element 2i in the low nibble.
  *   k_scales, v_scales  [pages, H, page, D/16] E4M3 (NVFP4) or [pages, H, page, D/32] E8M0 (MXFP4).
  *   k_S, v_S FP32 [H], NVFP4 only: the heads' tensor decode scales (a calibrated amax / 2688), positive
- *            and fixed while the cache lives.  No alignment needed.
+ *            and fixed while the cache lives.  4-byte aligned.
  * Codes and scales are 16-byte aligned.
  */
 typedef struct {
@@ -835,6 +835,7 @@ QF_API qf_status qf_kv_read(const qf_kv_cache* c, const qf_kv_seqs* q, int64_t T
  * MXFP4 values of 2^100 or more may come out infinite; blocks of V with scale code 0 count as zeros.
  *   ws     qf_kv_attention_workspace_size bytes of the same cache sizes, sequences' sizes (B, cols, max_len,
  *          with or without offsets), T, Hq and window, 256-byte aligned; may be NULL where that is 0.
+ * O must not overlap Q or the cache; calls that may run at the same time need workspaces of their own.
  * Limits: T Hq < 2^30, Hq / H <= 512.  Deterministic: the order of the sums depends on these sizes alone.
  */
 QF_API qf_status qf_kv_attention_workspace_size(const qf_kv_cache* c, const qf_kv_seqs* q, int64_t T,
@@ -851,7 +852,7 @@ QF_API qf_status qf_kv_attention(const qf_kv_cache* c, const qf_kv_seqs* q, int6
  *   scale   FP32 [n] (alpha / r).
  *   ranks   int32 [n] or NULL (all r): adapter a uses the first ranks[a] rows of A[a] and columns of B[a],
  *           whatever the others hold.
- * scale and ranks need no alignment.
+ * scale and ranks 4-byte aligned.
  */
 typedef struct {
     int64_t n, r, N, K;
@@ -870,6 +871,7 @@ typedef struct {
  *          not overlap.
  *   Y      bf16 (y_f32 = 0) or FP32 (y_f32 = 1) [M, N] (row stride ldy).
  *   ws     qf_lora_rows_workspace_size bytes, 256-byte aligned.
+ * Calls that may run at the same time need workspaces of their own.
  * Rows of an adapter may lie anywhere; they cost least side by side.  FP32 sums in a fixed order; X A^T is
  * taken into the second product as the sum of two bf16 halves (2^-17 relative), Y rounded once.
  * Limits: M < 2^24, N < 2^24, K < 2^30, n < 2^30.
