@@ -1901,6 +1901,8 @@ qf_status check_kv_call(const char* fn, const qf_kv_cache* c, const qf_kv_seqs* 
   }
   if (c->fmt == QF_FMT_NVFP4 && (!c->k_S || !c->v_S)) return fail(QF_EINVAL, "%s: NVFP4 needs the heads' scales k_S and v_S", fn);
   if (!q->lens || (q->cols > 0 && !q->table)) return fail(QF_EINVAL, "%s: null lens or table", fn);
+  if (c->fmt == QF_FMT_NVFP4 && (!aligned_to(c->k_S, 4) || !aligned_to(c->v_S, 4)))
+    return fail(QF_EALIGN, "%s: k_S or v_S not aligned to its elements", fn);
   if (!aligned_to(q->lens, 4) || !aligned_to(q->table, 4) || !aligned_to(q->offsets, 8))
     return fail(QF_EALIGN, "%s: lens, table or offsets not aligned to their elements", fn);
   return QF_OK;

@@ -48,7 +48,8 @@ BAD_CACHE = [(dict(fmt=0), QF_EINVAL), (dict(fmt=3), QF_EINVAL), (dict(pages=-1)
              (dict(page=8), QF_ENOTSUP), (dict(page=48), QF_ENOTSUP), (dict(page=2048), QF_ENOTSUP), (dict(page=0), QF_ENOTSUP),
              (dict(D=96), QF_ENOTSUP), (dict(D=512), QF_ENOTSUP), (dict(D=0), QF_ENOTSUP), (dict(H=1 << 14), QF_ENOTSUP),
              (dict(pages=1 << 31), QF_ENOTSUP), (dict(k_codes=None), QF_EINVAL), (dict(v_scales=None), QF_EINVAL),
-             (dict(k_S=None), QF_EINVAL), (dict(v_S=None), QF_EINVAL), (dict(k_codes=P(8)), QF_EALIGN), (dict(v_scales=P(24)), QF_EALIGN)]
+             (dict(k_S=None), QF_EINVAL), (dict(v_S=None), QF_EINVAL), (dict(k_codes=P(8)), QF_EALIGN), (dict(v_scales=P(24)), QF_EALIGN),
+             (dict(k_S=P(2)), QF_EALIGN), (dict(v_S=P(6)), QF_EALIGN)]
 BAD_SEQS = [(dict(B_=-1), QF_ESHAPE), (dict(cols=-1), QF_ESHAPE), (dict(max_len=-1), QF_ESHAPE), (dict(max_len=1 << 30), QF_ENOTSUP),
             (dict(B_=1 << 28), QF_ENOTSUP), (dict(cols=1 << 31), QF_ENOTSUP), (dict(offsets=None), QF_ESHAPE),
             (dict(lens=None), QF_EINVAL), (dict(table=None), QF_EINVAL), (dict(lens=P(2)), QF_EALIGN), (dict(table=P(6)), QF_EALIGN),
