@@ -341,11 +341,12 @@ __global__ __launch_bounds__(256) void merge_kernel(AttendArgs p) {
       const int s = min(s0 + i * P, p.splits - 1);      // (past the last: the last again, which does not count)
       w[i] = row_sums(p, s, row, D);
       v[i] = *reinterpret_cast<const f32x4_t*>(p.part + (s * R + row) * D + 4 * e);
-      if (s0 + i * P >= p.splits) w[i][0] = neg_inf();
+      if (s0 + i * P >= p.splits) w[i][1] = 0.0f;
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      if (w[i][0] == neg_inf()) continue;               // (a piece without tokens holds no outputs)
+      // (a piece without tokens holds no outputs; its sum says so, for a maximum of -inf has one that saw NaN alone too)
+      if (w[i][1] == 0.0f) continue;
       const float now = fmaxf(top, w[i][0]), down = __builtin_amdgcn_exp2f(top - now), f = __builtin_amdgcn_exp2f(w[i][0] - now);
       l = l * down + f * w[i][1];
       acc = acc * down + f * v[i];
