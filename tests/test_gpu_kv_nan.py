@@ -106,3 +106,43 @@ def test_keys_of_a_whole_piece(qf, fmt, D, lens, new, G, pieces, which):
     ref = c.ref()
     assert np.isnan(ref[1]).any() and np.isfinite(ref[1]).any()
     c.check(*c.run(), ref)
+
+
+@pytest.mark.parametrize("fmt", ["nvfp4", "mxfp4"])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("lens,new,G", [([3, 40], [10, 12], 4), ([30, 300], [60, 200], 3), ([0, 700], [9, 9], 4), ([9, 2700], [60, 50], 3)])
+@pytest.mark.parametrize("spoil", ["query", "scale nan", "scale inf"])
+def test_rows_that_see_nothing(qf, fmt, D, lens, new, G, spoil):
+    """Rows below position zero, among rows that see something: zeros, whatever their queries and the scale are."""
+    c = Call(qf, fmt, lens, new, G, D)
+    empty = new[0] - lens[0]
+    if spoil == "query":
+        c.q[:empty] = np.random.default_rng(0).choice([0x7FC0, 0x7F80, 0xFF80, 0x3F80], c.q[:empty].shape)
+    scale = {"query": None, "scale nan": float("nan"), "scale inf": float("inf")}[spoil]
+    o, l = c.run(scale)
+    assert np.all(o[:empty] == 0) and np.all(l[:empty] == -np.inf)
+    if spoil == "query":
+        c.check(o, l, c.ref())
+    else:
+        assert np.isnan(o[empty:]).all() and np.isnan(l[empty:]).all()
+
+
+@pytest.mark.parametrize("fmt", ["nvfp4", "mxfp4"])
+@pytest.mark.parametrize("lens,new,G", [([150, 90], None, 4), ([150, 90], [12, 30], 4), ([150, 140], [70, 90], 3)])
+def test_tokens_that_are_not_seen(qf, fmt, lens, new, G):
+    """Pages that are none, and a window that lies behind max_len: zeros for queries of NaN too."""
+    c = Call(qf, fmt, lens, new, G, 64)
+    c.table[0] = -5
+    own = c.T // 2 if new is None else new[0]                      # rows of the first sequence
+    c.q[:own] = 0x7FC0
+    o, l = c.run()
+    assert np.all(o[:own] == 0) and np.all(l[:own] == -np.inf)
+    c.check(o, l, c.ref())
+    c = Call(qf, fmt, lens, new, G, 64, window=20, max_len=100)
+    ref = c.ref()
+    blind = ref[1][:, 0] == -np.inf
+    assert blind.any() and not blind.all()
+    c.q[blind] = 0x7F80
+    o, l = c.run()
+    assert np.all(o[blind] == 0) and np.all(l[blind] == -np.inf)
+    c.check(o, l, c.ref())
