@@ -203,7 +203,7 @@ __device__ __forceinline__ void copy_values(const uint8_t* p, int u, int lane, c
 
 // A row of Q as the products take it, lane group g's quarter of D, and the factor that brings its scores to units of
 // log 2: positive and finite, so that hidden scores stay -inf.  A row with an infinity or NaN, or whose factor would be
-// one, is all NaN and its factor 1: its scores are NaN where it sees a token, and nowhere else.
+// one, gets NaNs and the factor 1: its scores are NaN where it sees a token, and nowhere else.
 template <int FMT, int D>
 __device__ __forceinline__ float load_query(const AttendArgs& p, int row_at, int g, float S_k, uint4 (&q)[D / 32]) {
   constexpr int CS = D / 32;
@@ -222,9 +222,6 @@ __device__ __forceinline__ float load_query(const AttendArgs& p, int row_at, int
   top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
   top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
   const int e = (int)(top >> 7) - 127 - 14;             // (zeros and subnormals: any factor will do)
-  const float f = __builtin_ldexpf(__builtin_fabsf(p.a.scale * S_k) * kLog2e, e);
-  const bool nan = top >= 0x7F80u || !__builtin_isfinite(f);
-  const uint32_t two_nans = FMT == QF_FMT_NVFP4 ? 0x7E007E00u : 0x7FC07FC0u;
 #pragma unroll
   for (int s = 0; s < CS; ++s) {
     const uint32_t w[4] = {q[s].x, q[s].y, q[s].z, q[s].w};
@@ -232,10 +229,13 @@ __device__ __forceinline__ float load_query(const AttendArgs& p, int row_at, int
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const float lo = __builtin_ldexpf(codec::as_f32(w[k] << 16), -e), hi = __builtin_ldexpf(codec::as_f32(w[k] & 0xFFFF0000u), -e);
-      o[k] = nan ? two_nans : FMT == QF_FMT_NVFP4 ? pack_f16(lo, hi) : codec::bf16x2_rne_nonnan(lo, hi);
+      o[k] = FMT == QF_FMT_NVFP4 ? pack_f16(lo, hi) : codec::bf16x2_rne_nonnan(lo, hi);
     }
     q[s] = make_uint4(o[0], o[1], o[2], o[3]);
   }
+  const float f = __builtin_ldexpf(__builtin_fabsf(p.a.scale * S_k) * kLog2e, e);
+  const bool nan = top >= 0x7F80u || !__builtin_isfinite(f);
+  q[0].x = nan ? (FMT == QF_FMT_NVFP4 ? 0x7E007E00u : 0x7FC07FC0u) : q[0].x;
   return nan ? 1.0f : f < 0x1p-126f ? 0x1p-126f : f;
 }
 
