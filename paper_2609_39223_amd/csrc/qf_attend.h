@@ -324,10 +324,16 @@ __device__ __forceinline__ float row_max(float x) {
 // One step of the rows' running softmax over the tile's 64 tokens, of which the lane holds scores z of 16 u + 4 g + i: a
 // row sees those from `from` to below `to` that have a page (whole: no lane has to look).  Probabilities go to pw in FP16.
 // (All rows' maxima first, then one branch: taken one row after the other each waits for its own exchanges.)
+// A row whose reference m is kFar or more from zero rounds its scores first, as the reference was, and then takes the
+// difference, which is exact: 14 - m is not exact there, and the reference is off the largest score's exact product
+// by more than FP16 has room for.  It goes by the row's own reference, so that equal scores count the same in every
+// tile.  `far`: some row of the wave is one.  (One branch for all rows: one for each kept their exponents apart, 363 us for 350.)
+constexpr float kFar = 0x1p22f;
+__device__ __forceinline__ bool is_far(float m) { return __builtin_fabsf(m) >= kFar && m != neg_inf(); }
 template <int DT, int NQ>
 __device__ __forceinline__ void softmax_step(float (&z)[NQ][16], const float (&cz)[NQ], const int (&from)[NQ], const int (&to)[NQ],
                                              bool whole, uint32_t bad, int g, float (&m)[NQ], float (&l)[NQ], f32x4_t (&acc)[NQ][DT],
-                                             uint32_t (&pw)[NQ][8]) {
+                                             uint32_t (&pw)[NQ][8], int& far) {
   bool all = whole;
 #pragma unroll
   for (int j = 0; j < NQ; ++j) all = all && to[j] >= kTile && from[j] <= 0;
@@ -351,9 +357,10 @@ __device__ __forceinline__ void softmax_step(float (&z)[NQ][16], const float (&c
     // largest by one (probabilities up to 2^15): fewer steps have to scale what was
     // summed (355 -> 350 us for 2048 new tokens behind 8192).
     top[j] = fmaxf(__builtin_ceilf(row_max(top[j]) * cz[j]), m[j]);
-    grows = grows || top[j] > m[j] + 1.0f;
+    grows = grows || top[j] - m[j] > 1.0f;              // (m + 1 may round up to m + 2)
   }
   if (__any(grows)) {
+    bool any = false;
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {
       const float down = __builtin_amdgcn_exp2f(m[j] - (top[j] == neg_inf() ? 0.0f : top[j]));
@@ -361,16 +368,33 @@ __device__ __forceinline__ void softmax_step(float (&z)[NQ][16], const float (&c
 #pragma unroll
       for (int d = 0; d < DT; ++d) acc[j][d] *= down;
       m[j] = top[j];
+      any = any || is_far(m[j]);
     }
+    far = __builtin_amdgcn_readfirstlane(__any(any));
+  }
+  float by[NQ], up[NQ];
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    by[j] = cz[j];
+    up[j] = m[j] == neg_inf() ? 0.0f : kUp - m[j];      // (nothing seen yet: probabilities of zero)
+  }
+  if (__builtin_expect(far, 0)) {
+#pragma unroll
+    for (int j = 0; j < NQ; ++j)
+      if (is_far(m[j])) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) z[j][i] = z[j][i] * by[j] - m[j];
+        up[j] = kUp;
+        by[j] = 1.0f;
+      }
   }
 #pragma unroll
   for (int j = 0; j < NQ; ++j) {
-    const float up = m[j] == neg_inf() ? 0.0f : kUp - m[j];       // (nothing seen yet: probabilities of zero)
     float sum[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
-      const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][i], cz[j], up));
-      const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][i + 1], cz[j], up));
+      const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][i], by[j], up[j]));
+      const float b = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][i + 1], by[j], up[j]));
       sum[0] += a;
       sum[1] += b;
       pw[j][i / 2] = pack_f16(a, b);

@@ -162,6 +162,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 && D == 256 ? 1 : NQ == 2 || D
   __syncthreads();
 
   float m[NQ], l[NQ];
+  int far = 0;
   f32x4_t acc[NQ][DT];
 #pragma unroll
   for (int j = 0; j < NQ; ++j) {
@@ -222,7 +223,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 && D == 256 ? 1 : NQ == 2 || D
         from[j] = p.window > 0 ? row_pos[j] - p.window + 1 - base : 0;
         to[j] = min(row_pos[j] + 1 - base, todo - t0);
       }
-      softmax_step<DT>(z, cz, from, to, whole, bad_now, g, m, l, acc, pw);
+      softmax_step<DT>(z, cz, from, to, whole, bad_now, g, m, l, acc, pw, far);
       // ---- outputs
       asm volatile("" ::: "memory");
       __builtin_amdgcn_s_waitcnt(0x0F70);               // vmcnt(0): this wave's copies of V are in its region

@@ -159,6 +159,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_rows_kernel(AttendArgs 
 
   uint4 q[NQ][CS];
   float cz[NQ], m[NQ], l[NQ];
+  int far = 0;
   f32x4_t acc[NQ][DT];
   const float S_k = FMT == QF_FMT_NVFP4 ? c.S[0][h] : 1.0f;
 #pragma unroll
@@ -235,7 +236,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void attend_rows_kernel(AttendArgs 
         from[j] = p.window > 0 ? row_pos[j] - p.window + 1 - base : 0;
         to[j] = min(row_pos[j] + 1 - base, todo - t0);
       }
-      softmax_step<DT>(z, cz, from, to, whole, bad, g, m, l, acc, pw);
+      softmax_step<DT>(z, cz, from, to, whole, bad, g, m, l, acc, pw, far);
       __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
