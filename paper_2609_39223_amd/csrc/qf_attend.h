@@ -207,7 +207,7 @@ __device__ __forceinline__ void copy_values(const uint8_t* p, int u, int lane, c
 template <int FMT, int D>
 __device__ __forceinline__ float load_query(const AttendArgs& p, int row_at, int g, float S_k, uint4 (&q)[D / 32]) {
   constexpr int CS = D / 32;
-  const uint32_t flip = p.a.scale * S_k < 0.0f ? 0x80008000u : 0u;
+  const uint32_t flip = (p.a.scale < 0.0f) != (S_k < 0.0f) ? 0x80008000u : 0u;
   const int t = row_at / (int)p.a.Hq, hq = row_at - t * (int)p.a.Hq;
   const uint16_t* const src = p.a.Q + t * p.a.ldq + (int64_t)hq * D + g * (D / 4);
   uint32_t top = 0;
@@ -233,7 +233,15 @@ __device__ __forceinline__ float load_query(const AttendArgs& p, int row_at, int
     }
     q[s] = make_uint4(o[0], o[1], o[2], o[3]);
   }
-  const float f = __builtin_ldexpf(__builtin_fabsf(p.a.scale * S_k) * kLog2e, e);
+  // (mantissas and exponents apart: scale S_k alone may be out of range or have few bits left)
+#if defined(__HIP_DEVICE_COMPILE__)
+  const float a = __builtin_amdgcn_frexp_mantf(p.a.scale) * __builtin_amdgcn_frexp_mantf(S_k);
+  const int ea = __builtin_amdgcn_frexp_expf(p.a.scale) + __builtin_amdgcn_frexp_expf(S_k);
+#else
+  const float a = 0.0f;
+  const int ea = 0;
+#endif
+  const float f = __builtin_ldexpf(__builtin_fabsf(a) * kLog2e, e + ea);
   const bool nan = top >= 0x7F80u || !__builtin_isfinite(f);
   q[0].x = nan ? (FMT == QF_FMT_NVFP4 ? 0x7E007E00u : 0x7FC07FC0u) : q[0].x;
   return nan ? 1.0f : f < 0x1p-126f ? 0x1p-126f : f;

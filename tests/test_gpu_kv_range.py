@@ -76,3 +76,27 @@ def test_scores_of_any_size(qf, fmt, lens, new, G, size, one):
                     top = z[t, h, g] * (2 if twice else 1)
                     lbound = (D + 16) * U * big[t, h, g] * 2 + (n / 4 + 80) * U + 4 * U * abs(top)
                     assert abs(l[t, h, g] - (top + np.log(n))) <= lbound, (t, h, g)
+
+
+@pytest.mark.parametrize("lens,new,G", CALLS)
+@pytest.mark.parametrize("scale,S,query", [(1.3 * 2.0 ** -100, 2.0 ** -46, 2.0 ** 127), (-(2.0 ** -110), 2.0 ** -43, 2.0 ** 127),
+                                           (2.0 ** -149, 2.0 ** 20, 2.0 ** 119), (2.0 ** 90, 2.0 ** 39, 2.0 ** -126),
+                                           (-(2.0 ** 90), 2.0 ** 39, 2.0 ** -126)])
+def test_scales_that_meet_in_the_middle(qf, lens, new, G, scale, S, query):
+    """A scale times a head's tensor scale outside FP32's range, or where it has few bits left, times queries that bring
+    the scores back to ordinary size."""
+    D, H, page = 256, 2, 16
+    rng = np.random.default_rng(3)
+    B, cols, T = len(lens), -(-max(lens) // page), len(lens) if new is None else sum(new)
+    table, offsets = kc.table(rng, B, cols, B * cols), None if new is None else kc.offsets_of(new)
+    k, v = kc.pool(rng, "nvfp4", B * cols, H, page, D), kc.pool(rng, "nvfp4", B * cols, H, page, D)
+    k[0][:] &= 0x77                                                # (all positive, so that 256 of them add up)
+    k[1][:] = rng.integers(0x08, 0x10, k[1].shape) if query < 1 else rng.integers(0x70, 0x7E, k[1].shape)
+    k = k[0], k[1], np.full(H, S, np.float32)
+    qh = np.full((T, H * G * D), int(np.float32(query).view(np.uint32)) >> 16, np.uint16)
+    qh[:, ::5] -= 0x20                                             # (some a little smaller)
+    ref = sv.attention(bf16_to_f64(qh).reshape(T, H * G, D), sv.values(*k, "nvfp4"), sv.values(*v, "nvfp4"), offsets, lens, table,
+                       scale)
+    assert 2.0 ** -10 < np.abs(ref[2]).max() < 2.0 ** 10
+    o, l = _attend(qf, _cache(qf, "nvfp4", k, v), _seqs(qf, lens, table, offsets), to_dev(qh), H, D, H * G, scale)
+    _check(o, l, ref, max(lens), D)
