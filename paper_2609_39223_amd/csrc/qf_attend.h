@@ -458,14 +458,14 @@ __device__ __forceinline__ void emit_row(const AttendArgs& p, int split, int row
     if (g == 0) row_sums(p, split, row_at, D) = f32x2_t{m, l};
     return;
   }
-  const float f = l == 0.0f ? 0.0f : (FMT == QF_FMT_NVFP4 ? p.c.S[1][h] : 0x1p-6f) / l;
+  const float f = 1.0f / l, S = FMT == QF_FMT_NVFP4 ? p.c.S[1][h] : 0x1p-6f;   // (S / l may have few bits left)
   const int t = row_at / (int)p.a.Hq;
   uint16_t* const to = p.a.O + t * p.a.ldo + (int64_t)(row_at - t * (int)p.a.Hq) * D + 4 * g;
 #pragma unroll
   for (int d = 0; d < D / 16; ++d) {
     uint32_t w[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = codec::bf16_rne(l == 0.0f ? 0.0f : acc[d][k] * f);
+    for (int k = 0; k < 4; ++k) w[k] = codec::bf16_rne(l == 0.0f ? 0.0f : acc[d][k] * f * S);
     *reinterpret_cast<uint2*>(to + 16 * d) = make_uint2(w[0] | (w[1] << 16), w[2] | (w[3] << 16));
   }
   if (p.a.lse && g == 0) p.a.lse[row_at] = l == 0.0f ? neg_inf() : (m + (__builtin_log2f(l) - kUp)) * kLn2;

@@ -375,10 +375,10 @@ __global__ __launch_bounds__(256) void merge_kernel(AttendArgs p) {
       l += f * l_of[i];
     }
   }
-  const float f = l == 0.0f ? 0.0f : (FMT == QF_FMT_NVFP4 ? p.c.S[1][hq / p.G] : 0x1p-6f) / l;
+  const float f = 1.0f / l, S = FMT == QF_FMT_NVFP4 ? p.c.S[1][hq / p.G] : 0x1p-6f;   // (S / l may have few bits left)
   uint32_t w[4];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) w[k] = codec::bf16_rne(l == 0.0f ? 0.0f : acc[k] * f);
+  for (int k = 0; k < 4; ++k) w[k] = codec::bf16_rne(l == 0.0f ? 0.0f : acc[k] * f * S);
   *reinterpret_cast<uint2*>(p.a.O + t * p.a.ldo + (int64_t)hq * D + 4 * e) = make_uint2(w[0] | (w[1] << 16), w[2] | (w[3] << 16));
   if (p.a.lse && e == 0) p.a.lse[row] = l == 0.0f ? neg_inf() : (top + (__builtin_log2f(l) - kUp)) * kLn2;
 }

@@ -100,3 +100,21 @@ def test_scales_that_meet_in_the_middle(qf, lens, new, G, scale, S, query):
     assert 2.0 ** -10 < np.abs(ref[2]).max() < 2.0 ** 10
     o, l = _attend(qf, _cache(qf, "nvfp4", k, v), _seqs(qf, lens, table, offsets), to_dev(qh), H, D, H * G, scale)
     _check(o, l, ref, max(lens), D)
+
+
+@pytest.mark.parametrize("D", [64, 256])
+@pytest.mark.parametrize("lens,new,G", CALLS)
+@pytest.mark.parametrize("S", [2.0 ** -100, 2.0 ** -118, 2.0 ** -124])
+def test_heads_of_tiny_values(qf, D, lens, new, G, S):
+    """Values near the least normal number come out as precise as any."""
+    H, page = 2, 16
+    rng = np.random.default_rng(4)
+    B, cols, T = len(lens), -(-max(lens) // page), len(lens) if new is None else sum(new)
+    table, offsets = kc.table(rng, B, cols, B * cols), None if new is None else kc.offsets_of(new)
+    k, v = kc.pool(rng, "nvfp4", B * cols, H, page, D), kc.pool(rng, "nvfp4", B * cols, H, page, D)
+    v = v[0], v[1], np.full(H, S, np.float32)
+    qh = workloads.normal_bf16(rng, (T, H * G * D))
+    ref = sv.attention(bf16_to_f64(qh).reshape(T, H * G, D), sv.values(*k, "nvfp4"), sv.values(*v, "nvfp4"), offsets, lens, table,
+                       D ** -0.5)
+    o, l = _attend(qf, _cache(qf, "nvfp4", k, v), _seqs(qf, lens, table, offsets), to_dev(qh), H, D, H * G)
+    _check(o, l, ref, max(lens), D)
