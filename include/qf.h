@@ -813,8 +813,9 @@ QF_API qf_status qf_kv_write(const qf_kv_cache* c, const qf_kv_seqs* q, int64_t 
 
 /*
  * qf_kv_read -- the inverse: the rows' keys and values as the cache holds them, x_hat of the quantizers bit
- * for bit, zeros for a row without a place; rows that belong to nobody are left alone.  K or V may be
- * NULL.  With offsets the prefix sums of lens, whole sequences.  max_len is not used.
+ * for bit (blocks with the NaN scale read as NaN, where the NVFP4 quantizer's own x_hat takes that code for
+ * 480), zeros for a row without a place; rows that belong to nobody are left alone.  K or V may be NULL.
+ * With offsets the prefix sums of lens, whole sequences.  max_len is not used.
  */
 QF_API qf_status qf_kv_read(const qf_kv_cache* c, const qf_kv_seqs* q, int64_t T, uint16_t* K,
                             int64_t ldk, uint16_t* V, int64_t ldv, qf_stream_t stream);
