@@ -789,7 +789,8 @@ typedef struct {
  *            row offsets[b] + i is the token at position lens[b] - n + i of its n rows.
  *   table    int32 [B, cols]: the page of tokens j page .. j page + page - 1 of sequence b in table[b][j].
  *            Entries that a sequence does not reach are not read; one outside 0 .. pages - 1 is no page.
- *   max_len  no sequence is longer (the caller's word, so that launches need not provide for more).
+ *   max_len  no sequence is longer (the caller's word, so that launches need not provide for more).  Attention
+ *            shares its work out by it: sequences far shorter than it says take longer than under a near bound.
  * lens and table 4-byte aligned, offsets 8-byte aligned.  Limits: T < 2^28, B < 2^28, max_len < 2^30.
  */
 typedef struct {
@@ -832,8 +833,11 @@ QF_API qf_status qf_kv_read(const qf_kv_cache* c, const qf_kv_seqs* q, int64_t T
  * Tokens without a page are not seen, positions from max_len on neither; rows that belong to nobody are
  * left alone.  K and V count as their codes decode (not rounded to bf16); sums, maxima and normalizers are
  * FP32, probabilities are rounded to FP16 relative to the row's largest (2^-11 each, 2^-38 absolute).
- * A NaN or infinity in q makes its row NaN; NaN scales reach the rows that see their tokens, and no others.
- * MXFP4 values of 2^100 or more may come out infinite; blocks of V with scale code 0 count as zeros.
+ * A NaN or infinity in q makes its row NaN if it sees a token; NaN scales reach the rows that see their tokens, and
+ * no others.  Scores count as FP32 holds them, however large.
+ * MXFP4 values of 2^100 or more may come out infinite or NaN; blocks of V with scale code 0 count as zeros.
+ * With offsets, the kernel and its pieces are chosen by the call's average number of rows: a prompt and single
+ * tokens of long sequences take least time in calls of their own.
  *   ws     qf_kv_attention_workspace_size bytes of the same cache sizes, sequences' sizes (B, cols, max_len,
  *          with or without offsets), T, Hq and window, 256-byte aligned; may be NULL where that is 0.
  * O must not overlap Q or the cache; calls that may run at the same time need workspaces of their own.
@@ -874,7 +878,8 @@ typedef struct {
  *   ws     qf_lora_rows_workspace_size bytes, 256-byte aligned.
  * Calls that may run at the same time need workspaces of their own.
  * Rows of an adapter may lie anywhere; they cost least side by side.  FP32 sums in a fixed order; X A^T is
- * taken into the second product as the sum of two bf16 halves (2^-17 relative), Y rounded once.
+ * taken into the second product as the sum of two bf16 halves (2^-17 relative), Y rounded once.  An infinity in
+ * B makes the outputs that it reaches NaN.
  * Limits: M < 2^24, N < 2^24, K < 2^30, n < 2^30.
  */
 QF_API qf_status qf_lora_rows_workspace_size(const qf_adapters* a, int64_t M, size_t* bytes);

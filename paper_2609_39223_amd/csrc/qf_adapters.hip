@@ -201,8 +201,10 @@ constexpr int kDownLds = kDownWaves * (kDownStaged<TILES, HALVES> ? (TILES + 1) 
 // z of adapter a's rows among 16; each wave a part of the slice, 128 k at once.  Of many rows and 17 to 32 ranks 128 bytes
 // a row are loaded, by eight lanes each, and go through LDS to the lanes that multiply them (staged; 4099 rows of 6
 // adapters, rank 32, K 4096: 18.7 us; loaded as they are multiplied, 64 bytes of 16 rows, every line is asked for
-// twice: 28.5).  Elsewhere the way through LDS costs more than it saves (in all, staged and not: 4000 rows of 200
-// adapters, rank 16, 80.5 and 70.9 us; of 9, rank 256, 235 and 185; 61 rows of 24, rank 64, 20.5 and 17.2).
+// twice: 28.5).  Elsewhere the way through LDS costs more than it saves.  4000 rows, 4096 -> 8192, the whole call in us,
+// staged / not:  of 6 adapters, ranks 16, 32, 64, 128, 256:  62 / 59   58 / 68   110 / 101   175 / 149   309 / 238
+//                of 200, mixed:                               83 / 73   89 / 94   182 / 158   334 / 281   651 / 539
+// (and 61 rows of 24, rank 64, 20.5 / 17.2).
 template <int TILES, bool HALVES>
 __device__ __forceinline__ void down_rows(const RowsArgs& p, char* smem, const Group& grp, int a, int slice, int j0) {
   const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4;
@@ -607,9 +609,11 @@ Plan plan_of(const AdapterSet& s, int64_t M) {
   p.sorted = M > kFew && M <= kSortRows && s.n <= kSortAdapters;
   p.rb = M <= kFew ? 0 : M / n >= 64 ? 2 : 1;
   p.groups = p.rb == 0 ? 1 : (M + 16 * p.rb - 1) / (16 * p.rb);
-  // adapters among 16 sorted rows, one more than there would be if every group began with a new one, side by side
-  // (100 rows of 10 adapters, 4096 x 8192: 25.5 -> 17.1 us, 2048 of 100: 43.6 -> 38.1), unless there are workgroups
-  // enough without the last, which few groups need (4099 of 6, 24576 wide: down 28 us then, with it 35)
+  // adapters among 16 sorted rows, one more than there would be if every group began with a new one, side by side, unless
+  // there are workgroups enough without the last, which few groups need.  Rank 16, 4096 -> 8192, us with / without it:
+  // 100 rows of 10 adapters 17 / 26, 1000 of 30 25 / 33, 2048 of 6 32 / 39, of 100 37 / 42, 2900 of 6 43 / 44,
+  // of 100 59 / 56, 4099 of 6 62 / 59, of 100 75 / 70.  n counts the adapters that are there, not those in use
+  // (which only the device knows).
   p.abreast = p.rb == 0 ? (int)n : (int)std::min<int64_t>({16, n, 1 + (16 * n + (M < 12 * cus ? M - 1 : 0)) / M});
   const int64_t each = p.groups * p.abreast, want = (2 * cus + each - 1) / each;
   // slices of K for few rows, 1024 each (61 rows, K 4096, us by slices of 4096 / 2048 / 1024 / 512 / 256: 26.6 / 20.0 /

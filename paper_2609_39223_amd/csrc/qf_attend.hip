@@ -23,9 +23,11 @@
 // largest and absolute 2^-38 of it below, so that many small ones still sum.  The sum of
 // probabilities is of the unrounded ones, in FP32.
 // Bound by memory where the batch fills the card: 64 sequences x 8192 tokens x 8 heads of 128 (NVFP4, 4 rows a
-// head) 115 us, 5.3 TB/s; its loads alone take 103.  One sequence of 131072: 39 us, 3.9 TB/s, loads alone 33.  With
+// head) 117 us, 5.2 TB/s (MXFP4 114); its loads alone take 103.  One sequence of 131072: 39 us, 3.9 TB/s, loads alone 33.  With
 // several rows a head (5 drafted tokens) by the softmax, 16 exponents a lane, row and 64 tokens, and by what
-// decoding costs each wave; short sequences by trips to memory one after the other (row, length, page, codes), 7 us.
+// decoding costs each wave; short sequences by trips to memory one after the other (row, length, page, codes), 7 us.  Prompts with heads of
+// 256 (32 rows that each wave decodes for, one wave a SIMD: 2048 new tokens behind 8192, NVFP4, 1276 us, 0.48 PFLOP/s) by
+// what that wave does one after the other, vector units half of the time, matrix units a fifth.
 // What did not pay: four or two workgroups a compute unit for three (registers spilled at 128: 127 us for 117),
 // waves taking every fourth tile of the piece instead of a quarter of it (129), workgroups of 8 or 16 waves
 // (129 - 144), 64 rows a wave.

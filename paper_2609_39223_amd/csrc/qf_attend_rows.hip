@@ -9,7 +9,7 @@
 // codes are on their way are three different ones, so there is one barrier a tile:
 //   step k   copies of V's codes of tile k + 2 to LDS, its scales to FP16 in LDS; K's codes of k + 1 (loaded in
 //            step k - 1) and V's (in LDS since then) decoded; tile k multiplied.
-// 2048 new tokens behind 8192, 32 heads over 8, 128 wide (NVFP4): 350 us, 0.88 PFLOP/s; 32 rows a wave that each decode
+// 2048 new tokens behind 8192, 32 heads over 8, 128 wide (NVFP4): 353 us, 0.88 PFLOP/s (MXFP4 374); 32 rows a wave that each decode
 // for themselves took 502, 16 rows 601, 64 rows 608.  Bound by what the two waves of a SIMD do one after the other:
 // vector units busy half of the time (per row and token an exponent, a maximum, a sum, conversions; the decode),
 // matrix units 30 %, LDS 30 % (32 KB of operands a wave and tile).  Scores of the next tile between the

@@ -7,7 +7,8 @@
 // memory one after the other), and leaves them in LDS; rows to be written are loaded meanwhile.  NVFP4's tensor
 // scale S is given per head, so one pass suffices.  Bound by memory: 2 bytes an element one way, 0.53 or 0.56
 // the other; few tokens by the trips.  32768 tokens x 1024 of K and of V read back (MXFP4): 41 us, 4.1 TB/s;
-// 13600 x 1024 written (NVFP4): 27 us, 2.6 TB/s, the vector units nearly as busy (maxima, a division, 16 codes).
+// 15852 x 1024 written: 27.5 us, 3.0 TB/s (NVFP4), 25.7 (MXFP4), waiting: the places' trips, the rows, the codes and the
+// stores come one after the other.  The vector units are busy 35 % of it, 23 % in MXFP4.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -62,7 +63,7 @@ struct Nvfp4Known {
 
 // Codes and scale bytes of N chunks.  NVFP4: the two lanes of a block share the scales' work, the even one takes
 // chunks 0, 2 .., the odd one chunks 1, 3 .., and each hands the other its results (two divisions a block instead of
-// a lane; 13600 tokens x 2048: 34 -> 32 us).
+// a lane; 15852 tokens x 2048: 34 -> 32 us).
 template <int FMT, int N>
 __device__ __forceinline__ void encode(const uint4 in[N], float S, uint32_t cw[N], uint32_t sc[N]) {
   uint32_t h[8], xh[8];
@@ -117,7 +118,7 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(KvRows p) {
       if (has && t0 + mine + i * abreast < p.q.T) in[i] = *reinterpret_cast<const uint4*>(row + i * step);
     }
   };
-  // (several rows behind the places: in front of them each trip waited for the rows, 13600 tokens took 32 us for 27)
+  // (several rows behind the places: in front of them each trip waited for the rows, 15852 tokens took 32 us for 27)
   if (!READ && N == 1) load();
   if ((int)threadIdx.x < abreast * N) places[threadIdx.x] = kv_place(p.c, p.q, t0 + threadIdx.x);
   const float S = FMT == QF_FMT_NVFP4 ? p.c.S[v][h] : 1.0f;
@@ -194,7 +195,7 @@ hipError_t launch_n(KvRows p, hipStream_t s) {
 // Tokens a lane takes, by lanes of one token each in units of two workgroups a compute unit (8 heads of 128; us,
 // writing / reading NVFP4):  4 units (2048 tokens)  1: 12.2 / 5.9   2: 11.5 / 5.6
 //   8 (4096)  1: 18.9 / 8.7   2: 14.6 / 6.7   8: 16.3 / 7.4     16 (8192)  2: 23.6 / 11.6   8: 22.7 / 10.2
-// (4 a lane at 13600 tokens: 49.0 us for both directions, 16: 50.1, 8: 48.1.)
+// (4 a lane at 15852 tokens: 49.0 us for both directions, 16: 50.1, 8: 48.1.)
 template <int FMT, bool READ>
 hipError_t launch_rows(const KvRows& p, hipStream_t s) {
   const int64_t lanes = p.q.T * (2 * p.c.H * p.c.D / 8), unit = 512 * compute_units();
